@@ -24,6 +24,13 @@
  *                        (App. A), also as one orbit patch over orderings
  *                        (Sec. 5, reorder).
  *
+ * and, for the program that goes on to answer from the cache:
+ *
+ *   kamera_page_tables   pages and token slots for requests that grow;
+ *   kamera_append_paged8 bf16 K, V rows into a paged cache held in 8 bits;
+ *   kamera_select_pages  the pages a query needs most, by a cheap score;
+ *   kamera_attend_paged  attention over the paged cache (8 bits or bf16).
+ *
  * Conventions shared by every entry point
  *   - Every tensor pointer is a DEVICE pointer owned by the caller.  The
  *     library never allocates, frees or synchronises; a call enqueues its
@@ -400,6 +407,255 @@ int kamera_shift(const kamera_shift_args* args, void* stream);
 int kamera_scatter_paged(const kamera_scatter_args* args, void* stream);
 int kamera_gather_paged(const kamera_scatter_args* args, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Serving from the paged cache: pages for requests, the cache in 8 bits, and
+ * attention over it.
+ *
+ * The 8-bit cache.  A page holds page_size (16, 32 or 64) tokens of one layer
+ * as e4m3 bytes (4 exponent and 3 fraction bits, largest value 448, no
+ * infinity; NaN is 0x7f / 0xff), with ONE fp32 scale for each (page, KV head)
+ * and plane: value = byte * scale.  Scales are powers of two, 2^e with
+ * -100 <= e <= 120, and e is the least exponent at which the page's largest
+ * finite magnitude is at most 448 * 2^e.  A byte's value, its scaling to bf16
+ * and a later change of e by whole steps are therefore exact wherever the
+ * byte stays a normal number, and none of it depends on an order of summation:
+ * the stored bytes are a function of the rows alone.
+ * Element (layer l, page p, token t of the page, head h, column j) is at
+ *   base + l*stride[0] + p*stride[1] + t*stride[2] + h*stride[3] + j,
+ * any strides that are multiples of 16 bytes (e.g. [layer][page][head][token]
+ * [dim], which keeps what one (page, head) needs together, or the row order
+ * [layer][slot][head][dim] of the bf16 pool).
+ * ------------------------------------------------------------------------ */
+
+/* further bits of the optional device status word */
+#define KAMERA_STATUS_NO_PAGE 2u     /* the free list ran out                  */
+#define KAMERA_STATUS_BAD_LENGTH 4u  /* a request outgrew its page-table row   */
+
+/* Most requests of one kamera_page_tables call. */
+#define KAMERA_MAX_REQUESTS 8192
+/* Most pages of one request in kamera_select_pages (scores are kept in LDS). */
+#define KAMERA_MAX_SELECT_PAGES 32768
+/* Most query heads that share a KV head. */
+#define KAMERA_MAX_GROUP 64
+
+/* kamera_page_tables -- pages and token slots for requests that grow from
+ * tokens_before[r] to tokens_after[r] cached tokens (negative counts as 0; a
+ * request that shrinks does not move).  Request r needs
+ *   ceil(after / page_size) - ceil(before / page_size)
+ * pages; they are taken from free_pages[free_begin ..) in request order and
+ * written to page_table[r][ceil(before / page_size) ..); entries of pages
+ * already held are left alone.  free_end[0] receives the place of the first
+ * page not taken.  token_base[r] receives the number of new tokens of the
+ * requests before r, token_base[n_requests] their sum (the row base of each
+ * request in a packed batch of new tokens); slots[token_base[r] + i] the pool
+ * slot page * page_size + offset of new token i of request r, and every entry
+ * of slots past the sum -1.
+ * Where the free list ends the remaining entries are -1, as are the slots in
+ * them (KAMERA_STATUS_NO_PAGE); a page number outside the pool gives -1
+ * (KAMERA_STATUS_BAD_PAGE); a request is cut at pt_stride pages
+ * (KAMERA_STATUS_BAD_LENGTH), and its further tokens have no slot entry.
+ * No output may overlap an input or another output, except that page_table is
+ * both. */
+typedef struct {
+  int32_t n_requests;            /* 0 .. KAMERA_MAX_REQUESTS                   */
+  int32_t page_size;             /* > 0; n_requests * pt_stride * page_size    */
+  int32_t pt_stride;             /*   must be below 2^31                       */
+  int32_t n_pool_pages;
+  const int32_t* tokens_before;  /* device [n_requests], or NULL = 0           */
+  const int32_t* tokens_after;   /* device [n_requests]                        */
+  const int32_t* free_pages;     /* device [n_free]                            */
+  int32_t n_free;
+  const int32_t* free_begin;     /* device [1], or NULL = 0                    */
+  int32_t* free_end;             /* device [1]                                 */
+  int32_t* page_table;           /* device [n_requests][pt_stride]             */
+  int32_t* token_base;           /* device [n_requests + 1]                    */
+  int64_t* slots;                /* device [n_slots], or NULL                  */
+  int64_t n_slots;
+  uint32_t* status;
+} kamera_page_tables_args;
+
+/* kamera_append_paged8 -- n = chunk_tokens[c] (n_tokens if NULL) bf16 K and V
+ * rows of every chunk c and layer into the 8-bit cache, behind the
+ * tokens_before[c] (0 if NULL) tokens that the chunk's pages hold already:
+ * row i becomes token tokens_before[c] + i, in page page_table[c][token /
+ * page_size].  Rows are read as in kamera_shift: token i of chunk c at
+ *   k + c*k_stride[0] + l*k_stride[1] + (row_base[c] + i)*k_stride[2]
+ *     + h*k_stride[3]                                   (row_base NULL = 0).
+ * A page that receives rows takes the exponent e of its new rows' largest
+ * finite magnitude; a page that held tokens before keeps its own where that
+ * is larger, and is otherwise brought to the new one (bytes rounded to
+ * nearest even where they leave the normal range).  Elements are rounded to
+ * the nearest e4m3 value, ties to even; infinities and NaN are stored as NaN
+ * and take no part in e.  Slots past the last token are not written.
+ *
+ * k_sum (with k_sum_scale; both or neither): when a page is filled, the sum
+ * of its page_size keys, column by column, as int8 with one power-of-two
+ * scale: t = sum of the bytes' values (NaN counts as 0; exact in fp32),
+ * f the least exponent (>= -100) with max |t| <= 127 * 2^f,
+ *   k_sum[j] = round(t[j] * 2^-f) (ties to even), k_sum_scale = scale * 2^f
+ * (fp32: 0 for a page of zeros).
+ * kamera_select_pages scores pages by it.
+ * A page may receive rows of one chunk only. */
+typedef struct {
+  int32_t n_chunks;
+  int32_t n_layers;
+  int32_t n_heads;               /* KV heads                                   */
+  int32_t head_dim;              /* 64 or 128                                  */
+  int32_t n_tokens;              /* most new tokens of a chunk                 */
+  int32_t page_size;             /* 16, 32 or 64                               */
+  int32_t pt_stride;
+  int32_t n_pool_pages;
+  const int32_t* chunk_tokens;   /* device [n_chunks], or NULL                 */
+  const int32_t* tokens_before;  /* device [n_chunks], or NULL                 */
+  const int32_t* row_base;       /* device [n_chunks], or NULL                 */
+  const int32_t* page_table;     /* device [n_chunks][pt_stride]               */
+  const void* k;
+  int64_t k_stride[4];           /* chunk, layer, row, head                    */
+  const void* v;
+  int64_t v_stride[4];
+  void* k_cache;
+  int64_t k_cache_stride[4];     /* layer, page, token, head                   */
+  void* v_cache;
+  int64_t v_cache_stride[4];
+  float* k_scale;
+  int64_t k_scale_stride[3];     /* layer, page, head                          */
+  float* v_scale;
+  int64_t v_scale_stride[3];
+  int8_t* k_sum;                 /* optional                                   */
+  int64_t k_sum_stride[3];       /* layer, page, head (multiples of 16)        */
+  float* k_sum_scale;
+  int64_t k_sum_scale_stride[3];
+  uint32_t* status;
+} kamera_append_args;
+
+/* kamera_select_pages -- for one query token a request and every KV head, the
+ * n_keep pages of the request (of the first ceil(kv_tokens / page_size)) that
+ * matter most, as ascending page indices into its page-table row; fewer, where
+ * the request has fewer.  sel[r][h][0 .. sel_count[r][h]) receives them, the
+ * rest of the n_keep entries -1.  The first n_first and the last n_last pages
+ * are always among them (the last one need not be full); the others are ranked
+ * by
+ *   score(p) = (max over the group's query heads g of
+ *               sum_j q8[g][j] * k_sum[p][h][j]) * k_sum_scale[p][h],
+ * ties to the lower index.  q8 is the group's query rows as int8 with one
+ * power-of-two scale: round(q * 2^-f), ties to even, f the least exponent
+ * (>= -100) at which the group's largest finite magnitude is at most 127 * 2^f;
+ * what is not finite counts as 0.  The integer sums are exact, so the
+ * selection is one answer, whatever computes it.  A page number outside the
+ * pool is flagged and its page ranked last. */
+typedef struct {
+  int32_t n_requests;
+  int32_t n_q_heads;             /* a multiple of n_kv_heads; group <= 64      */
+  int32_t n_kv_heads;
+  int32_t head_dim;              /* 64 or 128                                  */
+  int32_t n_keys;                /* most cached tokens of a request            */
+  int32_t page_size;
+  int32_t pt_stride;
+  int32_t n_pool_pages;
+  const int32_t* kv_tokens;      /* device [n_requests], at most n_keys        */
+  const int32_t* page_table;     /* device [n_requests][pt_stride]             */
+  const void* q;                 /* bf16, request r, head g at                 */
+  int64_t q_stride[2];           /*   q + r*q_stride[0] + g*q_stride[1]        */
+  const int8_t* k_sum;
+  int64_t k_sum_stride[2];       /* page, head                                 */
+  const float* k_sum_scale;
+  int64_t k_sum_scale_stride[2];
+  int32_t n_keep;                /* >= n_first + n_last                        */
+  int32_t n_first;               /* >= 0                                       */
+  int32_t n_last;                /* >= 1                                       */
+  int32_t* sel;                  /* device [n_requests][n_kv_heads][n_keep]    */
+  int32_t* sel_count;            /* device [n_requests][n_kv_heads]            */
+  uint32_t* status;
+} kamera_select_args;
+
+typedef enum {
+  KAMERA_CACHE_BF16 = 0,         /* the pool that kamera_rehydrate writes      */
+  KAMERA_CACHE_E4M3 = 1          /* the 8-bit cache of kamera_append_paged8    */
+} kamera_cache_type;
+
+/* kamera_attend_paged -- softmax attention of a batch of requests over one
+ * layer of the paged cache.  Request r has n = q_tokens[r] (n_queries if NULL)
+ * query tokens, rows q_base[r] + i (r*n_queries + i if NULL) of q and out, and
+ * kv = kv_tokens[r] tokens in the cache, its queries' own included.  Query
+ * head g reads KV head g / (n_q_heads / n_kv_heads):
+ *   out[i][g] = sum_t p[t] V[t],  p = softmax over the seen t of
+ *               scale * <q[i][g], K[t]>,
+ * where query i sees the keys t in [0, kv), with causal = 1 those with
+ * t <= kv - n + i, and with window > 0 (causal only) of these the last
+ * `window`.  A row that sees no key gets 0 (and lse = -infinity).  What a row
+ * does not see does not touch it, whatever it holds.  lse (optional, fp32)
+ * receives the natural logarithm of sum exp(scale * <q, K[t]>) at
+ * lse + row*lse_stride[0] + g*lse_stride[1]; with it, results over parts of a
+ * context can be joined.
+ * Scores, softmax statistics and sums are fp32; p is rounded to bf16 for the
+ * product with V, the output once to bf16.
+ *
+ * sel (optional; n_queries must be 1): only the pages sel[r][h][0 ..
+ * sel_count[r][h]) (indices into the page-table row, as kamera_select_pages
+ * writes them) are read.
+ * Keys in pages whose number is outside the pool are not seen (and flagged).
+ *
+ * Work is split over the keys where there are few rows: n_splits parts a row
+ * (0: chosen from the sizes), joined by a second kernel on the same stream.
+ * workspace then holds the parts: device memory of at least
+ * kamera_attend_workspace(args) bytes, 16-byte aligned, not used by other work
+ * at the same time; its contents need not be kept or cleared.
+ * Outputs must not overlap inputs, the workspace or each other. */
+typedef struct {
+  int32_t n_requests;
+  int32_t n_q_heads;             /* a multiple of n_kv_heads; group <= 64      */
+  int32_t n_kv_heads;
+  int32_t head_dim;              /* 64 or 128                                  */
+  int32_t n_queries;             /* most query tokens of a request             */
+  int32_t n_keys;                /* most cached tokens of a request            */
+  int32_t page_size;             /* a multiple of 16                           */
+  int32_t pt_stride;
+  int32_t n_pool_pages;
+  int32_t cache_type;            /* kamera_cache_type                          */
+  int32_t causal;                /* 1 or 0                                     */
+  int32_t window;                /* > 0: keys seen at most; 0: all             */
+  float scale;                   /* finite                                     */
+  int32_t n_splits;              /* 0: automatic; else 1 .. 512                */
+  const int32_t* q_tokens;       /* device [n_requests], or NULL               */
+  const int32_t* q_base;         /* device [n_requests], or NULL               */
+  const int32_t* kv_tokens;      /* device [n_requests], at most n_keys        */
+  const int32_t* page_table;     /* device [n_requests][pt_stride]             */
+  const void* q;                 /* bf16                                       */
+  int64_t q_stride[2];           /* row, head                                  */
+  void* out;                     /* bf16                                       */
+  int64_t out_stride[2];
+  float* lse;
+  int64_t lse_stride[2];
+  const void* k_cache;
+  int64_t k_cache_stride[3];     /* page, token, head                          */
+  const void* v_cache;
+  int64_t v_cache_stride[3];
+  const float* k_scale;          /* E4M3 only                                  */
+  int64_t k_scale_stride[2];     /* page, head                                 */
+  const float* v_scale;
+  int64_t v_scale_stride[2];
+  const int32_t* sel;            /* optional: device [n_requests][n_kv_heads]  */
+  const int32_t* sel_count;      /*   [sel_stride], and their counts           */
+  int32_t sel_stride;
+  void* workspace;
+  int64_t workspace_bytes;
+  uint32_t* status;
+} kamera_attend_args;
+
+int kamera_page_tables(const kamera_page_tables_args* args, void* stream);
+int kamera_append_paged8(const kamera_append_args* args, void* stream);
+int kamera_select_pages(const kamera_select_args* args, void* stream);
+int kamera_attend_paged(const kamera_attend_args* args, void* stream);
+
+/* Bytes of workspace that kamera_attend_paged needs for `args` (its pointers
+ * are not looked at, workspace and workspace_bytes included), 0 where the work
+ * is not split; or the negative error code of a refused size. */
+int64_t kamera_attend_workspace(const kamera_attend_args* args);
+
+/* As kamera_validate, for the entry points above: 0 kamera_page_tables,
+ * 1 kamera_append_paged8, 2 kamera_select_pages, 3 kamera_attend_paged. */
+int kamera_validate_cache(int32_t which, const void* args);
+
 /* Host-side check of a page table copy (host memory, n_chunks x pt_stride,
  * the first ceil(tokens/page_size) entries of each row are used): every used
  * entry in [0, n_pool_pages) and no page used twice.  Returns KAMERA_OK or
@@ -440,7 +696,7 @@ int kamera_rehydrate_schedule(const kamera_rehydrate_args* args);
 const char* kamera_last_error(void);
 int kamera_abi_version(void);
 /* sizeof of the argument structs: 0 rehydrate, 1 shift, 2 scatter, 3 plane,
- * 4 rope, 5 form; -1 otherwise.  Lets a foreign-function binding check its
+ * 4 rope, 5 form, 6 page tables, 7 append, 8 select, 9 attend; -1 otherwise.  Lets a foreign-function binding check its
  * layout. */
 int64_t kamera_struct_size(int32_t which);
 

@@ -16,6 +16,8 @@ Entry points (same names as the C ABI):
 * ``gather_paged``  the inverse copy, pool slots back into dense rows
 * ``form_patch``    the compile step's truncated SVD of given deficits
                     (App. A): U = U_svd S [:, :m], W = Vt[:m]
+* ``page_tables``, ``append_paged8``, ``select_pages``, ``attend_paged``
+                    serving from the paged cache (module ``cache``)
 """
 
 from __future__ import annotations
@@ -146,6 +148,8 @@ def lib() -> ctypes.CDLL:
     global _LIB
     if _LIB is not None:
         return _LIB
+    from . import cache as _cache
+
     # torch ships its own HIP runtime: load it first so that the library binds
     # to the same runtime instance torch's tensors and streams live in
     import torch  # noqa: F401
@@ -187,7 +191,9 @@ def lib() -> ctypes.CDLL:
     L.kamera_rehydrate_schedule.restype = _i32
     L.kamera_struct_size.argtypes = [_i32]
     L.kamera_struct_size.restype = _i64
-    sizes = {0: CRehydrateArgs, 1: CShiftArgs, 2: CScatterArgs, 3: CPlane, 4: CRope, 5: CFormArgs}
+    _cache.declare(L)
+    sizes = {0: CRehydrateArgs, 1: CShiftArgs, 2: CScatterArgs, 3: CPlane, 4: CRope, 5: CFormArgs,
+             **_cache.STRUCTS}
     for k, cls in sizes.items():
         if L.kamera_struct_size(k) != ctypes.sizeof(cls):
             raise KameraUnavailable(f"struct layout mismatch for {cls.__name__}: "
@@ -591,3 +597,9 @@ def check_page_table(page_table_host, n_tokens: int, page_size: int, n_pool_page
     stride = arr.shape[1] if arr.ndim == 2 else 0
     _check(lib().kamera_check_page_table(arr.ctypes.data if arr.size else None, C, stride, n_tokens,
                                          page_size, n_pool_pages))
+
+
+from .cache import *  # noqa: E402,F401,F403
+from .cache import EXPORTS as _CACHE_EXPORTS  # noqa: E402
+
+EXPORTS = EXPORTS + _CACHE_EXPORTS

@@ -36,7 +36,10 @@ def _run(cmd, verbose):
     return res
 
 
-DEVICE_SOURCES = ("kamera_kernels.hip", "kamera_rows.hip", "kamera_patch.hip", "kamera_tridiag.hip")
+DEVICE_SOURCES = ("kamera_kernels.hip", "kamera_rows.hip", "kamera_patch.hip", "kamera_tridiag.hip",
+                  "kamera_tables.hip", "kamera_append.hip", "kamera_select.hip", "kamera_attend.hip",
+                  "kamera_attend_tiles.hip")
+HOST_SOURCES = ("kamera_abi.cpp", "kamera_cache.cpp")
 
 
 def build(verbose: bool = False, save_temps: bool = False) -> str:
@@ -56,11 +59,12 @@ def build(verbose: bool = False, save_temps: bool = False) -> str:
             cmd.insert(2, "-save-temps=obj")
         cmds.append(cmd)
         objs.append(obj)
-    # the ABI layer is plain host C++: validation and launch set-up only
-    aobj = os.path.join(BUILD, "kamera_abi.o")
-    cmds.append(["g++", "-c", "-O2", "-Wall", "-Wextra", "-D__HIP_PLATFORM_AMD__", "-I", "/opt/rocm/include",
-                 *common, os.path.join(CSRC, "kamera_abi.cpp"), "-o", aobj])
-    objs.append(aobj)
+    # the ABI layers are plain host C++: validation and launch set-up only
+    for src in HOST_SOURCES:
+        obj = os.path.join(BUILD, os.path.splitext(src)[0] + ".o")
+        cmds.append(["g++", "-c", "-O2", "-Wall", "-Wextra", "-D__HIP_PLATFORM_AMD__", "-I", "/opt/rocm/include",
+                     *common, os.path.join(CSRC, src), "-o", obj])
+        objs.append(obj)
     with ThreadPoolExecutor(max_workers=len(cmds)) as ex:
         for f in [ex.submit(_run, c, verbose) for c in cmds]:
             f.result()

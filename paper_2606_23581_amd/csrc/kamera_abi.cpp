@@ -3,38 +3,19 @@
 // The operator itself is defined in include/kamera.h.
 
 #include <math.h>
-#include <stdarg.h>
-#include <stdio.h>
 #include <string.h>
 
 #include <algorithm>
 #include <cstdint>
-#include <initializer_list>
 #include <vector>
 
 #include "kamera.h"
+#include "kamera_host.h"
 #include "kamera_launch.h"
 
+using namespace kamera::host;
+
 namespace {
-
-thread_local char g_err[512] = "";
-
-int fail(int code, const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_err, sizeof(g_err), fmt, ap);
-  va_end(ap);
-  return code;
-}
-
-int ok() {
-  g_err[0] = '\0';
-  return KAMERA_OK;
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 constexpr double kTwoPi = 6.283185307179586476925286766559;
 
@@ -133,47 +114,11 @@ bool strides_ok(const int64_t* s, int n) {
   return true;
 }
 
-// Largest work a call may describe (elements, rows or tasks): far beyond any
-// device, and small enough that the host arithmetic on it cannot overflow.
-constexpr int64_t kMaxWork = (int64_t)1 << 50;
-
-// product of non-negative factors, or -1 once it exceeds kMaxWork
-int64_t bounded_product(std::initializer_list<int64_t> factors) {
-  __int128 p = 1;
-  for (const int64_t f : factors) {
-    if (f < 0) return -1;
-    p *= f;
-    if (p > kMaxWork) return -1;
-  }
-  return (int64_t)p;
-}
-
-// byte range [lo, hi) of an n-D strided view (element strides, elem_bytes
-// each) whose innermost rows are row_elems contiguous elements; false when
-// the range does not fit in the address space (the arithmetic is 128-bit)
-bool span(const void* base, const int64_t* s, const int64_t* ext, int nd, int64_t row_elems, int elem_bytes,
-          uintptr_t& lo, uintptr_t& hi) {
-  __int128 a = 0, b = 0;
-  for (int k = 0; k < nd; ++k) {
-    if (ext[k] <= 0) continue;
-    const __int128 d = (__int128)(ext[k] - 1) * s[k];
-    if (d < 0) a += d; else b += d;
-  }
-  const __int128 p = (__int128)reinterpret_cast<uintptr_t>(base);
-  const __int128 l = p + a * elem_bytes, h = p + (b + row_elems) * elem_bytes;
-  if (l < 0 || h > (__int128)UINTPTR_MAX) return false;
-  lo = (uintptr_t)l;
-  hi = (uintptr_t)h;
-  return true;
-}
-
-// the same for a 4-D bf16 view
+// byte range of a 4-D bf16 view
 bool extent(const void* base, const int64_t* s, const int64_t* ext, int64_t row_elems, uintptr_t& lo,
             uintptr_t& hi) {
   return span(base, s, ext, 4, row_elems, 2, lo, hi);
 }
-
-bool overlap(uintptr_t a0, uintptr_t a1, uintptr_t b0, uintptr_t b1) { return a0 < b1 && b0 < a1; }
 
 int pick_grid(int64_t n_tasks, int32_t& per_xcd, const char* who) {
   const int64_t px = ceil_div(n_tasks, 8);
@@ -921,6 +866,10 @@ extern "C" int64_t kamera_struct_size(int32_t which) {
     case 3: return (int64_t)sizeof(kamera_plane);
     case 4: return (int64_t)sizeof(kamera_rope);
     case 5: return (int64_t)sizeof(kamera_form_args);
+    case 6: return (int64_t)sizeof(kamera_page_tables_args);
+    case 7: return (int64_t)sizeof(kamera_append_args);
+    case 8: return (int64_t)sizeof(kamera_select_args);
+    case 9: return (int64_t)sizeof(kamera_attend_args);
     default: return -1;
   }
 }

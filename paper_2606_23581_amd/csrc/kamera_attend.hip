@@ -1,0 +1,476 @@
+// kamera_attend_paged, few query rows: attention over the paged cache where
+// reading the cache is the work (decode, a few speculated tokens).
+//
+// Rows.  The query rows that share a KV head -- every query token's `group`
+// heads -- are one matrix of rows (token, head), taken 16 at a time as the N
+// side of the 16x16x32 bf16 MFMA, NR such tiles a workgroup, so a key is
+// fetched and converted once for all of them.
+//
+// A step of a wave is 32 tokens, two 16-token parts that each lie in one page.
+//   S^T = K Q^T: K's rows are the A operand; a lane takes 16 bytes of one
+//     token's row at a time, which is 16 columns of e4m3 or 8 of bf16.  Which
+//     columns make up a K-step of the product is free, so Q is loaded in the
+//     order that these loads give.  Lane l gets the scores of row l % 16 for
+//     tokens 4 (l / 16) + i of each part.
+//   O^T = V^T P^T: P goes in as the B operand straight from those registers,
+//     when the product's inner index is read as (part, token): lane group g holds
+//     tokens 4g .. 4g+3 of part 0, then of part 1.  V^T as the A operand needs
+//     the same 8 tokens of one column in a lane: it loads VC = D / 16
+//     neighbouring columns of each of its 8 tokens, pairs tokens with v_perm,
+//     and feeds product b the columns c * VC + b, c = l % 16.  Nothing passes
+//     through LDS, and each row is read in whole 64- to 256-byte runs.
+// e4m3 becomes bf16 with the page's power-of-two scale inside the conversion
+// (v_cvt_scalef32_pk_bf16_fp8, exact).
+//
+// Softmax: scores in powers of two (scale * log2 e folded in), fp32.  A row's
+// running maximum moves only when a score passes it by more than 8, so p <= 2^8
+// and the sums stay far inside fp32, while most steps skip the rescaling; the
+// row sum stays per lane until the end.
+//
+// Bound by HBM.  The next step's loads are in flight while a step is computed;
+// the four waves of a workgroup take steps in turn and join in LDS; with few
+// rows the keys are split over workgroups too, and attend_join_kernel joins.
+
+#include <algorithm>
+
+#include "kamera_attend_device.h"
+
+namespace kamera {
+
+namespace {
+
+constexpr int kAttThreads = 256;
+constexpr int kAttWaves = kAttThreads / 64;
+constexpr float kLow = -3.402823466e38f;           // running maximum of a row that saw no key
+constexpr float kSlack = 8.0f;
+
+template <int D, int FMT>
+struct Tile {
+  static constexpr int kEl = FMT == KAMERA_CACHE_BF16 ? 2 : 1;   // bytes an element
+  static constexpr int kLoads = D * kEl / 64;      // 16-byte loads of a K row by its 4 lanes
+  static constexpr int kSteps = D / 32;            // K-steps of the score product
+  static constexpr int VC = D / 16;                // V columns a lane
+  static constexpr int kVW = VC * kEl / 4;         // dwords of a V load (1, 2 or 4)
+};
+
+// The loads of one step: two parts of 16 tokens.
+template <int D, int FMT>
+struct Step {
+  u32x4 k[2][Tile<D, FMT>::kLoads];
+  uint32_t v[2][4][Tile<D, FMT>::kVW];
+  float ks[2], vs[2];
+  int page[2], pos[2];
+};
+
+template <int D, int FMT>
+__device__ __forceinline__ void load_step(const AttendParams& p, const int32_t* table, const int32_t* sel, int part0,
+                                          int part1, int step, int h, uint32_t k_lane, uint32_t v_lane, Step<D, FMT>& s) {
+  using T = Tile<D, FMT>;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const Part a = part_of(p, table, sel, part0, part1, 2 * step + u);
+    s.page[u] = a.page;
+    s.pos[u] = a.pos;
+    const int64_t page = a.page < 0 ? 0 : a.page;  // a page that may be read
+    const uint8_t* kb = p.k + page * p.k_s[0] + a.in_page * p.k_s[1] + h * p.k_s[2];
+    const uint8_t* vb = p.v + page * p.v_s[0] + a.in_page * p.v_s[1] + h * p.v_s[2];
+#pragma unroll
+    for (int i = 0; i < T::kLoads; ++i) s.k[u][i] = *reinterpret_cast<const u32x4*>(kb + k_lane + i * 64);
+    const uint32_t vt = (uint32_t)p.v_s[1];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint8_t* at = vb + v_lane + j * vt;
+      if (T::kVW == 1) s.v[u][j][0] = *reinterpret_cast<const uint32_t*>(at);
+      else if (T::kVW == 2) {
+        const u32x2 w = *reinterpret_cast<const u32x2*>(at);
+        s.v[u][j][0] = w.x;
+        s.v[u][j][T::kVW > 1 ? 1 : 0] = w.y;
+      } else {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(at);
+#pragma unroll
+        for (int e = 0; e < T::kVW; ++e) s.v[u][j][e] = u4_get(w, e);
+      }
+    }
+    if (FMT == KAMERA_CACHE_E4M3) {
+      s.ks[u] = uniform_load(p.k_scale + page * p.k_scale_s[0] + h * p.k_scale_s[1]);
+      s.vs[u] = uniform_load(p.v_scale + page * p.v_scale_s[0] + h * p.v_scale_s[1]);
+    } else {
+      s.ks[u] = s.vs[u] = 1.0f;
+    }
+  }
+}
+
+// The A operand of K-step ks for part u.
+template <int D, int FMT>
+__device__ __forceinline__ bf16x8 k_frag(const Step<D, FMT>& s, int u, int ks) {
+  if (FMT == KAMERA_CACHE_BF16) return __builtin_bit_cast(bf16x8, s.k[u][FMT == KAMERA_CACHE_BF16 ? ks : 0]);
+  const u32x4 w = s.k[u][FMT == KAMERA_CACHE_BF16 ? 0 : ks >> 1];
+  const uint32_t a = (ks & 1) ? w.z : w.x, b = (ks & 1) ? w.w : w.y;
+  u32x4 f;
+  f.x = e4m3_to_bf16x2<false>(a, s.ks[u]);
+  f.y = e4m3_to_bf16x2<true>(a, s.ks[u]);
+  f.z = e4m3_to_bf16x2<false>(b, s.ks[u]);
+  f.w = e4m3_to_bf16x2<true>(b, s.ks[u]);
+  return __builtin_bit_cast(bf16x8, f);
+}
+
+// The A operand of column b (of VC): token pairs of both parts.
+template <int D, int FMT>
+__device__ __forceinline__ bf16x8 v_frag(const Step<D, FMT>& s, int b) {
+  u32x4 f;
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      uint32_t r;
+      if (FMT == KAMERA_CACHE_BF16) {
+        const uint32_t w0 = s.v[u][2 * t][b >> 1], w1 = s.v[u][2 * t + 1][b >> 1];
+        r = __builtin_amdgcn_perm(w1, w0, (b & 1) ? 0x07060302u : 0x05040100u);
+      } else {
+        // bytes (w0.0, w1.0, w0.1, w1.1) or (w0.2, w1.2, w0.3, w1.3): two columns' pairs
+        const uint32_t w0 = s.v[u][2 * t][b >> 2], w1 = s.v[u][2 * t + 1][b >> 2];
+        const uint32_t x = __builtin_amdgcn_perm(w1, w0, (b & 2) ? 0x07030602u : 0x05010400u);
+        r = (b & 1) ? e4m3_to_bf16x2<true>(x, s.vs[u]) : e4m3_to_bf16x2<false>(x, s.vs[u]);
+      }
+      if (u == 0 && t == 0) f.x = r;
+      if (u == 0 && t == 1) f.y = r;
+      if (u == 1 && t == 0) f.z = r;
+      if (u == 1 && t == 1) f.w = r;
+    }
+  return __builtin_bit_cast(bf16x8, f);
+}
+
+// Zero the V rows of this lane's tokens outside [lo, hi], and what is not finite
+// in the others (the result says whether there was any; see add_nonfinite).
+template <int D, int FMT>
+__device__ __forceinline__ bool clear_unseen(Step<D, FMT>& s, int g, int lo, int hi) {
+  uint32_t odd = 0;
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int pos = s.pos[u] + 4 * g + j;
+      const bool keep = s.page[u] >= 0 && pos >= lo && pos <= hi;
+#pragma unroll
+      for (int e = 0; e < Tile<D, FMT>::kVW; ++e) {
+        const uint32_t w = keep ? s.v[u][j][e] : 0u;
+        odd |= nonfinite<FMT>(w);
+        s.v[u][j][e] = finite_only<FMT>(w);
+      }
+    }
+  return odd != 0;
+}
+
+}  // namespace
+
+template <int D, int FMT, int NR>
+__global__ __launch_bounds__(kAttThreads, 2) void attend_rows_kernel(AttendParams) {
+  using T = Tile<D, FMT>;
+  const AttendParams& p = kernel_params<AttendParams>();
+  constexpr int kPad = 4;
+  __shared__ float s_o[kAttWaves][16][D + kPad];
+  __shared__ float s_ml[kAttWaves][NR * 16][3];
+  __shared__ int s_odd;                            // a value that is not finite was taken as 0
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c16 = lane & 15, g = lane >> 4;
+  uint32_t w = blockIdx.x, d;
+  d = fast_div(w, p.fd_splits);
+  const int split = (int)(w - d * p.n_splits);
+  w = d;
+  d = fast_div(w, p.fd_blocks);
+  const int rb = (int)(w - d * p.n_row_blocks);
+  w = d;
+  d = fast_div(w, p.fd_heads);
+  const int h = (int)(w - d * p.n_kv_heads), r = (int)d;
+
+  const Request rq = request_of(p, r);
+  const int rows = rq.n * p.group;                 // rows of this KV head
+  const int row_first = rb * NR * 16, row_end = min(rows, row_first + NR * 16);
+  if (row_first >= rows) return;
+  const int i_first = (int)fast_div((uint32_t)row_first, p.fd_group);
+  const int i_last = (int)fast_div((uint32_t)row_end - 1, p.fd_group);
+
+  // keys that some row of the block sees, and those that every row sees
+  const int32_t* table = p.page_table + (int64_t)r * p.pt_stride;
+  const int32_t* sel = nullptr;
+  const int hi = min(last_key(p, rq, i_last), rq.kv - 1), all_hi = last_key(p, rq, i_first);
+  const int lo = first_key(p, last_key(p, rq, i_first)), all_lo = first_key(p, last_key(p, rq, i_last));
+  int part0 = lo >> 4, part1 = (hi >> 4) + 1;
+  if (p.sel != nullptr) {
+    const int64_t at = (int64_t)r * p.n_kv_heads + h;
+    sel = p.sel + at * p.sel_stride;
+    part0 = 0;
+    part1 = min(max(uniform_load(p.sel_count + at), 0), p.sel_stride) * (p.page_size >> 4);
+  }
+  const int step0 = part0 >> 1, step1 = (part1 + 1) >> 1;
+  const int n_steps = max(step1 - step0, 0);
+  const int per = (n_steps + p.n_splits - 1) / p.n_splits;
+  const int s_begin = step0 + split * per, s_end = min(step1, s_begin + per);
+
+  // Q rows as B operands, in the column order of the K loads; rows past the end are zero
+  bf16x8 qf[NR][T::kSteps];
+  int row_hi[NR], row_lo[NR];
+#pragma unroll
+  for (int t = 0; t < NR; ++t) {
+    const int row = row_first + t * 16 + c16;
+    const int i = (int)fast_div((uint32_t)row, p.fd_group), hq = row - i * p.group;
+    const bool there = row < row_end;
+    row_hi[t] = there ? min(last_key(p, rq, i), rq.kv - 1) : -1;
+    row_lo[t] = there ? first_key(p, last_key(p, rq, i)) : 0;
+    const uint16_t* src = p.q + (rq.row0 + i) * p.q_s[0] + ((int64_t)h * p.group + hq) * p.q_s[1];
+#pragma unroll
+    for (int ks = 0; ks < T::kSteps; ++ks) {
+      const int col = FMT == KAMERA_CACHE_BF16 ? (g + 4 * ks) * 8 : (g + 4 * (ks >> 1)) * 16 + (ks & 1) * 8;
+      u32x4 x = {0u, 0u, 0u, 0u};
+      if (there) x = *reinterpret_cast<const u32x4*>(src + col) ^ p.q_sign;
+      qf[t][ks] = __builtin_bit_cast(bf16x8, x);
+    }
+  }
+
+  f32x4 o[NR][T::VC];
+  float m[NR], l[NR], lx[NR];
+#pragma unroll
+  for (int t = 0; t < NR; ++t) {
+    m[t] = kLow;
+    l[t] = lx[t] = 0.f;
+#pragma unroll
+    for (int b = 0; b < T::VC; ++b) o[t][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const uint32_t k_lane = (uint32_t)(c16 * p.k_s[1]) + g * 16;
+  const uint32_t v_lane = (uint32_t)(4 * g * p.v_s[1]) + c16 * T::VC * T::kEl;
+
+  if (threadIdx.x == 0) s_odd = 0;
+  __syncthreads();
+  Step<D, FMT> cur, nxt;
+  int step = s_begin + wave;
+  if (step < s_end) load_step<D, FMT>(p, table, sel, part0, part1, step, h, k_lane, v_lane, cur);
+  for (; step < s_end; step += kAttWaves) {
+    if (step + kAttWaves < s_end)
+      load_step<D, FMT>(p, table, sel, part0, part1, step + kAttWaves, h, k_lane, v_lane, nxt);
+
+    // a step that some row does not see whole
+    const bool partial = cur.page[0] < 0 || cur.page[1] < 0 || max(cur.pos[0], cur.pos[1]) + 15 > all_hi ||
+                         min(cur.pos[0], cur.pos[1]) < all_lo;
+    if (partial && clear_unseen<D, FMT>(cur, g, lo, hi)) s_odd = 1;
+
+    f32x4 sc[NR][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int t = 0; t < NR; ++t) sc[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < T::kSteps; ++ks) {
+        const bf16x8 a = k_frag<D, FMT>(cur, u, ks);
+#pragma unroll
+        for (int t = 0; t < NR; ++t) sc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, qf[t][ks], sc[t][u], 0, 0, 0);
+      }
+    }
+
+    bf16x8 pf[NR];
+#pragma unroll
+    for (int t = 0; t < NR; ++t) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[u * 4 + i] = sc[t][u][i];
+      if (partial) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int pos = cur.pos[u] + 4 * g + i;
+            const bool seen = cur.page[u] >= 0 && pos >= row_lo[t] && pos <= row_hi[t];
+            x[u * 4 + i] = seen ? x[u * 4 + i] : -INFINITY;
+          }
+      }
+      float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) * p.scale2;
+      if (__ballot(top > m[t] + kSlack) != 0) {
+        top = max_x32(max_x16(top));
+        const float m_new = fmaxf(m[t], top);
+        const float down = exp2_fast(m[t] - m_new);
+        m[t] = m_new;
+        l[t] *= down;
+        lx[t] *= down;
+#pragma unroll
+        for (int b = 0; b < T::VC; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[t][b][i] *= down;
+      }
+      u32x4 pk;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = exp2_fast(__builtin_fmaf(x[i], p.scale2, -m[t]));
+      if (p.lse != nullptr) lx[t] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+      pk.x = pack_bf16x2(x[0], x[1]);
+      pk.y = pack_bf16x2(x[2], x[3]);
+      pk.z = pack_bf16x2(x[4], x[5]);
+      pk.w = pack_bf16x2(x[6], x[7]);
+      l[t] = add_pair(pk.w, add_pair(pk.z, add_pair(pk.y, add_pair(pk.x, l[t]))));
+      pf[t] = __builtin_bit_cast(bf16x8, pk);
+    }
+
+#pragma unroll
+    for (int b = 0; b < T::VC; ++b) {
+      const bf16x8 a = v_frag<D, FMT>(cur, b);
+#pragma unroll
+      for (int t = 0; t < NR; ++t) o[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, pf[t], o[t][b], 0, 0, 0);
+    }
+    cur = nxt;
+  }
+
+  // join the four waves
+#pragma unroll
+  for (int t = 0; t < NR; ++t) {
+    l[t] = sum_x32(sum_x16(l[t]));
+    lx[t] = sum_x32(sum_x16(lx[t]));
+    if (g == 0) {
+      s_ml[wave][t * 16 + c16][0] = m[t];
+      s_ml[wave][t * 16 + c16][1] = l[t];
+      s_ml[wave][t * 16 + c16][2] = lx[t];
+    }
+  }
+  __syncthreads();
+  const int row_t = threadIdx.x >> 4, col = (threadIdx.x & 15) * T::VC;   // output: 16 rows x 16 threads
+#pragma unroll
+  for (int t = 0; t < NR; ++t) {
+    float top = kLow;
+#pragma unroll
+    for (int k = 0; k < kAttWaves; ++k) top = fmaxf(top, s_ml[k][t * 16 + c16][0]);
+    const float down = exp2_fast(m[t] - top);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int b = 0; b < T::VC; ++b) s_o[wave][c16][(4 * g + i) * T::VC + b] = o[t][b][i] * down;
+    __syncthreads();
+    const int row = row_first + t * 16 + row_t;
+    if (row < row_end) {
+      float mm = kLow, ll = 0.f, lxx = 0.f;
+#pragma unroll
+      for (int k = 0; k < kAttWaves; ++k) mm = fmaxf(mm, s_ml[k][t * 16 + row_t][0]);
+#pragma unroll
+      for (int k = 0; k < kAttWaves; ++k) {
+        const float f = exp2_fast(s_ml[k][t * 16 + row_t][0] - mm);
+        ll += s_ml[k][t * 16 + row_t][1] * f;
+        lxx += s_ml[k][t * 16 + row_t][2] * f;
+      }
+      float a[T::VC];
+#pragma unroll
+      for (int b = 0; b < T::VC; ++b)
+        a[b] = (s_o[0][row_t][col + b] + s_o[1][row_t][col + b]) + (s_o[2][row_t][col + b] + s_o[3][row_t][col + b]);
+      if (p.n_splits > 1) {
+        const int64_t at = (((int64_t)r * p.n_kv_heads + h) * p.rows_max + row) * p.n_splits + split;
+#pragma unroll
+        for (int b = 0; b < T::VC; b += 4)
+          *reinterpret_cast<f32x4*>(p.part_o + at * D + col + b) = f32x4{a[b], a[b + 1], a[b + 2], a[b + 3]};
+        if ((threadIdx.x & 15) == 0) *reinterpret_cast<f32x4*>(p.part_ml + at * 4) = f32x4{mm, ll, lxx, 0.f};
+      } else {
+        const int i = (int)fast_div((uint32_t)row, p.fd_group);
+        const int64_t hq = (int64_t)h * p.group + (row - i * p.group);
+        const float inv = ll == 0.f ? 0.f : 1.0f / ll;
+        uint16_t* dst = p.out + (rq.row0 + i) * p.out_s[0] + hq * p.out_s[1] + col;
+#pragma unroll
+        for (int b = 0; b < T::VC; b += 4)
+          *reinterpret_cast<u32x2*>(dst + b) =
+              u32x2{pack_bf16x2(a[b] * inv, a[b + 1] * inv), pack_bf16x2(a[b + 2] * inv, a[b + 3] * inv)};
+        if (p.lse != nullptr && (threadIdx.x & 15) == 0)
+          p.lse[(rq.row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] = row_lse(mm, lxx);
+      }
+    }
+    __syncthreads();
+  }
+  if (s_odd)
+    add_nonfinite<D, FMT>(p, rq, table, sel, part0, part1, 2 * s_begin, 2 * s_end, 2, all_lo, all_hi, h, r, row_first,
+                          row_end, split);
+}
+
+// Joins the parts of each row: with M the largest of the parts' maxima m_s,
+// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.  One workgroup a row, its
+// four waves take parts in turn.
+template <int D>
+__global__ __launch_bounds__(kAttThreads) void attend_join_kernel(AttendParams) {
+  const AttendParams& p = kernel_params<AttendParams>();
+  constexpr int C = D / 64;                        // columns a lane
+  __shared__ float s_o[kAttWaves][D];
+  __shared__ float s_l[2][kAttWaves];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t w = blockIdx.x, d;
+  d = fast_div(w, p.fd_rows);
+  const int row = (int)(w - d * p.rows_max);
+  w = d;
+  d = fast_div(w, p.fd_heads);
+  const int h = (int)(w - d * p.n_kv_heads), r = (int)d;
+  const Request rq = request_of(p, r);
+  const int i = (int)fast_div((uint32_t)row, p.fd_group);
+  if (i >= rq.n) return;
+  const int64_t at = (((int64_t)r * p.n_kv_heads + h) * p.rows_max + row) * p.n_splits;
+  float top = kLow;
+  for (int s = lane; s < p.n_splits; s += 64) top = fmaxf(top, p.part_ml[(at + s) * 4]);
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
+  float acc[C], l = 0.f, lx = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) acc[c] = 0.f;
+  for (int s = wave; s < p.n_splits; s += kAttWaves) {
+    const f32x4 ml = *reinterpret_cast<const f32x4*>(p.part_ml + (at + s) * 4);
+    const float f = exp2_fast(ml.x - top);
+    l += ml.y * f;
+    lx += ml.z * f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) acc[c] += p.part_o[(at + s) * D + lane * C + c] * f;
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c) s_o[wave][lane * C + c] = acc[c];
+  if (lane == 0) {
+    s_l[0][wave] = l;
+    s_l[1][wave] = lx;
+  }
+  __syncthreads();
+  const int t = threadIdx.x;
+  const float ll = (s_l[0][0] + s_l[0][1]) + (s_l[0][2] + s_l[0][3]);
+  const int64_t hq = (int64_t)h * p.group + (row - i * p.group);
+  if (t < D / 2) {
+    const float inv = ll == 0.f ? 0.f : 1.0f / ll;
+    float v[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      v[e] = ((s_o[0][2 * t + e] + s_o[1][2 * t + e]) + (s_o[2][2 * t + e] + s_o[3][2 * t + e])) * inv;
+    *reinterpret_cast<uint32_t*>(p.out + (rq.row0 + i) * p.out_s[0] + hq * p.out_s[1] + 2 * t) =
+        pack_bf16x2(v[0], v[1]);
+  }
+  if (t == 0 && p.lse != nullptr)
+    p.lse[(rq.row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] =
+        row_lse(top, (s_l[1][0] + s_l[1][1]) + (s_l[1][2] + s_l[1][3]));
+}
+
+namespace {
+
+template <int D, int FMT>
+hipError_t launch_rows(const AttendParams& p, hipStream_t s) {
+  const dim3 grid((uint32_t)p.n_tasks), block(kAttThreads);
+  switch (p.row_tiles) {
+    case 1: hipLaunchKernelGGL((attend_rows_kernel<D, FMT, 1>), grid, block, 0, s, p); break;
+    default: hipLaunchKernelGGL((attend_rows_kernel<D, FMT, 2>), grid, block, 0, s, p); break;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attend(const AttendParams& p, hipStream_t s) {
+  hipError_t e;
+  if (p.tiles)
+    e = launch_attend_tiles(p, s);
+  else if (p.cache_type == KAMERA_CACHE_E4M3)
+    e = p.head_dim == 128 ? launch_rows<128, KAMERA_CACHE_E4M3>(p, s) : launch_rows<64, KAMERA_CACHE_E4M3>(p, s);
+  else
+    e = p.head_dim == 128 ? launch_rows<128, KAMERA_CACHE_BF16>(p, s) : launch_rows<64, KAMERA_CACHE_BF16>(p, s);
+  if (e != hipSuccess || p.n_splits == 1) return e;
+  const dim3 grid((uint32_t)p.n_requests * p.n_kv_heads * p.rows_max), block(kAttThreads);
+  if (p.head_dim == 128) hipLaunchKernelGGL(attend_join_kernel<128>, grid, block, 0, s, p);
+  else hipLaunchKernelGGL(attend_join_kernel<64>, grid, block, 0, s, p);
+  return hipGetLastError();
+}
+
+}  // namespace kamera

@@ -1,0 +1,190 @@
+// Device code shared by the attention kernels: cache formats, page look-up and
+// the bookkeeping of which keys a row sees.
+#pragma once
+
+#include "kamera_cache.h"
+#include "kamera_device.h"
+
+namespace kamera {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// v_exp_f32 and v_log_f32: 2^x and log2 x, about 1 ulp
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Two neighbouring bytes of w (the low or the high half) as bf16 times a power
+// of two: exact.
+template <bool HI>
+__device__ __forceinline__ uint32_t e4m3_to_bf16x2(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI));
+}
+
+// Memory that no kernel writes while this one runs, at a wave-uniform address:
+// a scalar load.
+template <typename T>
+__device__ __forceinline__ T uniform_load(const T* p) {
+  return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
+}
+
+// The largest / sum over the lanes l, l ^ 32 and (groups of 16) l ^ 16, l ^ 32.
+__device__ __forceinline__ float max_x32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_x16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_x32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float sum_x16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Not a finite number among the elements of w (four e4m3 bytes / two bf16): the
+// top bit of each such element.
+template <int FMT>
+__device__ __forceinline__ uint32_t nonfinite(uint32_t w) {
+  if (FMT == KAMERA_CACHE_E4M3) return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+  return ((w & 0x7fff7fffu) + 0x00800080u) & 0x80008000u;
+}
+
+// w with these elements zero.
+template <int FMT>
+__device__ __forceinline__ uint32_t finite_only(uint32_t w) {
+  const uint32_t top = nonfinite<FMT>(w);
+  const uint32_t all = FMT == KAMERA_CACHE_E4M3 ? (top >> 7) * 0xffu : (top >> 15) * 0xffffu;
+  return w & ~all;
+}
+
+// a + the sum of a pair of bf16 values, in fp32.
+__device__ __forceinline__ float add_pair(uint32_t pair, float a) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3f803f80u), a,
+                                         false);
+}
+
+// A row's weights are p as the product with V takes them, rounded to bf16, over
+// the sum of these, so that they add up to one; lse is taken from the sum of p
+// itself, kept beside it where a call asks for lse.
+__device__ __forceinline__ float row_lse(float m, float l_exact) {
+  return l_exact == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l_exact)) * 0.69314718055994530942f;
+}
+
+// A request of the batch as every wave of a workgroup sees it.
+struct Request {
+  int n;                             // query tokens
+  int kv;                            // cached tokens
+  int64_t row0;                      // row of query 0 in q and out
+};
+
+__device__ __forceinline__ Request request_of(const AttendParams& p, int r) {
+  Request q;
+  q.n = p.n_queries;
+  if (p.q_tokens != nullptr) q.n = min(max(uniform_load(p.q_tokens + r), 0), p.n_queries);
+  q.kv = min(max(uniform_load(p.kv_tokens + r), 0), p.n_keys);
+  q.row0 = p.q_base != nullptr ? (int64_t)uniform_load(p.q_base + r) : (int64_t)r * p.n_queries;
+  return q;
+}
+
+// Query i sees the keys [first, last].
+__device__ __forceinline__ int last_key(const AttendParams& p, const Request& q, int i) {
+  return p.causal ? q.kv - q.n + i : q.kv - 1;
+}
+__device__ __forceinline__ int first_key(const AttendParams& p, int last) {
+  return p.window > 0 ? max(0, last - p.window + 1) : 0;
+}
+
+// One 16-token part of a page: where it is in the pool and in the request.
+struct Part {
+  int page;                          // -1: not in the pool, or past the end
+  int in_page;                       // first token within the page
+  int pos;                           // first token of the request
+};
+
+// Part number n of the walk over a request's keys: tokens [16 n, 16 n + 16), or
+// with selected pages the n-th part of those.  Parts outside [begin, end) are
+// not looked up: what lies before a window may have left the pool.
+__device__ __forceinline__ Part part_of(const AttendParams& p, const int32_t* table, const int32_t* sel, int begin,
+                                        int end, int n) {
+  Part a;
+  const int k = (int)fast_div((uint32_t)n, p.fd_page16);
+  a.in_page = (n - k * (p.page_size >> 4)) * 16;
+  a.page = -1;
+  a.pos = n * 16;
+  if (n >= begin && n < end) {
+    int idx = k;
+    if (sel != nullptr) {
+      idx = uniform_load(sel + k);
+      a.pos = idx * p.page_size + a.in_page;
+    }
+    if (idx >= 0 && idx < p.pt_stride) {
+      a.page = uniform_load(table + idx);
+      if (a.page >= p.n_pool_pages) a.page = -1;
+    }
+    if (a.page < 0) {
+      a.page = -1;
+      if (p.status != nullptr && (threadIdx.x & 63) == 0) atomicOr(p.status, KAMERA_STATUS_BAD_PAGE);
+    }
+  }
+  return a;
+}
+
+// A value that is not finite must reach the rows that see its token, and no
+// others: 0 * NaN is NaN, so a product over a tile that some row does not see
+// whole takes such values as 0, and this adds them to those rows' results in
+// memory afterwards (v itself: any positive weight of it is the same).  It runs
+// only where the workgroup met one.  Parts [first, end) in groups of `group`, the
+// tiles of the caller; all_lo, all_hi: the keys that every row of the block sees.
+// Called by all threads after their results are stored.
+template <int D, int FMT>
+__device__ __forceinline__ void add_nonfinite(const AttendParams& p, const Request& rq, const int32_t* table,
+                                           const int32_t* sel, int part0, int part1, int first, int end, int group,
+                                           int all_lo, int all_hi, int h, int r, int row_first, int row_end, int split) {
+  constexpr int kEl = FMT == KAMERA_CACHE_BF16 ? 2 : 1;
+  __threadfence();
+  __syncthreads();
+  const int col = threadIdx.x % D, sub = threadIdx.x / D, subs = kThreads / D;
+  for (int g0 = first; g0 < end; g0 += group) {
+    bool partial = false;
+    for (int n = g0; n < g0 + group; ++n) {
+      const Part a = part_of(p, table, sel, part0, part1, n);
+      partial = partial || a.page < 0 || a.pos + 15 > all_hi || a.pos < all_lo;
+    }
+    if (!partial) continue;
+    for (int n = g0; n < g0 + group; ++n) {
+      const Part a = part_of(p, table, sel, part0, part1, n);
+      if (a.page < 0) continue;
+      const uint8_t* vb = p.v + a.page * p.v_s[0] + a.in_page * p.v_s[1] + h * p.v_s[2] + col * kEl;
+      for (int t = 0; t < 16 && a.pos + t < rq.kv; ++t) {
+        float v;
+        if (FMT == KAMERA_CACHE_BF16) {
+          const uint32_t w = *reinterpret_cast<const uint16_t*>(vb + t * p.v_s[1]);
+          if ((w & 0x7f80u) != 0x7f80u) continue;
+          v = bf_lo(w);
+        } else {
+          const uint32_t w = vb[t * p.v_s[1]];
+          if ((w & 0x7fu) != 0x7fu) continue;
+          v = __uint_as_float(0x7fc00000u);
+        }
+        for (int row = row_first + sub; row < row_end; row += subs) {
+          const int i = (int)fast_div((uint32_t)row, p.fd_group);
+          const int last = last_key(p, rq, i);
+          if (a.pos + t > last || a.pos + t < first_key(p, last)) continue;
+          if (p.n_splits > 1) {
+            float* o = p.part_o + ((((int64_t)r * p.n_kv_heads + h) * p.rows_max + row) * p.n_splits + split) * D + col;
+            *o += v;
+          } else {
+            uint16_t* o = p.out + (rq.row0 + i) * p.out_s[0] + ((int64_t)h * p.group + (row - i * p.group)) * p.out_s[1] + col;
+            *o = (uint16_t)pack_bf16x2(bf_lo(*o) + v, 0.f);
+          }
+        }
+      }
+    }
+  }
+}
+
+}  // namespace kamera

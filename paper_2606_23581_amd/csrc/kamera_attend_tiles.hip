@@ -1,0 +1,418 @@
+// kamera_attend_paged, many query rows: attention over the paged cache where the
+// matrix products are the work (prompt chunks).
+//
+// Rows as in the few-rows kernel: (query token, head of the group) of one KV
+// head.  A wave takes RT tiles of 32 rows, a workgroup four waves, all over the
+// same 64-token tiles of K and V, which the workgroup stages in LDS as bf16: K as
+// [token][D], V transposed, [D][token].  e4m3 becomes bf16 on the way, once for
+// all rows.
+//
+//   S^T = K Q^T and O^T = V^T P^T with 32x32x16 bf16 MFMAs, K and V^T the A
+//   operands.  In S^T lane l holds row l % 32 and tokens 8 (i / 4) + 4 (l / 32) +
+//   i % 4; these registers are P^T's B operand as they are when the inner index
+//   of the second product runs over the tokens in that order, so V^T is stored
+//   with the 4-token runs 0 1 2 3 of each 16 as 0 2 1 3.  A row's scores lie in
+//   two lanes: its maximum takes one exchange.
+//
+// LDS: 16-byte chunks are exchanged by an exclusive-or with bits of the row
+// number, so that the 16 lanes that read a chunk together (16 rows, one column)
+// and those that write transposed columns spread over all banks.  Two buffers:
+// the loads of the next tile are issued before a tile is computed and stored
+// after it, with one barrier a tile.
+//
+// Softmax as in the few-rows kernel; the rescaling of O runs only when a row's
+// maximum passes the running one by more than 2^8.
+
+#include <algorithm>
+
+#include "kamera_attend_device.h"
+
+namespace kamera {
+
+namespace {
+
+constexpr int kTileThreads = 256;
+constexpr int kTileKeys = 64;
+constexpr float kLow = -3.402823466e38f;
+constexpr float kSlack = 8.0f;
+
+// Place of 16-byte chunk `c` of row `r` in a tile whose rows are 8 or 16 chunks.
+template <int CHUNKS>
+__device__ __forceinline__ uint32_t chunk_at(uint32_t r, uint32_t c) {
+  if (CHUNKS == 16) return r * 16 + (c ^ (r & 15));
+  return r * 8 + (c ^ (((r >> 1) ^ (r >> 4)) & 7));
+}
+
+template <int D, int FMT>
+struct Stage {                                     // a thread's share of a tile
+  static constexpr int kEl = FMT == KAMERA_CACHE_BF16 ? 2 : 1;
+  static constexpr int kRowLoads = D * kEl / 16;   // 16-byte loads of a K row
+  static constexpr int KN = kTileKeys * kRowLoads / kTileThreads;
+  static constexpr int VC = D / 16;                // V columns a thread, of 4 tokens
+  static constexpr int VW = VC * kEl / 4;          // dwords of them in one token
+  u32x4 k[KN];
+  uint32_t v[4][VW];
+  float ks[KN], vs;
+  int v_pos;                                       // first of the 4 tokens; very large: none
+};
+
+struct Keys {                                      // what a workgroup walks
+  const int32_t* table;
+  int lo, hi;                                      // keys that some row sees
+  int part0, part1;
+};
+
+__device__ __forceinline__ void find_part(const AttendParams& p, const Keys& w, int n, int& page, int& in_page) {
+  const Part a = part_of(p, w.table, nullptr, w.part0, w.part1, n);
+  page = __builtin_amdgcn_readfirstlane(a.page);
+  in_page = __builtin_amdgcn_readfirstlane(a.in_page);
+}
+
+template <int D, int FMT>
+__device__ __forceinline__ void load_tile(const AttendParams& p, const Keys& w, int tile, int h, int wave,
+                                          Stage<D, FMT>& s, uint32_t& bad) {
+  using S = Stage<D, FMT>;
+  int pg0, pg1, pg2, pg3, in0, in1, in2, in3;
+  find_part(p, w, tile * 4, pg0, in0);
+  find_part(p, w, tile * 4 + 1, pg1, in1);
+  find_part(p, w, tile * 4 + 2, pg2, in2);
+  find_part(p, w, tile * 4 + 3, pg3, in3);
+  bad = (pg0 < 0 ? 1u : 0u) | (pg1 < 0 ? 2u : 0u) | (pg2 < 0 ? 4u : 0u) | (pg3 < 0 ? 8u : 0u);
+  auto pick = [](int u, int a, int b, int c, int d) {
+    const int x = (u & 1) ? b : a, y = (u & 1) ? d : c;
+    return (u & 2) ? y : x;
+  };
+  auto page_of = [&](int u) { return pick(u, pg0, pg1, pg2, pg3); };
+  auto first_of = [&](int u) { return pick(u, in0, in1, in2, in3); };
+  const int tid = threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < S::KN; ++i) {
+    // a wave's tokens of one load lie in one part
+    const int unit = tid + i * kTileThreads, t = unit / S::kRowLoads, c = unit % S::kRowLoads;
+    const int u = (wave * 64 + i * kTileThreads) / S::kRowLoads / 16;
+    const int64_t page = max(page_of(u), 0);
+    const uint8_t* kb = p.k + page * p.k_s[0] + first_of(u) * p.k_s[1] + h * p.k_s[2];
+    s.k[i] = *reinterpret_cast<const u32x4*>(kb + (uint32_t)((t & 15) * (uint32_t)p.k_s[1] + c * 16));
+    s.ks[i] = FMT == KAMERA_CACHE_E4M3 ? uniform_load(p.k_scale + page * p.k_scale_s[0] + h * p.k_scale_s[1]) : 1.0f;
+  }
+  const int64_t page = max(page_of(wave), 0);
+  const uint8_t* vb = p.v + page * p.v_s[0] + first_of(wave) * p.v_s[1] + h * p.v_s[2];
+  const int q4 = (tid >> 4) & 3, cg = tid & 15;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint8_t* at = vb + (uint32_t)((q4 * 4 + j) * (uint32_t)p.v_s[1] + cg * S::VC * S::kEl);
+    if (S::VW == 1) s.v[j][0] = *reinterpret_cast<const uint32_t*>(at);
+    else if (S::VW == 2) {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(at);
+      s.v[j][0] = x.x;
+      s.v[j][S::VW > 1 ? 1 : 0] = x.y;
+    } else {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(at);
+#pragma unroll
+      for (int e = 0; e < S::VW; ++e) s.v[j][e] = u4_get(x, e);
+    }
+  }
+  s.vs = FMT == KAMERA_CACHE_E4M3 ? uniform_load(p.v_scale + page * p.v_scale_s[0] + h * p.v_scale_s[1]) : 1.0f;
+  s.v_pos = page_of(wave) < 0 ? INT32_MAX - 16 : tile * kTileKeys + wave * 16 + q4 * 4;
+}
+
+// Registers -> LDS.  With `clear`, V rows that no row of the block sees become
+// zero, and so does what is not finite in the others (the result says whether
+// there was any; see add_nonfinite).
+template <int D, int FMT>
+__device__ __forceinline__ bool store_tile(Stage<D, FMT>& s, u32x4* k_lds, u32x2* v_lds, bool clear, const Keys& w) {
+  using S = Stage<D, FMT>;
+  constexpr int KC = D / 8;                        // chunks of a K row in LDS
+  const int tid = threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < S::KN; ++i) {
+    const int unit = tid + i * kTileThreads, t = unit / S::kRowLoads, c = unit % S::kRowLoads;
+    if (FMT == KAMERA_CACHE_BF16) {
+      k_lds[chunk_at<KC>(t, c)] = s.k[i];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t a = e ? s.k[i].z : s.k[i].x, b = e ? s.k[i].w : s.k[i].y;
+        k_lds[chunk_at<KC>(t, 2 * c + e)] =
+            u32x4{e4m3_to_bf16x2<false>(a, s.ks[i]), e4m3_to_bf16x2<true>(a, s.ks[i]),
+                  e4m3_to_bf16x2<false>(b, s.ks[i]), e4m3_to_bf16x2<true>(b, s.ks[i])};
+      }
+    }
+  }
+  uint32_t odd = 0;
+  if (clear) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool keep = s.v_pos + j >= w.lo && s.v_pos + j <= w.hi;
+#pragma unroll
+      for (int e = 0; e < S::VW; ++e) {
+        s.v[j][e] = keep ? s.v[j][e] : 0u;
+        odd |= nonfinite<FMT>(s.v[j][e]);
+        s.v[j][e] = finite_only<FMT>(s.v[j][e]);
+      }
+    }
+  }
+  // tokens 4 q .. 4 q + 3 of the tile: run q % 4 of 16-token group q / 4
+  const int q = tid >> 4, cg = tid & 15;
+  const uint32_t run = (q & 3) == 1 ? 2 : ((q & 3) == 2 ? 1 : (q & 3));
+  const uint32_t chunk = (q >> 2) * 2 + (run >> 1), half = run & 1;
+#pragma unroll
+  for (int c = 0; c < S::VC; ++c) {
+    u32x2 r;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      uint32_t y;
+      if (FMT == KAMERA_CACHE_BF16) {
+        y = __builtin_amdgcn_perm(s.v[2 * t + 1][c >> 1], s.v[2 * t][c >> 1], (c & 1) ? 0x07060302u : 0x05040100u);
+      } else {
+        const uint32_t x =
+            __builtin_amdgcn_perm(s.v[2 * t + 1][c >> 2], s.v[2 * t][c >> 2], (c & 2) ? 0x07030602u : 0x05010400u);
+        y = (c & 1) ? e4m3_to_bf16x2<true>(x, s.vs) : e4m3_to_bf16x2<false>(x, s.vs);
+      }
+      if (t == 0) r.x = y; else r.y = y;
+    }
+    v_lds[chunk_at<8>(cg * S::VC + c, chunk) * 2 + half] = r;
+  }
+  return odd != 0;
+}
+
+}  // namespace
+
+template <int D, int FMT, int RT>
+__global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_kernel(AttendParams) {
+  const AttendParams& p = kernel_params<AttendParams>();
+  constexpr int KC = D / 8, KS = D / 16, DT = D / 32;
+  constexpr int kRows = 4 * RT * 32;
+  constexpr int kBuf = kTileKeys * KC + D * 8;     // chunks of one buffer: K, then V^T
+  extern __shared__ u32x4 s_buf[];
+  __shared__ int s_odd;                            // a value that is not finite was taken as 0
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c32 = lane & 31, hf = lane >> 5;
+  // neighbouring row blocks of one KV head on one XCD, the longest first
+  const uint32_t task = (blockIdx.x & 7) * (uint32_t)p.per_xcd + (blockIdx.x >> 3);
+  if (task >= (uint32_t)p.n_tasks) return;
+  uint32_t w = task, d;
+  d = fast_div(w, p.fd_splits);
+  const int split = (int)(w - d * p.n_splits);
+  w = d;
+  d = fast_div(w, p.fd_blocks);
+  const int rb = p.n_row_blocks - 1 - (int)(w - d * p.n_row_blocks);
+  w = d;
+  d = fast_div(w, p.fd_heads);
+  const int h = (int)(w - d * p.n_kv_heads), r = (int)d;
+
+  const Request rq = request_of(p, r);
+  const int rows = rq.n * p.group;
+  const int row_first = rb * kRows, row_end = min(rows, row_first + kRows);
+  if (row_first >= rows) return;
+  const int i_first = (int)fast_div((uint32_t)row_first, p.fd_group);
+  const int i_last = (int)fast_div((uint32_t)row_end - 1, p.fd_group);
+  Keys keys;
+  keys.table = p.page_table + (int64_t)r * p.pt_stride;
+  keys.hi = min(last_key(p, rq, i_last), rq.kv - 1);
+  keys.lo = first_key(p, last_key(p, rq, i_first));
+  keys.part0 = keys.lo >> 4;
+  keys.part1 = (keys.hi >> 4) + 1;
+  const int all_hi = last_key(p, rq, i_first), all_lo = first_key(p, last_key(p, rq, i_last));
+  const int tile0 = keys.lo / kTileKeys, tile1 = (keys.hi + kTileKeys) / kTileKeys;   // hi = -1: none
+  const int per = (max(tile1 - tile0, 0) + p.n_splits - 1) / p.n_splits;
+  const int t_begin = tile0 + split * per, t_end = min(tile1, t_begin + per);
+
+  // this wave's rows
+  const int wave_row = row_first + wave * RT * 32;
+  bf16x8 qf[RT][KS];
+  int row_hi[RT], row_lo[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int row = wave_row + t * 32 + c32;
+    const int i = (int)fast_div((uint32_t)row, p.fd_group), hq = row - i * p.group;
+    const bool there = row < row_end;
+    row_hi[t] = there ? min(last_key(p, rq, i), rq.kv - 1) : -1;
+    row_lo[t] = there ? first_key(p, last_key(p, rq, i)) : 0;
+    const uint16_t* src = p.q + (rq.row0 + i) * p.q_s[0] + ((int64_t)h * p.group + hq) * p.q_s[1] + hf * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      u32x4 x = {0u, 0u, 0u, 0u};
+      if (there) x = *reinterpret_cast<const u32x4*>(src + ks * 16) ^ p.q_sign;
+      qf[t][ks] = __builtin_bit_cast(bf16x8, x);
+    }
+  }
+
+  f32x16 o[RT][DT];
+  float m[RT], l[RT], lx[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    m[t] = kLow;
+    l[t] = lx[t] = 0.f;
+#pragma unroll
+    for (int b = 0; b < DT; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[t][b][i] = 0.f;
+  }
+
+  Stage<D, FMT> st;
+  uint32_t bad = 0, bad_next = 0;
+  auto is_partial = [&](int tile, uint32_t missing) {
+    return missing != 0 || tile * kTileKeys + kTileKeys - 1 > all_hi || tile * kTileKeys < all_lo;
+  };
+  if (threadIdx.x == 0) s_odd = 0;
+  __syncthreads();
+  if (t_begin < t_end) {
+    load_tile<D, FMT>(p, keys, t_begin, h, wave, st, bad);
+    u32x4* buf = s_buf + (t_begin & 1) * kBuf;
+    if (store_tile<D, FMT>(st, buf, reinterpret_cast<u32x2*>(buf + kTileKeys * KC), is_partial(t_begin, bad), keys))
+      s_odd = 1;
+  }
+  __syncthreads();
+
+  for (int tile = t_begin; tile < t_end; ++tile) {
+    const u32x4* kb = s_buf + (tile & 1) * kBuf;
+    const u32x4* vb = kb + kTileKeys * KC;
+    if (tile + 1 < t_end) load_tile<D, FMT>(p, keys, tile + 1, h, wave, st, bad_next);
+    const bool partial = is_partial(tile, bad);
+
+    f32x16 sc[RT][2];
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[t][u][i] = 0.f;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const bf16x8 a = __builtin_bit_cast(bf16x8, kb[chunk_at<KC>(u * 32 + c32, 2 * ks + hf)]);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) sc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[t][ks], sc[t][u], 0, 0, 0);
+      }
+
+    bf16x8 pf[RT][4];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      if (partial) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int off = u * 32 + 8 * (i >> 2) + 4 * hf + (i & 3), pos = tile * kTileKeys + off;
+            const bool seen = pos >= row_lo[t] && pos <= row_hi[t] && ((bad >> (u * 2 + (i >> 3))) & 1) == 0;
+            sc[t][u][i] = seen ? sc[t][u][i] : -INFINITY;
+          }
+      }
+      float top = fmaxf(sc[t][0][0], sc[t][1][0]);
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, fmaxf(sc[t][0][i], sc[t][1][i]));
+      top *= p.scale2;
+      if (__ballot(top > m[t] + kSlack) != 0) {
+        const float m_new = fmaxf(m[t], max_x32(top));
+        const float down = exp2_fast(m[t] - m_new);
+        m[t] = m_new;
+        l[t] *= down;
+        lx[t] *= down;
+#pragma unroll
+        for (int b = 0; b < DT; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[t][b][i] *= down;
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = exp2_fast(__builtin_fmaf(sc[t][u][i], p.scale2, -m[t]));
+        if (p.lse != nullptr) {
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) lx[t] += (x[i] + x[i + 1]) + (x[i + 2] + x[i + 3]);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const u32x4 w = {pack_bf16x2(x[8 * s], x[8 * s + 1]), pack_bf16x2(x[8 * s + 2], x[8 * s + 3]),
+                           pack_bf16x2(x[8 * s + 4], x[8 * s + 5]), pack_bf16x2(x[8 * s + 6], x[8 * s + 7])};
+          l[t] = add_pair(w.w, add_pair(w.z, add_pair(w.y, add_pair(w.x, l[t]))));
+          pf[t][u * 2 + s] = __builtin_bit_cast(bf16x8, w);
+        }
+      }
+    }
+
+#pragma unroll
+    for (int b = 0; b < DT; ++b)
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const bf16x8 a = __builtin_bit_cast(bf16x8, vb[chunk_at<8>(b * 32 + c32, 2 * s + hf)]);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) o[t][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf[t][s], o[t][b], 0, 0, 0);
+      }
+
+    bad = bad_next;
+    if (tile + 1 < t_end) {
+      u32x4* buf = s_buf + ((tile + 1) & 1) * kBuf;
+      if (store_tile<D, FMT>(st, buf, reinterpret_cast<u32x2*>(buf + kTileKeys * KC), is_partial(tile + 1, bad), keys))
+        s_odd = 1;
+    }
+    __syncthreads();
+  }
+
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int row = wave_row + t * 32 + c32;
+    const float ll = sum_x32(l[t]), lxx = sum_x32(lx[t]);
+    if (row >= row_end) continue;
+    if (p.n_splits > 1) {
+      const int64_t at = (((int64_t)r * p.n_kv_heads + h) * p.rows_max + row) * p.n_splits + split;
+#pragma unroll
+      for (int b = 0; b < DT; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<f32x4*>(p.part_o + at * D + b * 32 + 2 * i + 4 * hf) =
+              f32x4{o[t][b][i], o[t][b][i + 1], o[t][b][i + 2], o[t][b][i + 3]};
+      if (hf == 0) {
+        *reinterpret_cast<f32x4*>(p.part_ml + at * 4) = f32x4{m[t], ll, lxx, 0.f};
+      }
+    } else {
+      const int i = (int)fast_div((uint32_t)row, p.fd_group);
+      const int64_t hq = (int64_t)h * p.group + (row - i * p.group);
+      const float inv = ll == 0.f ? 0.f : 1.0f / ll;
+      uint16_t* dst = p.out + (rq.row0 + i) * p.out_s[0] + hq * p.out_s[1] + 4 * hf;
+#pragma unroll
+      for (int b = 0; b < DT; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+          *reinterpret_cast<u32x2*>(dst + b * 32 + 2 * e) =
+              u32x2{pack_bf16x2(o[t][b][e] * inv, o[t][b][e + 1] * inv),
+                    pack_bf16x2(o[t][b][e + 2] * inv, o[t][b][e + 3] * inv)};
+      if (p.lse != nullptr && hf == 0)
+        p.lse[(rq.row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] = row_lse(m[t], lxx);
+    }
+  }
+  if (s_odd)
+    add_nonfinite<D, FMT>(p, rq, keys.table, nullptr, keys.part0, keys.part1, t_begin * 4, t_end * 4, 4, all_lo, all_hi,
+                          h, r, row_first, row_end, split);
+}
+
+namespace {
+
+template <int D, int FMT, int RT>
+hipError_t launch_one(const AttendParams& p, hipStream_t s) {
+  static std::atomic<bool> done[kMaxDevices];
+  const int lds = 2 * (kTileKeys * (D / 8) + D * 8) * 16;
+  const hipError_t e = ensure_lds_limit((const void*)attend_tiles_kernel<D, FMT, RT>, lds, done);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((attend_tiles_kernel<D, FMT, RT>), dim3((uint32_t)p.per_xcd * 8), dim3(kTileThreads), lds, s, p);
+  return hipGetLastError();
+}
+
+template <int RT>
+hipError_t launch_rt(const AttendParams& p, hipStream_t s) {
+  if (p.cache_type == KAMERA_CACHE_E4M3)
+    return p.head_dim == 128 ? launch_one<128, KAMERA_CACHE_E4M3, RT>(p, s) : launch_one<64, KAMERA_CACHE_E4M3, RT>(p, s);
+  return p.head_dim == 128 ? launch_one<128, KAMERA_CACHE_BF16, RT>(p, s) : launch_one<64, KAMERA_CACHE_BF16, RT>(p, s);
+}
+
+}  // namespace
+
+hipError_t launch_attend_tiles(const AttendParams& p, hipStream_t s) {
+  return p.row_tiles == 1 ? launch_rt<1>(p, s) : launch_rt<2>(p, s);
+}
+
+}  // namespace kamera
