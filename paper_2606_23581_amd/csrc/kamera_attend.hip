@@ -59,21 +59,22 @@ struct Step {
   u32x4 k[2][Tile<D, FMT>::kLoads];
   uint32_t v[2][4][Tile<D, FMT>::kVW];
   float ks[2], vs[2];
-  int page[2], pos[2];
+  int pos[2];
+  uint32_t ok;                                     // bit u: part u is in the pool
 };
 
+// Parts `lane` and `lane + 1` of a batch.
 template <int D, int FMT>
-__device__ __forceinline__ void load_step(const AttendParams& p, const int32_t* table, const int32_t* sel, int part0,
-                                          int part1, int step, int h, uint32_t k_lane, uint32_t v_lane, Step<D, FMT>& s) {
+__device__ __forceinline__ void load_step(const AttendParams& p, const Parts& a, int lane, int h, uint32_t k_lane,
+                                          uint32_t v_lane, Step<D, FMT>& s) {
   using T = Tile<D, FMT>;
+  s.ok = (uint32_t)(a.ok >> lane) & 3u;
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
-    const Part a = part_of(p, table, sel, part0, part1, 2 * step + u);
-    s.page[u] = a.page;
-    s.pos[u] = a.pos;
-    const int64_t page = a.page < 0 ? 0 : a.page;  // a page that may be read
-    const uint8_t* kb = p.k + page * p.k_s[0] + a.in_page * p.k_s[1] + h * p.k_s[2];
-    const uint8_t* vb = p.v + page * p.v_s[0] + a.in_page * p.v_s[1] + h * p.v_s[2];
+    s.pos[u] = lane_int(a.pos, lane + u);
+    const int64_t page = lane_int(a.page, lane + u), in_page = lane_int(a.in_page, lane + u);
+    const uint8_t* kb = p.k + page * p.k_s[0] + in_page * p.k_s[1] + h * p.k_s[2];
+    const uint8_t* vb = p.v + page * p.v_s[0] + in_page * p.v_s[1] + h * p.v_s[2];
 #pragma unroll
     for (int i = 0; i < T::kLoads; ++i) s.k[u][i] = *reinterpret_cast<const u32x4*>(kb + k_lane + i * 64);
     const uint32_t vt = (uint32_t)p.v_s[1];
@@ -91,12 +92,8 @@ __device__ __forceinline__ void load_step(const AttendParams& p, const int32_t* 
         for (int e = 0; e < T::kVW; ++e) s.v[u][j][e] = u4_get(w, e);
       }
     }
-    if (FMT == KAMERA_CACHE_E4M3) {
-      s.ks[u] = uniform_load(p.k_scale + page * p.k_scale_s[0] + h * p.k_scale_s[1]);
-      s.vs[u] = uniform_load(p.v_scale + page * p.v_scale_s[0] + h * p.v_scale_s[1]);
-    } else {
-      s.ks[u] = s.vs[u] = 1.0f;
-    }
+    s.ks[u] = lane_float(a.ks, lane + u);
+    s.vs[u] = lane_float(a.vs, lane + u);
   }
 }
 
@@ -150,7 +147,7 @@ __device__ __forceinline__ bool clear_unseen(Step<D, FMT>& s, int g, int lo, int
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int pos = s.pos[u] + 4 * g + j;
-      const bool keep = s.page[u] >= 0 && pos >= lo && pos <= hi;
+      const bool keep = ((s.ok >> u) & 1) && pos >= lo && pos <= hi;
 #pragma unroll
       for (int e = 0; e < Tile<D, FMT>::kVW; ++e) {
         const uint32_t w = keep ? s.v[u][j][e] : 0u;
@@ -192,18 +189,20 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_rows_kernel(AttendParam
   const int i_last = (int)fast_div((uint32_t)row_end - 1, p.fd_group);
 
   // keys that some row of the block sees, and those that every row sees
-  const int32_t* table = p.page_table + (int64_t)r * p.pt_stride;
-  const int32_t* sel = nullptr;
+  Walk walk;
+  walk.table = p.page_table + (int64_t)r * p.pt_stride;
+  walk.sel = nullptr;
   const int hi = min(last_key(p, rq, i_last), rq.kv - 1), all_hi = last_key(p, rq, i_first);
   const int lo = first_key(p, last_key(p, rq, i_first)), all_lo = first_key(p, last_key(p, rq, i_last));
-  int part0 = lo >> 4, part1 = (hi >> 4) + 1;
+  walk.begin = lo >> 4;
+  walk.end = (hi >> 4) + 1;
   if (p.sel != nullptr) {
     const int64_t at = (int64_t)r * p.n_kv_heads + h;
-    sel = p.sel + at * p.sel_stride;
-    part0 = 0;
-    part1 = min(max(uniform_load(p.sel_count + at), 0), p.sel_stride) * (p.page_size >> 4);
+    walk.sel = p.sel + at * p.sel_stride;
+    walk.begin = 0;
+    walk.end = min(max(uniform_load(p.sel_count + at), 0), p.sel_stride) * (p.page_size >> 4);
   }
-  const int step0 = part0 >> 1, step1 = (part1 + 1) >> 1;
+  const int step0 = walk.begin >> 1, step1 = (walk.end + 1) >> 1;
   const int n_steps = max(step1 - step0, 0);
   const int per = (n_steps + p.n_splits - 1) / p.n_splits;
   const int s_begin = step0 + split * per, s_end = min(step1, s_begin + per);
@@ -243,16 +242,26 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_rows_kernel(AttendParam
 
   if (threadIdx.x == 0) s_odd = 0;
   __syncthreads();
+  // The wave's steps s_begin + wave + 4 j, looked up 32 at a time: lane i has part
+  // i % 2 of step i / 2 of the batch.  The look-up of a batch is issued a batch ahead.
+  const int first = s_begin + wave, n_own = s_end > first ? (s_end - first + kAttWaves - 1) / kAttWaves : 0;
+  auto batch = [&](int j) {
+    return fetch_parts<FMT>(p, walk, j < n_own ? 2 * (first + (j + (lane >> 1)) * kAttWaves) + (lane & 1) : -1, h);
+  };
   Step<D, FMT> cur, nxt;
-  int step = s_begin + wave;
-  if (step < s_end) load_step<D, FMT>(p, table, sel, part0, part1, step, h, k_lane, v_lane, cur);
-  for (; step < s_end; step += kAttWaves) {
-    if (step + kAttWaves < s_end)
-      load_step<D, FMT>(p, table, sel, part0, part1, step + kAttWaves, h, k_lane, v_lane, nxt);
+  Parts parts = batch(0), ahead = batch(32);
+  if (n_own > 0) load_step<D, FMT>(p, parts, 0, h, k_lane, v_lane, cur);
+  for (int j = 0; j < n_own; ++j) {
+    if (j + 1 < n_own) {
+      if (((j + 1) & 31) == 0) {
+        parts = ahead;
+        ahead = batch(j + 33);
+      }
+      load_step<D, FMT>(p, parts, 2 * ((j + 1) & 31), h, k_lane, v_lane, nxt);
+    }
 
     // a step that some row does not see whole
-    const bool partial = cur.page[0] < 0 || cur.page[1] < 0 || max(cur.pos[0], cur.pos[1]) + 15 > all_hi ||
-                         min(cur.pos[0], cur.pos[1]) < all_lo;
+    const bool partial = cur.ok != 3u || max(cur.pos[0], cur.pos[1]) + 15 > all_hi || min(cur.pos[0], cur.pos[1]) < all_lo;
     if (partial && clear_unseen<D, FMT>(cur, g, lo, hi)) s_odd = 1;
 
     f32x4 sc[NR][2];
@@ -282,7 +291,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_rows_kernel(AttendParam
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int pos = cur.pos[u] + 4 * g + i;
-            const bool seen = cur.page[u] >= 0 && pos >= row_lo[t] && pos <= row_hi[t];
+            const bool seen = ((cur.ok >> u) & 1) && pos >= row_lo[t] && pos <= row_hi[t];
             x[u * 4 + i] = seen ? x[u * 4 + i] : -INFINITY;
           }
       }
@@ -381,8 +390,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_rows_kernel(AttendParam
     __syncthreads();
   }
   if (s_odd)
-    add_nonfinite<D, FMT>(p, rq, table, sel, part0, part1, 2 * s_begin, 2 * s_end, 2, all_lo, all_hi, h, r, row_first,
-                          row_end, split);
+    add_nonfinite<D, FMT>(p, rq, walk, 2 * s_begin, 2 * s_end, 2, all_lo, all_hi, h, r, row_first, row_end, split);
 }
 
 // Joins the parts of each row: with M the largest of the parts' maxima m_s,

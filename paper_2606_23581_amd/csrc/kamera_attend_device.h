@@ -98,39 +98,58 @@ __device__ __forceinline__ int first_key(const AttendParams& p, int last) {
   return p.window > 0 ? max(0, last - p.window + 1) : 0;
 }
 
-// One 16-token part of a page: where it is in the pool and in the request.
-struct Part {
-  int page;                          // -1: not in the pool, or past the end
+// 16-token parts of pages, one a lane: where each is in the pool and in the
+// request, and its scales.  A wave looks up 64 parts at once and then takes them
+// lane by lane as wave-uniform values, so that no look-up stands between two
+// steps of the walk.
+struct Parts {
+  int page;                          // a page that may be read, also where ok is clear
   int in_page;                       // first token within the page
   int pos;                           // first token of the request
+  float ks, vs;
+  uint64_t ok;                       // lanes whose part is in the pool
 };
 
-// Part number n of the walk over a request's keys: tokens [16 n, 16 n + 16), or
-// with selected pages the n-th part of those.  Parts outside [begin, end) are
-// not looked up: what lies before a window may have left the pool.
-__device__ __forceinline__ Part part_of(const AttendParams& p, const int32_t* table, const int32_t* sel, int begin,
-                                        int end, int n) {
-  Part a;
+// The walk over a request's keys: part n is tokens [16 n, 16 n + 16), or with
+// selected pages the n-th part of those.  Parts outside [begin, end) are not
+// looked up: what lies before a window may have left the pool.
+struct Walk {
+  const int32_t* table;
+  const int32_t* sel;
+  int begin, end;
+};
+
+template <int FMT>
+__device__ __forceinline__ Parts fetch_parts(const AttendParams& p, const Walk& w, int n, int h) {
+  Parts a;
   const int k = (int)fast_div((uint32_t)n, p.fd_page16);
   a.in_page = (n - k * (p.page_size >> 4)) * 16;
-  a.page = -1;
   a.pos = n * 16;
-  if (n >= begin && n < end) {
-    int idx = k;
-    if (sel != nullptr) {
-      idx = uniform_load(sel + k);
-      a.pos = idx * p.page_size + a.in_page;
+  int idx = k;
+  int page = -1;
+  const bool look = n >= w.begin && n < w.end;
+  if (look) {
+    if (w.sel != nullptr) {
+      idx = w.sel[k];
+      a.pos = (int)((uint32_t)idx * (uint32_t)p.page_size) + a.in_page;
     }
-    if (idx >= 0 && idx < p.pt_stride) {
-      a.page = uniform_load(table + idx);
-      if (a.page >= p.n_pool_pages) a.page = -1;
-    }
-    if (a.page < 0) {
-      a.page = -1;
-      if (p.status != nullptr && (threadIdx.x & 63) == 0) atomicOr(p.status, KAMERA_STATUS_BAD_PAGE);
-    }
+    if (idx >= 0 && idx < p.pt_stride) page = w.table[idx];
+  }
+  const bool ok = page >= 0 && page < p.n_pool_pages;
+  a.ok = __ballot(ok);
+  if (look && !ok && p.status != nullptr) atomicOr(p.status, KAMERA_STATUS_BAD_PAGE);
+  a.page = ok ? page : 0;
+  a.ks = a.vs = 1.0f;
+  if (FMT == KAMERA_CACHE_E4M3) {
+    a.ks = p.k_scale[a.page * p.k_scale_s[0] + h * p.k_scale_s[1]];
+    a.vs = p.v_scale[a.page * p.v_scale_s[0] + h * p.v_scale_s[1]];
   }
   return a;
+}
+
+__device__ __forceinline__ int lane_int(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ __forceinline__ float lane_float(float x, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
 }
 
 // A value that is not finite must reach the rows that see its token, and no
@@ -141,44 +160,47 @@ __device__ __forceinline__ Part part_of(const AttendParams& p, const int32_t* ta
 // tiles of the caller; all_lo, all_hi: the keys that every row of the block sees.
 // Called by all threads after their results are stored.
 template <int D, int FMT>
-__device__ __forceinline__ void add_nonfinite(const AttendParams& p, const Request& rq, const int32_t* table,
-                                           const int32_t* sel, int part0, int part1, int first, int end, int group,
-                                           int all_lo, int all_hi, int h, int r, int row_first, int row_end, int split) {
+__device__ __forceinline__ void add_nonfinite(const AttendParams& p, const Request& rq, const Walk& w, int first,
+                                              int end, int group, int all_lo, int all_hi, int h, int r, int row_first,
+                                              int row_end, int split) {
   constexpr int kEl = FMT == KAMERA_CACHE_BF16 ? 2 : 1;
   __threadfence();
   __syncthreads();
   const int col = threadIdx.x % D, sub = threadIdx.x / D, subs = kThreads / D;
   for (int g0 = first; g0 < end; g0 += group) {
+    const Parts a = fetch_parts<KAMERA_CACHE_BF16>(p, w, g0 + (int)(threadIdx.x & 63), h);   // scales are not needed
     bool partial = false;
-    for (int n = g0; n < g0 + group; ++n) {
-      const Part a = part_of(p, table, sel, part0, part1, n);
-      partial = partial || a.page < 0 || a.pos + 15 > all_hi || a.pos < all_lo;
+    for (int u = 0; u < group; ++u) {
+      const int pos = lane_int(a.pos, u);
+      partial = partial || ((a.ok >> u) & 1) == 0 || pos + 15 > all_hi || pos < all_lo;
     }
     if (!partial) continue;
-    for (int n = g0; n < g0 + group; ++n) {
-      const Part a = part_of(p, table, sel, part0, part1, n);
-      if (a.page < 0) continue;
-      const uint8_t* vb = p.v + a.page * p.v_s[0] + a.in_page * p.v_s[1] + h * p.v_s[2] + col * kEl;
-      for (int t = 0; t < 16 && a.pos + t < rq.kv; ++t) {
+    for (int u = 0; u < group; ++u) {
+      if (((a.ok >> u) & 1) == 0) continue;
+      const int pos = lane_int(a.pos, u);
+      const uint8_t* vb = p.v + (int64_t)lane_int(a.page, u) * p.v_s[0] + lane_int(a.in_page, u) * p.v_s[1] +
+                          h * p.v_s[2] + col * kEl;
+      for (int t = 0; t < 16 && pos + t < rq.kv; ++t) {
         float v;
         if (FMT == KAMERA_CACHE_BF16) {
-          const uint32_t w = *reinterpret_cast<const uint16_t*>(vb + t * p.v_s[1]);
-          if ((w & 0x7f80u) != 0x7f80u) continue;
-          v = bf_lo(w);
+          const uint32_t x = *reinterpret_cast<const uint16_t*>(vb + t * p.v_s[1]);
+          if ((x & 0x7f80u) != 0x7f80u) continue;
+          v = bf_lo(x);
         } else {
-          const uint32_t w = vb[t * p.v_s[1]];
-          if ((w & 0x7fu) != 0x7fu) continue;
+          const uint32_t x = vb[t * p.v_s[1]];
+          if ((x & 0x7fu) != 0x7fu) continue;
           v = __uint_as_float(0x7fc00000u);
         }
         for (int row = row_first + sub; row < row_end; row += subs) {
           const int i = (int)fast_div((uint32_t)row, p.fd_group);
           const int last = last_key(p, rq, i);
-          if (a.pos + t > last || a.pos + t < first_key(p, last)) continue;
+          if (pos + t > last || pos + t < first_key(p, last)) continue;
           if (p.n_splits > 1) {
             float* o = p.part_o + ((((int64_t)r * p.n_kv_heads + h) * p.rows_max + row) * p.n_splits + split) * D + col;
             *o += v;
           } else {
-            uint16_t* o = p.out + (rq.row0 + i) * p.out_s[0] + ((int64_t)h * p.group + (row - i * p.group)) * p.out_s[1] + col;
+            uint16_t* o =
+                p.out + (rq.row0 + i) * p.out_s[0] + ((int64_t)h * p.group + (row - i * p.group)) * p.out_s[1] + col;
             *o = (uint16_t)pack_bf16x2(bf_lo(*o) + v, 0.f);
           }
         }

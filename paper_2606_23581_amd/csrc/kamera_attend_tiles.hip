@@ -56,47 +56,25 @@ struct Stage {                                     // a thread's share of a tile
   int v_pos;                                       // first of the 4 tokens; very large: none
 };
 
-struct Keys {                                      // what a workgroup walks
-  const int32_t* table;
-  int lo, hi;                                      // keys that some row sees
-  int part0, part1;
-};
-
-__device__ __forceinline__ void find_part(const AttendParams& p, const Keys& w, int n, int& page, int& in_page) {
-  const Part a = part_of(p, w.table, nullptr, w.part0, w.part1, n);
-  page = __builtin_amdgcn_readfirstlane(a.page);
-  in_page = __builtin_amdgcn_readfirstlane(a.in_page);
-}
-
+// Tile number `tile` % 16 of a batch of looked-up parts.
 template <int D, int FMT>
-__device__ __forceinline__ void load_tile(const AttendParams& p, const Keys& w, int tile, int h, int wave,
+__device__ __forceinline__ void load_tile(const AttendParams& p, const Parts& a, int tile, int h, int wave,
                                           Stage<D, FMT>& s, uint32_t& bad) {
   using S = Stage<D, FMT>;
-  int pg0, pg1, pg2, pg3, in0, in1, in2, in3;
-  find_part(p, w, tile * 4, pg0, in0);
-  find_part(p, w, tile * 4 + 1, pg1, in1);
-  find_part(p, w, tile * 4 + 2, pg2, in2);
-  find_part(p, w, tile * 4 + 3, pg3, in3);
-  bad = (pg0 < 0 ? 1u : 0u) | (pg1 < 0 ? 2u : 0u) | (pg2 < 0 ? 4u : 0u) | (pg3 < 0 ? 8u : 0u);
-  auto pick = [](int u, int a, int b, int c, int d) {
-    const int x = (u & 1) ? b : a, y = (u & 1) ? d : c;
-    return (u & 2) ? y : x;
-  };
-  auto page_of = [&](int u) { return pick(u, pg0, pg1, pg2, pg3); };
-  auto first_of = [&](int u) { return pick(u, in0, in1, in2, in3); };
-  const int tid = threadIdx.x;
+  const int lane0 = (tile & 15) * 4, tid = threadIdx.x;
+  bad = ~(uint32_t)(a.ok >> lane0) & 15u;
 #pragma unroll
   for (int i = 0; i < S::KN; ++i) {
     // a wave's tokens of one load lie in one part
     const int unit = tid + i * kTileThreads, t = unit / S::kRowLoads, c = unit % S::kRowLoads;
-    const int u = (wave * 64 + i * kTileThreads) / S::kRowLoads / 16;
-    const int64_t page = max(page_of(u), 0);
-    const uint8_t* kb = p.k + page * p.k_s[0] + first_of(u) * p.k_s[1] + h * p.k_s[2];
+    const int u = lane0 + (wave * 64 + i * kTileThreads) / S::kRowLoads / 16;
+    const int64_t page = lane_int(a.page, u), in_page = lane_int(a.in_page, u);
+    const uint8_t* kb = p.k + page * p.k_s[0] + in_page * p.k_s[1] + h * p.k_s[2];
     s.k[i] = *reinterpret_cast<const u32x4*>(kb + (uint32_t)((t & 15) * (uint32_t)p.k_s[1] + c * 16));
-    s.ks[i] = FMT == KAMERA_CACHE_E4M3 ? uniform_load(p.k_scale + page * p.k_scale_s[0] + h * p.k_scale_s[1]) : 1.0f;
+    s.ks[i] = lane_float(a.ks, u);
   }
-  const int64_t page = max(page_of(wave), 0);
-  const uint8_t* vb = p.v + page * p.v_s[0] + first_of(wave) * p.v_s[1] + h * p.v_s[2];
+  const int64_t page = lane_int(a.page, lane0 + wave), in_page = lane_int(a.in_page, lane0 + wave);
+  const uint8_t* vb = p.v + page * p.v_s[0] + in_page * p.v_s[1] + h * p.v_s[2];
   const int q4 = (tid >> 4) & 3, cg = tid & 15;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -112,15 +90,16 @@ __device__ __forceinline__ void load_tile(const AttendParams& p, const Keys& w, 
       for (int e = 0; e < S::VW; ++e) s.v[j][e] = u4_get(x, e);
     }
   }
-  s.vs = FMT == KAMERA_CACHE_E4M3 ? uniform_load(p.v_scale + page * p.v_scale_s[0] + h * p.v_scale_s[1]) : 1.0f;
-  s.v_pos = page_of(wave) < 0 ? INT32_MAX - 16 : tile * kTileKeys + wave * 16 + q4 * 4;
+  s.vs = lane_float(a.vs, lane0 + wave);
+  s.v_pos = ((bad >> wave) & 1) ? INT32_MAX - 16 : tile * kTileKeys + wave * 16 + q4 * 4;
 }
 
 // Registers -> LDS.  With `clear`, V rows that no row of the block sees become
 // zero, and so does what is not finite in the others (the result says whether
 // there was any; see add_nonfinite).
 template <int D, int FMT>
-__device__ __forceinline__ bool store_tile(Stage<D, FMT>& s, u32x4* k_lds, u32x2* v_lds, bool clear, const Keys& w) {
+__device__ __forceinline__ bool store_tile(Stage<D, FMT>& s, u32x4* k_lds, u32x2* v_lds, bool clear, int lo,
+                                           int hi) {
   using S = Stage<D, FMT>;
   constexpr int KC = D / 8;                        // chunks of a K row in LDS
   const int tid = threadIdx.x;
@@ -143,7 +122,7 @@ __device__ __forceinline__ bool store_tile(Stage<D, FMT>& s, u32x4* k_lds, u32x2
   if (clear) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const bool keep = s.v_pos + j >= w.lo && s.v_pos + j <= w.hi;
+      const bool keep = s.v_pos + j >= lo && s.v_pos + j <= hi;
 #pragma unroll
       for (int e = 0; e < S::VW; ++e) {
         s.v[j][e] = keep ? s.v[j][e] : 0u;
@@ -208,14 +187,15 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_ke
   if (row_first >= rows) return;
   const int i_first = (int)fast_div((uint32_t)row_first, p.fd_group);
   const int i_last = (int)fast_div((uint32_t)row_end - 1, p.fd_group);
-  Keys keys;
-  keys.table = p.page_table + (int64_t)r * p.pt_stride;
-  keys.hi = min(last_key(p, rq, i_last), rq.kv - 1);
-  keys.lo = first_key(p, last_key(p, rq, i_first));
-  keys.part0 = keys.lo >> 4;
-  keys.part1 = (keys.hi >> 4) + 1;
+  Walk walk;
+  walk.table = p.page_table + (int64_t)r * p.pt_stride;
+  walk.sel = nullptr;
+  // keys that some row of the block sees, and those that every row sees
+  const int hi = min(last_key(p, rq, i_last), rq.kv - 1), lo = first_key(p, last_key(p, rq, i_first));
+  walk.begin = lo >> 4;
+  walk.end = (hi >> 4) + 1;
   const int all_hi = last_key(p, rq, i_first), all_lo = first_key(p, last_key(p, rq, i_last));
-  const int tile0 = keys.lo / kTileKeys, tile1 = (keys.hi + kTileKeys) / kTileKeys;   // hi = -1: none
+  const int tile0 = lo / kTileKeys, tile1 = (hi + kTileKeys) / kTileKeys;   // hi = -1: none
   const int per = (max(tile1 - tile0, 0) + p.n_splits - 1) / p.n_splits;
   const int t_begin = tile0 + split * per, t_end = min(tile1, t_begin + per);
 
@@ -258,10 +238,13 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_ke
   };
   if (threadIdx.x == 0) s_odd = 0;
   __syncthreads();
+  // parts looked up 16 tiles at a time, a batch ahead
+  auto batch = [&](int tile) { return fetch_parts<FMT>(p, walk, tile < t_end ? (tile & ~15) * 4 + lane : -1, h); };
+  Parts parts = batch(t_begin), ahead = batch((t_begin & ~15) + 16);
   if (t_begin < t_end) {
-    load_tile<D, FMT>(p, keys, t_begin, h, wave, st, bad);
+    load_tile<D, FMT>(p, parts, t_begin, h, wave, st, bad);
     u32x4* buf = s_buf + (t_begin & 1) * kBuf;
-    if (store_tile<D, FMT>(st, buf, reinterpret_cast<u32x2*>(buf + kTileKeys * KC), is_partial(t_begin, bad), keys))
+    if (store_tile<D, FMT>(st, buf, reinterpret_cast<u32x2*>(buf + kTileKeys * KC), is_partial(t_begin, bad), lo, hi))
       s_odd = 1;
   }
   __syncthreads();
@@ -269,7 +252,13 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_ke
   for (int tile = t_begin; tile < t_end; ++tile) {
     const u32x4* kb = s_buf + (tile & 1) * kBuf;
     const u32x4* vb = kb + kTileKeys * KC;
-    if (tile + 1 < t_end) load_tile<D, FMT>(p, keys, tile + 1, h, wave, st, bad_next);
+    if (tile + 1 < t_end) {
+      if (((tile + 1) & 15) == 0) {
+        parts = ahead;
+        ahead = batch(tile + 17);
+      }
+      load_tile<D, FMT>(p, parts, tile + 1, h, wave, st, bad_next);
+    }
     const bool partial = is_partial(tile, bad);
 
     f32x16 sc[RT][2];
@@ -347,7 +336,7 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_ke
     bad = bad_next;
     if (tile + 1 < t_end) {
       u32x4* buf = s_buf + ((tile + 1) & 1) * kBuf;
-      if (store_tile<D, FMT>(st, buf, reinterpret_cast<u32x2*>(buf + kTileKeys * KC), is_partial(tile + 1, bad), keys))
+      if (store_tile<D, FMT>(st, buf, reinterpret_cast<u32x2*>(buf + kTileKeys * KC), is_partial(tile + 1, bad), lo, hi))
         s_odd = 1;
     }
     __syncthreads();
@@ -386,8 +375,7 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_ke
     }
   }
   if (s_odd)
-    add_nonfinite<D, FMT>(p, rq, keys.table, nullptr, keys.part0, keys.part1, t_begin * 4, t_end * 4, 4, all_lo, all_hi,
-                          h, r, row_first, row_end, split);
+    add_nonfinite<D, FMT>(p, rq, walk, t_begin * 4, t_end * 4, 4, all_lo, all_hi, h, r, row_first, row_end, split);
 }
 
 namespace {
