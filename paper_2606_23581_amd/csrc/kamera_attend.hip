@@ -65,16 +65,15 @@ struct Step {
 
 // Parts `lane` and `lane + 1` of a batch.
 template <int D, int FMT>
-__device__ __forceinline__ void load_step(const AttendParams& p, const Parts& a, int lane, int h, uint32_t k_lane,
-                                          uint32_t v_lane, Step<D, FMT>& s) {
+__device__ __forceinline__ void load_step(const AttendParams& p, const Parts& a, int lane, uint32_t k_lane, uint32_t v_lane,
+                                          Step<D, FMT>& s) {
   using T = Tile<D, FMT>;
   s.ok = (uint32_t)(a.ok >> lane) & 3u;
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     s.pos[u] = lane_int(a.pos, lane + u);
-    const int64_t page = lane_int(a.page, lane + u), in_page = lane_int(a.in_page, lane + u);
-    const uint8_t* kb = p.k + page * p.k_s[0] + in_page * p.k_s[1] + h * p.k_s[2];
-    const uint8_t* vb = p.v + page * p.v_s[0] + in_page * p.v_s[1] + h * p.v_s[2];
+    const uint8_t* kb = lane_address(a.k, lane + u);
+    const uint8_t* vb = lane_address(a.v, lane + u);
 #pragma unroll
     for (int i = 0; i < T::kLoads; ++i) s.k[u][i] = *reinterpret_cast<const u32x4*>(kb + k_lane + i * 64);
     const uint32_t vt = (uint32_t)p.v_s[1];
@@ -250,14 +249,14 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_rows_kernel(AttendParam
   };
   Step<D, FMT> cur, nxt;
   Parts parts = batch(0), ahead = batch(32);
-  if (n_own > 0) load_step<D, FMT>(p, parts, 0, h, k_lane, v_lane, cur);
+  if (n_own > 0) load_step<D, FMT>(p, parts, 0, k_lane, v_lane, cur);
   for (int j = 0; j < n_own; ++j) {
     if (j + 1 < n_own) {
       if (((j + 1) & 31) == 0) {
         parts = ahead;
         ahead = batch(j + 33);
       }
-      load_step<D, FMT>(p, parts, 2 * ((j + 1) & 31), h, k_lane, v_lane, nxt);
+      load_step<D, FMT>(p, parts, 2 * ((j + 1) & 31), k_lane, v_lane, nxt);
     }
 
     // a step that some row does not see whole
@@ -295,7 +294,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_rows_kernel(AttendParam
             x[u * 4 + i] = seen ? x[u * 4 + i] : -INFINITY;
           }
       }
-      float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) * p.scale2;
+      float top = max2(max2(max2(x[0], x[1]), max2(x[2], x[3])), max2(max2(x[4], x[5]), max2(x[6], x[7]))) * p.scale2;
       if (__ballot(top > m[t] + kSlack) != 0) {
         top = max_x32(max_x16(top));
         const float m_new = fmaxf(m[t], top);

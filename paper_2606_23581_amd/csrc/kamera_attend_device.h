@@ -27,6 +27,10 @@ __device__ __forceinline__ T uniform_load(const T* p) {
   return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
 }
 
+// The larger of two, NaN if one is: v_maximum3_f32 for two of these, with none of
+// the quieting that fmaxf needs.
+__device__ __forceinline__ float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 // The largest / sum over the lanes l, l ^ 32 and (groups of 16) l ^ 16, l ^ 32.
 __device__ __forceinline__ float max_x32(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -103,8 +107,7 @@ __device__ __forceinline__ int first_key(const AttendParams& p, int last) {
 // lane by lane as wave-uniform values, so that no look-up stands between two
 // steps of the walk.
 struct Parts {
-  int page;                          // a page that may be read, also where ok is clear
-  int in_page;                       // first token within the page
+  uint64_t k, v;                     // address of its first K and V row, readable also where ok is clear
   int pos;                           // first token of the request
   float ks, vs;
   uint64_t ok;                       // lanes whose part is in the pool
@@ -123,7 +126,7 @@ template <int FMT>
 __device__ __forceinline__ Parts fetch_parts(const AttendParams& p, const Walk& w, int n, int h) {
   Parts a;
   const int k = (int)fast_div((uint32_t)n, p.fd_page16);
-  a.in_page = (n - k * (p.page_size >> 4)) * 16;
+  const int in_page = (n - k * (p.page_size >> 4)) * 16;
   a.pos = n * 16;
   int idx = k;
   int page = -1;
@@ -131,23 +134,30 @@ __device__ __forceinline__ Parts fetch_parts(const AttendParams& p, const Walk& 
   if (look) {
     if (w.sel != nullptr) {
       idx = w.sel[k];
-      a.pos = (int)((uint32_t)idx * (uint32_t)p.page_size) + a.in_page;
+      a.pos = (int)((uint32_t)idx * (uint32_t)p.page_size) + in_page;
     }
     if (idx >= 0 && idx < p.pt_stride) page = w.table[idx];
   }
   const bool ok = page >= 0 && page < p.n_pool_pages;
   a.ok = __ballot(ok);
   if (look && !ok && p.status != nullptr) atomicOr(p.status, KAMERA_STATUS_BAD_PAGE);
-  a.page = ok ? page : 0;
+  const int64_t pg = ok ? page : 0, at = look ? in_page : 0;
+  a.k = (uint64_t)p.k + pg * p.k_s[0] + at * p.k_s[1] + h * p.k_s[2];
+  a.v = (uint64_t)p.v + pg * p.v_s[0] + at * p.v_s[1] + h * p.v_s[2];
   a.ks = a.vs = 1.0f;
   if (FMT == KAMERA_CACHE_E4M3) {
-    a.ks = p.k_scale[a.page * p.k_scale_s[0] + h * p.k_scale_s[1]];
-    a.vs = p.v_scale[a.page * p.v_scale_s[0] + h * p.v_scale_s[1]];
+    a.ks = p.k_scale[pg * p.k_scale_s[0] + h * p.k_scale_s[1]];
+    a.vs = p.v_scale[pg * p.v_scale_s[0] + h * p.v_scale_s[1]];
   }
   return a;
 }
 
 __device__ __forceinline__ int lane_int(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ __forceinline__ const uint8_t* lane_address(uint64_t x, int lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, lane);
+  const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(x >> 32), lane);
+  return reinterpret_cast<const uint8_t*>(((uint64_t)hi << 32) | lo);
+}
 __device__ __forceinline__ float lane_float(float x, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
 }
@@ -168,7 +178,8 @@ __device__ __forceinline__ void add_nonfinite(const AttendParams& p, const Reque
   __syncthreads();
   const int col = threadIdx.x % D, sub = threadIdx.x / D, subs = kThreads / D;
   for (int g0 = first; g0 < end; g0 += group) {
-    const Parts a = fetch_parts<KAMERA_CACHE_BF16>(p, w, g0 + (int)(threadIdx.x & 63), h);   // scales are not needed
+    const int lane = threadIdx.x & 63;
+    const Parts a = fetch_parts<KAMERA_CACHE_BF16>(p, w, lane < group ? g0 + lane : -1, h);   // no scales needed
     bool partial = false;
     for (int u = 0; u < group; ++u) {
       const int pos = lane_int(a.pos, u);
@@ -178,8 +189,7 @@ __device__ __forceinline__ void add_nonfinite(const AttendParams& p, const Reque
     for (int u = 0; u < group; ++u) {
       if (((a.ok >> u) & 1) == 0) continue;
       const int pos = lane_int(a.pos, u);
-      const uint8_t* vb = p.v + (int64_t)lane_int(a.page, u) * p.v_s[0] + lane_int(a.in_page, u) * p.v_s[1] +
-                          h * p.v_s[2] + col * kEl;
+      const uint8_t* vb = lane_address(a.v, u) + col * kEl;
       for (int t = 0; t < 16 && pos + t < rq.kv; ++t) {
         float v;
         if (FMT == KAMERA_CACHE_BF16) {

@@ -24,6 +24,7 @@
 // maximum passes the running one by more than 2^8.
 
 #include <algorithm>
+#include <type_traits>
 
 #include "kamera_attend_device.h"
 
@@ -36,12 +37,13 @@ constexpr int kTileKeys = 64;
 constexpr float kLow = -3.402823466e38f;
 constexpr float kSlack = 8.0f;
 
-// Place of 16-byte chunk `c` of row `r` in a tile whose rows are 8 or 16 chunks.
+// Place of 16-byte chunk `c` of row `r`: K rows of 16 or 8 chunks (the exchange
+// repeats every 16 rows), V^T rows of 8.
 template <int CHUNKS>
-__device__ __forceinline__ uint32_t chunk_at(uint32_t r, uint32_t c) {
-  if (CHUNKS == 16) return r * 16 + (c ^ (r & 15));
-  return r * 8 + (c ^ (((r >> 1) ^ (r >> 4)) & 7));
+__device__ __forceinline__ uint32_t k_chunk(uint32_t r, uint32_t c) {
+  return CHUNKS == 16 ? r * 16 + (c ^ (r & 15)) : r * 8 + (c ^ ((r >> 1) & 7));
 }
+__device__ __forceinline__ uint32_t v_chunk(uint32_t r, uint32_t c) { return r * 8 + (c ^ (((r >> 1) ^ (r >> 4)) & 7)); }
 
 template <int D, int FMT>
 struct Stage {                                     // a thread's share of a tile
@@ -53,32 +55,27 @@ struct Stage {                                     // a thread's share of a tile
   u32x4 k[KN];
   uint32_t v[4][VW];
   float ks[KN], vs;
-  int v_pos;                                       // first of the 4 tokens; very large: none
 };
 
-// Tile number `tile` % 16 of a batch of looked-up parts.
+// Tile number `tile` % 16 of a batch of looked-up parts.  k_off, v_off: this
+// thread's place in a 16-token part.
 template <int D, int FMT>
-__device__ __forceinline__ void load_tile(const AttendParams& p, const Parts& a, int tile, int h, int wave,
-                                          Stage<D, FMT>& s, uint32_t& bad) {
+__device__ __forceinline__ void load_tile(const Parts& a, int tile, int wave, uint32_t k_off, uint32_t v_off,
+                                          int64_t v_token, Stage<D, FMT>& s, uint32_t& bad) {
   using S = Stage<D, FMT>;
-  const int lane0 = (tile & 15) * 4, tid = threadIdx.x;
+  const int lane0 = (tile & 15) * 4;
   bad = ~(uint32_t)(a.ok >> lane0) & 15u;
 #pragma unroll
   for (int i = 0; i < S::KN; ++i) {
     // a wave's tokens of one load lie in one part
-    const int unit = tid + i * kTileThreads, t = unit / S::kRowLoads, c = unit % S::kRowLoads;
     const int u = lane0 + (wave * 64 + i * kTileThreads) / S::kRowLoads / 16;
-    const int64_t page = lane_int(a.page, u), in_page = lane_int(a.in_page, u);
-    const uint8_t* kb = p.k + page * p.k_s[0] + in_page * p.k_s[1] + h * p.k_s[2];
-    s.k[i] = *reinterpret_cast<const u32x4*>(kb + (uint32_t)((t & 15) * (uint32_t)p.k_s[1] + c * 16));
+    s.k[i] = *reinterpret_cast<const u32x4*>(lane_address(a.k, u) + k_off);
     s.ks[i] = lane_float(a.ks, u);
   }
-  const int64_t page = lane_int(a.page, lane0 + wave), in_page = lane_int(a.in_page, lane0 + wave);
-  const uint8_t* vb = p.v + page * p.v_s[0] + in_page * p.v_s[1] + h * p.v_s[2];
-  const int q4 = (tid >> 4) & 3, cg = tid & 15;
+  const uint8_t* vb = lane_address(a.v, lane0 + wave);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const uint8_t* at = vb + (uint32_t)((q4 * 4 + j) * (uint32_t)p.v_s[1] + cg * S::VC * S::kEl);
+    const uint8_t* at = vb + v_off;
     if (S::VW == 1) s.v[j][0] = *reinterpret_cast<const uint32_t*>(at);
     else if (S::VW == 2) {
       const u32x2 x = *reinterpret_cast<const u32x2*>(at);
@@ -89,30 +86,36 @@ __device__ __forceinline__ void load_tile(const AttendParams& p, const Parts& a,
 #pragma unroll
       for (int e = 0; e < S::VW; ++e) s.v[j][e] = u4_get(x, e);
     }
+    vb += v_token;
   }
   s.vs = lane_float(a.vs, lane0 + wave);
-  s.v_pos = ((bad >> wave) & 1) ? INT32_MAX - 16 : tile * kTileKeys + wave * 16 + q4 * 4;
 }
+
+// This thread's places in a buffer, in bytes.
+template <int D, int FMT>
+struct Places {
+  using S = Stage<D, FMT>;
+  uint32_t k[FMT == KAMERA_CACHE_E4M3 ? 2 : 1];    // its first K chunks; those of load i lie i * kTileThreads / kRowLoads rows on
+  uint32_t v[S::VC];
+};
 
 // Registers -> LDS.  With `clear`, V rows that no row of the block sees become
 // zero, and so does what is not finite in the others (the result says whether
 // there was any; see add_nonfinite).
 template <int D, int FMT>
-__device__ __forceinline__ bool store_tile(Stage<D, FMT>& s, u32x4* k_lds, u32x2* v_lds, bool clear, int lo,
-                                           int hi) {
+__device__ __forceinline__ bool store_tile(Stage<D, FMT>& s, uint8_t* buf, const Places<D, FMT>& at, bool clear,
+                                           uint32_t bad, int wave, int v_pos, int lo, int hi) {
   using S = Stage<D, FMT>;
-  constexpr int KC = D / 8;                        // chunks of a K row in LDS
-  const int tid = threadIdx.x;
 #pragma unroll
   for (int i = 0; i < S::KN; ++i) {
-    const int unit = tid + i * kTileThreads, t = unit / S::kRowLoads, c = unit % S::kRowLoads;
+    uint8_t* row = buf + i * (kTileThreads / S::kRowLoads) * D * 2;
     if (FMT == KAMERA_CACHE_BF16) {
-      k_lds[chunk_at<KC>(t, c)] = s.k[i];
+      *reinterpret_cast<u32x4*>(row + at.k[0]) = s.k[i];
     } else {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const uint32_t a = e ? s.k[i].z : s.k[i].x, b = e ? s.k[i].w : s.k[i].y;
-        k_lds[chunk_at<KC>(t, 2 * c + e)] =
+        *reinterpret_cast<u32x4*>(row + at.k[FMT == KAMERA_CACHE_E4M3 ? e : 0]) =
             u32x4{e4m3_to_bf16x2<false>(a, s.ks[i]), e4m3_to_bf16x2<true>(a, s.ks[i]),
                   e4m3_to_bf16x2<false>(b, s.ks[i]), e4m3_to_bf16x2<true>(b, s.ks[i])};
       }
@@ -120,9 +123,10 @@ __device__ __forceinline__ bool store_tile(Stage<D, FMT>& s, u32x4* k_lds, u32x2
   }
   uint32_t odd = 0;
   if (clear) {
+    const bool missing = (bad >> wave) & 1;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const bool keep = s.v_pos + j >= lo && s.v_pos + j <= hi;
+      const bool keep = !missing && v_pos + j >= lo && v_pos + j <= hi;
 #pragma unroll
       for (int e = 0; e < S::VW; ++e) {
         s.v[j][e] = keep ? s.v[j][e] : 0u;
@@ -131,10 +135,6 @@ __device__ __forceinline__ bool store_tile(Stage<D, FMT>& s, u32x4* k_lds, u32x2
       }
     }
   }
-  // tokens 4 q .. 4 q + 3 of the tile: run q % 4 of 16-token group q / 4
-  const int q = tid >> 4, cg = tid & 15;
-  const uint32_t run = (q & 3) == 1 ? 2 : ((q & 3) == 2 ? 1 : (q & 3));
-  const uint32_t chunk = (q >> 2) * 2 + (run >> 1), half = run & 1;
 #pragma unroll
   for (int c = 0; c < S::VC; ++c) {
     u32x2 r;
@@ -150,7 +150,7 @@ __device__ __forceinline__ bool store_tile(Stage<D, FMT>& s, u32x4* k_lds, u32x2
       }
       if (t == 0) r.x = y; else r.y = y;
     }
-    v_lds[chunk_at<8>(cg * S::VC + c, chunk) * 2 + half] = r;
+    *reinterpret_cast<u32x2*>(buf + at.v[c]) = r;
   }
   return odd != 0;
 }
@@ -162,8 +162,11 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_ke
   const AttendParams& p = kernel_params<AttendParams>();
   constexpr int KC = D / 8, KS = D / 16, DT = D / 32;
   constexpr int kRows = 4 * RT * 32;
-  constexpr int kBuf = kTileKeys * KC + D * 8;     // chunks of one buffer: K, then V^T
+  constexpr int kVAt = kTileKeys * D * 2;          // a buffer holds K, then V^T: bytes to V^T, and of both
+  constexpr int kBuf = 2 * kVAt;
+  using S = Stage<D, FMT>;
   extern __shared__ u32x4 s_buf[];
+  uint8_t* const lds = reinterpret_cast<uint8_t*>(s_buf);
   __shared__ int s_odd;                            // a value that is not finite was taken as 0
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -231,10 +234,36 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_ke
       for (int i = 0; i < 16; ++i) o[t][b][i] = 0.f;
   }
 
-  Stage<D, FMT> st;
+  // this thread's places in global memory and in LDS
+  const int tid = threadIdx.x, q4 = (tid >> 4) & 3, cg = tid & 15;
+  const uint32_t k_off = (uint32_t)((tid / S::kRowLoads & 15) * (uint32_t)p.k_s[1] + tid % S::kRowLoads * 16);
+  const uint32_t v_off = (uint32_t)(q4 * 4 * (uint32_t)p.v_s[1] + cg * S::VC * S::kEl);
+  const int64_t v_token = p.v_s[1];
+  Places<D, FMT> at;
+#pragma unroll
+  for (int e = 0; e < (FMT == KAMERA_CACHE_E4M3 ? 2 : 1); ++e)
+    at.k[e] = 16 * k_chunk<KC>(tid / S::kRowLoads, (FMT == KAMERA_CACHE_E4M3 ? 2 : 1) * (tid % S::kRowLoads) + e);
+  // tokens 4 q .. 4 q + 3 of the tile: run q % 4 of 16-token group q / 4
+  const uint32_t run = q4 == 1 ? 2 : (q4 == 2 ? 1 : q4);
+#pragma unroll
+  for (int c = 0; c < S::VC; ++c) at.v[c] = kVAt + 16 * v_chunk(cg * S::VC + c, wave * 2 + (run >> 1)) + 8 * (run & 1);
+  uint32_t k_at[KS], v_at[DT][4];                  // the chunks of its MFMA operands
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) k_at[ks] = 16 * k_chunk<KC>(c32, 2 * ks + hf);
+#pragma unroll
+  for (int b = 0; b < DT; ++b)
+#pragma unroll
+    for (int s = 0; s < 4; ++s) v_at[b][s] = kVAt + 16 * v_chunk(b * 32 + c32, 2 * s + hf);
+
+  S st;
   uint32_t bad = 0, bad_next = 0;
   auto is_partial = [&](int tile, uint32_t missing) {
     return missing != 0 || tile * kTileKeys + kTileKeys - 1 > all_hi || tile * kTileKeys < all_lo;
+  };
+  auto store = [&](int tile, uint32_t missing, uint8_t* buf) {
+    if (store_tile<D, FMT>(st, buf, at, is_partial(tile, missing), missing, wave, tile * kTileKeys + wave * 16 + q4 * 4,
+                           lo, hi))
+      s_odd = 1;
   };
   if (threadIdx.x == 0) s_odd = 0;
   __syncthreads();
@@ -242,22 +271,20 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_ke
   auto batch = [&](int tile) { return fetch_parts<FMT>(p, walk, tile < t_end ? (tile & ~15) * 4 + lane : -1, h); };
   Parts parts = batch(t_begin), ahead = batch((t_begin & ~15) + 16);
   if (t_begin < t_end) {
-    load_tile<D, FMT>(p, parts, t_begin, h, wave, st, bad);
-    u32x4* buf = s_buf + (t_begin & 1) * kBuf;
-    if (store_tile<D, FMT>(st, buf, reinterpret_cast<u32x2*>(buf + kTileKeys * KC), is_partial(t_begin, bad), lo, hi))
-      s_odd = 1;
+    load_tile<D, FMT>(parts, t_begin, wave, k_off, v_off, v_token, st, bad);
+    store(t_begin, bad, lds);
   }
   __syncthreads();
 
-  for (int tile = t_begin; tile < t_end; ++tile) {
-    const u32x4* kb = s_buf + (tile & 1) * kBuf;
-    const u32x4* vb = kb + kTileKeys * KC;
+  // One tile, from buffer B; the next one goes into the other.
+  auto step = [&](auto which, int tile) {
+    constexpr int B = decltype(which)::value * kBuf, kOther = kBuf - B;
     if (tile + 1 < t_end) {
       if (((tile + 1) & 15) == 0) {
         parts = ahead;
         ahead = batch(tile + 17);
       }
-      load_tile<D, FMT>(p, parts, tile + 1, h, wave, st, bad_next);
+      load_tile<D, FMT>(parts, tile + 1, wave, k_off, v_off, v_token, st, bad_next);
     }
     const bool partial = is_partial(tile, bad);
 
@@ -272,7 +299,7 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_ke
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const bf16x8 a = __builtin_bit_cast(bf16x8, kb[chunk_at<KC>(u * 32 + c32, 2 * ks + hf)]);
+        const bf16x8 a = *reinterpret_cast<const bf16x8*>(lds + k_at[ks] + (B + u * 32 * D * 2));
 #pragma unroll
         for (int t = 0; t < RT; ++t) sc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[t][ks], sc[t][u], 0, 0, 0);
       }
@@ -290,9 +317,9 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_ke
             sc[t][u][i] = seen ? sc[t][u][i] : -INFINITY;
           }
       }
-      float top = fmaxf(sc[t][0][0], sc[t][1][0]);
+      float top = max2(sc[t][0][0], sc[t][1][0]);
 #pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, fmaxf(sc[t][0][i], sc[t][1][i]));
+      for (int i = 1; i < 16; ++i) top = max2(max2(top, sc[t][0][i]), sc[t][1][i]);
       top *= p.scale2;
       if (__ballot(top > m[t] + kSlack) != 0) {
         const float m_new = fmaxf(m[t], max_x32(top));
@@ -328,18 +355,18 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_ke
     for (int b = 0; b < DT; ++b)
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
-        const bf16x8 a = __builtin_bit_cast(bf16x8, vb[chunk_at<8>(b * 32 + c32, 2 * s + hf)]);
+        const bf16x8 a = *reinterpret_cast<const bf16x8*>(lds + v_at[b][s] + B);
 #pragma unroll
         for (int t = 0; t < RT; ++t) o[t][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf[t][s], o[t][b], 0, 0, 0);
       }
 
     bad = bad_next;
-    if (tile + 1 < t_end) {
-      u32x4* buf = s_buf + ((tile + 1) & 1) * kBuf;
-      if (store_tile<D, FMT>(st, buf, reinterpret_cast<u32x2*>(buf + kTileKeys * KC), is_partial(tile + 1, bad), lo, hi))
-        s_odd = 1;
-    }
+    if (tile + 1 < t_end) store(tile + 1, bad, lds + kOther);
     __syncthreads();
+  };
+  for (int tile = t_begin; tile < t_end; tile += 2) {
+    step(std::integral_constant<int, 0>{}, tile);
+    if (tile + 1 < t_end) step(std::integral_constant<int, 1>{}, tile + 1);
   }
 
 #pragma unroll
@@ -383,7 +410,7 @@ namespace {
 template <int D, int FMT, int RT>
 hipError_t launch_one(const AttendParams& p, hipStream_t s) {
   static std::atomic<bool> done[kMaxDevices];
-  const int lds = 2 * (kTileKeys * (D / 8) + D * 8) * 16;
+  const int lds = 4 * kTileKeys * D * 2;
   const hipError_t e = ensure_lds_limit((const void*)attend_tiles_kernel<D, FMT, RT>, lds, done);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((attend_tiles_kernel<D, FMT, RT>), dim3((uint32_t)p.per_xcd * 8), dim3(kTileThreads), lds, s, p);
