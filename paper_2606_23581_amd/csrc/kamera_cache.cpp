@@ -333,11 +333,19 @@ int size_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& laun
     if (a->window > 0) span_keys = std::min<int64_t>(span_keys, (int64_t)a->window + a->n_queries);
     P.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / tasks, span_keys / 256), 512));
   }
-  const int64_t wgs = bounded_product({tasks, P.n_splits}), join = bounded_product({a->n_requests, a->n_kv_heads, rows});
-  if (wgs < 0 || join < 0 || (std::max(wgs, join) + 8) * 256 > 0xFFFFFFFFLL)
+  int64_t wgs = bounded_product({tasks, P.n_splits});
+  const int64_t join = bounded_product({a->n_requests, a->n_kv_heads, rows});
+  if (P.tiles) {
+    const int64_t pairs = (int64_t)a->n_requests * a->n_kv_heads;
+    // every request's work on all XCDs alike, whatever the lengths
+    P.deal = a->n_kv_heads % 8 == 0 ? 1 : (a->n_kv_heads % 4 == 0 ? 2 : (a->n_kv_heads % 2 == 0 ? 4 : 8));
+    P.blocks_share = (int32_t)ceil_div(P.n_row_blocks, P.deal);
+    wgs = bounded_product({pairs * P.deal, P.blocks_share, P.n_splits});
+    P.n_shares = (int32_t)std::min<int64_t>(pairs * P.deal / 8, INT32_MAX);
+  }
+  if (wgs < 0 || join < 0 || std::max(wgs, join) * 256 > 0xFFFFFFFFLL)
     return fail(KAMERA_ERR_RANGE, "%s: too many workgroups for one launch", who);
   P.n_tasks = (int32_t)wgs;
-  P.per_xcd = (int32_t)ceil_div(wgs, 8);
   if (P.n_splits > 1) {
     workspace = bounded_product({join, P.n_splits, a->head_dim + 4, 4});
     if (workspace < 0) return fail(KAMERA_ERR_RANGE, "%s: workspace too large", who);
@@ -449,6 +457,8 @@ int build_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& lau
   P.fd_blocks = kamera::make_fast_div((uint32_t)P.n_row_blocks);
   P.fd_splits = kamera::make_fast_div((uint32_t)P.n_splits);
   P.fd_rows = kamera::make_fast_div((uint32_t)P.rows_max);
+  P.fd_shares = kamera::make_fast_div((uint32_t)std::max(P.n_shares, 1));
+  P.fd_deal = kamera::make_fast_div((uint32_t)std::max(P.deal, 1));
   P.fd_page16 = kamera::make_fast_div((uint32_t)a->page_size / 16);
   P.fd_page = kamera::make_fast_div((uint32_t)a->page_size);
   launch = true;

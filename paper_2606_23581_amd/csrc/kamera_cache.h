@@ -102,9 +102,11 @@ struct AttendParams {
   int32_t tiles;                     // 1: the many-rows kernel
   int32_t row_tiles;                 // tiles of 16 (few-rows) or 32 (many-rows kernel) rows a wave
   int32_t n_row_blocks;
-  int32_t n_tasks;                   // workgroups with work
-  int32_t per_xcd;                   // of these on an XCD (many-rows kernel)
-  FastDiv fd_group, fd_heads, fd_blocks, fd_splits, fd_rows;
+  int32_t n_tasks;                   // workgroups
+  int32_t deal;                      // many-rows kernel: shares that a (request, KV head) pair's row blocks
+  int32_t n_shares;                  // are dealt into, shares on an XCD, row blocks of a share
+  int32_t blocks_share;
+  FastDiv fd_group, fd_heads, fd_blocks, fd_splits, fd_rows, fd_shares, fd_deal;
   FastDiv fd_page16, fd_page;        // by page_size / 16 and page_size
 };
 
