@@ -12,8 +12,7 @@
 // page in registers between the maximum and the conversion, so rows are read
 // once; the page's key sums come from the converted bytes that it still holds.
 
-#include "kamera_cache.h"
-#include "kamera_device.h"
+#include "kamera_cache_device.h"
 
 namespace kamera {
 
@@ -74,16 +73,16 @@ __global__ __launch_bounds__(kAppThreads) void append_kernel(AppendParams) {
   q = fast_div(u, p.fd_layers);
   const int l = (int)(u - q * p.n_layers), c = (int)q;
 
-  const int before = p.tokens_before != nullptr ? max(p.tokens_before[c], 0) : 0;
-  int n = p.n_tokens;
-  if (p.chunk_tokens != nullptr) n = min(max(p.chunk_tokens[c], 0), n);
+  const int base = load_or(p.row_base, c, 0, p.page_table);
+  const int before = max(load_or(p.tokens_before, c, 0, p.page_table), 0);
+  const int n = min(max(load_or(p.chunk_tokens, c, p.n_tokens, p.page_table), 0), p.n_tokens);
   const int64_t j = before / P + jp;               // page of the chunk
   const int64_t p0 = j * P;
   const int64_t lo64 = max((int64_t)before, p0) - p0, hi64 = min((int64_t)before + n, p0 + P) - p0;
   if (hi64 <= lo64) return;
   const int lo = (int)lo64, hi = (int)hi64;        // new tokens of the page: [lo, hi)
   int page = -1;
-  if (j < p.pt_stride) page = p.page_table[(int64_t)c * p.pt_stride + j];
+  if (j < p.pt_stride) page = uniform_load(p.page_table + (int64_t)c * p.pt_stride + j);
   if (page < 0 || page >= p.n_pool_pages) {
     if (lane == 0 && p.status != nullptr)
       atomicOr(p.status, j < p.pt_stride ? KAMERA_STATUS_BAD_PAGE : KAMERA_STATUS_BAD_LENGTH);
@@ -92,7 +91,7 @@ __global__ __launch_bounds__(kAppThreads) void append_kernel(AppendParams) {
 
   const AppendPlane& pp = p.plane[pl];
   const int t_lane = lane / LPR, col = (lane % LPR) * 8;
-  const int64_t row0 = p0 - before + (p.row_base != nullptr ? p.row_base[c] : 0);   // row of the page's token 0
+  const int64_t row0 = p0 - before + base;         // row of the page's token 0
   const uint16_t* rows = pp.rows + c * pp.rows_s[0] + l * pp.rows_s[1] + h * pp.rows_s[3] + col;
   u32x4 x[IT];
   uint32_t top = 0;

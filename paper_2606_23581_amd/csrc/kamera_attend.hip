@@ -91,6 +91,10 @@ __device__ __forceinline__ void load_step(const AttendParams& p, const Parts& a,
         for (int e = 0; e < T::kVW; ++e) s.v[u][j][e] = u4_get(w, e);
       }
     }
+  }
+  // after the loads: these wait for the look-up's scales
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
     s.ks[u] = lane_float(a.ks, lane + u);
     s.vs[u] = lane_float(a.vs, lane + u);
   }
@@ -166,7 +170,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_rows_kernel(AttendParam
   constexpr int kPad = 4;
   __shared__ float s_o[kAttWaves][16][D + kPad];
   __shared__ float s_ml[kAttWaves][NR * 16][3];
-  __shared__ int s_odd;                            // a value that is not finite was taken as 0
+  __shared__ int s_odd[kAttWaves];                 // a value that is not finite was taken as 0
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, g = lane >> 4;
@@ -206,6 +210,29 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_rows_kernel(AttendParam
   const int per = (n_steps + p.n_splits - 1) / p.n_splits;
   const int s_begin = step0 + split * per, s_end = min(step1, s_begin + per);
 
+  f32x4 o[NR][T::VC];
+  float m[NR], l[NR], lx[NR];
+#pragma unroll
+  for (int t = 0; t < NR; ++t) {
+    m[t] = kLow;
+    l[t] = lx[t] = 0.f;
+#pragma unroll
+    for (int b = 0; b < T::VC; ++b) o[t][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const uint32_t k_lane = (uint32_t)(c16 * p.k_s[1]) + g * 16;
+  const uint32_t v_lane = (uint32_t)(4 * g * p.v_s[1]) + c16 * T::VC * T::kEl;
+
+  // The wave's steps s_begin + wave + 4 j, looked up 32 at a time: lane i has part
+  // i % 2 of step i / 2 of the batch.  The look-up of a batch is issued a batch ahead.
+  const int first = s_begin + wave, n_own = s_end > first ? (s_end - first + kAttWaves - 1) / kAttWaves : 0;
+  auto batch = [&](int j) {
+    return fetch_parts<FMT>(p, walk, j < n_own ? 2 * (first + (j + (lane >> 1)) * kAttWaves) + (lane & 1) : -1, h);
+  };
+  Step<D, FMT> cur, nxt;
+  bool odd = false;
+  Parts parts = batch(0), ahead = parts;
+
   // Q rows as B operands, in the column order of the K loads; rows past the end are zero
   bf16x8 qf[NR][T::kSteps];
   int row_hi[NR], row_lo[NR];
@@ -226,30 +253,8 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_rows_kernel(AttendParam
     }
   }
 
-  f32x4 o[NR][T::VC];
-  float m[NR], l[NR], lx[NR];
-#pragma unroll
-  for (int t = 0; t < NR; ++t) {
-    m[t] = kLow;
-    l[t] = lx[t] = 0.f;
-#pragma unroll
-    for (int b = 0; b < T::VC; ++b) o[t][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-
-  const uint32_t k_lane = (uint32_t)(c16 * p.k_s[1]) + g * 16;
-  const uint32_t v_lane = (uint32_t)(4 * g * p.v_s[1]) + c16 * T::VC * T::kEl;
-
-  if (threadIdx.x == 0) s_odd = 0;
-  __syncthreads();
-  // The wave's steps s_begin + wave + 4 j, looked up 32 at a time: lane i has part
-  // i % 2 of step i / 2 of the batch.  The look-up of a batch is issued a batch ahead.
-  const int first = s_begin + wave, n_own = s_end > first ? (s_end - first + kAttWaves - 1) / kAttWaves : 0;
-  auto batch = [&](int j) {
-    return fetch_parts<FMT>(p, walk, j < n_own ? 2 * (first + (j + (lane >> 1)) * kAttWaves) + (lane & 1) : -1, h);
-  };
-  Step<D, FMT> cur, nxt;
-  Parts parts = batch(0), ahead = batch(32);
   if (n_own > 0) load_step<D, FMT>(p, parts, 0, k_lane, v_lane, cur);
+  if (n_own > 32) ahead = batch(32);
   for (int j = 0; j < n_own; ++j) {
     if (j + 1 < n_own) {
       if (((j + 1) & 31) == 0) {
@@ -261,7 +266,7 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_rows_kernel(AttendParam
 
     // a step that some row does not see whole
     const bool partial = cur.ok != 3u || max(cur.pos[0], cur.pos[1]) + 15 > all_hi || min(cur.pos[0], cur.pos[1]) < all_lo;
-    if (partial && clear_unseen<D, FMT>(cur, g, lo, hi)) s_odd = 1;
+    if (partial) odd |= clear_unseen<D, FMT>(cur, g, lo, hi);
 
     f32x4 sc[NR][2];
 #pragma unroll
@@ -329,6 +334,8 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_rows_kernel(AttendParam
   }
 
   // join the four waves
+  odd = __ballot(odd) != 0;
+  if (lane == 0) s_odd[wave] = odd;
 #pragma unroll
   for (int t = 0; t < NR; ++t) {
     l[t] = sum_x32(sum_x16(l[t]));
@@ -388,20 +395,21 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_rows_kernel(AttendParam
     }
     __syncthreads();
   }
-  if (s_odd)
+  if (s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3])
     add_nonfinite<D, FMT>(p, rq, walk, 2 * s_begin, 2 * s_end, 2, all_lo, all_hi, h, r, row_first, row_end, split);
 }
 
 // Joins the parts of each row: with M the largest of the parts' maxima m_s,
-// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.  One workgroup a row, its
-// four waves take parts in turn.
+// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.  One workgroup a row: a
+// thread takes four columns of every eighth (or 16th) part, all loads in flight.
 template <int D>
 __global__ __launch_bounds__(kAttThreads) void attend_join_kernel(AttendParams) {
   const AttendParams& p = kernel_params<AttendParams>();
-  constexpr int C = D / 64;                        // columns a lane
-  __shared__ float s_o[kAttWaves][D];
-  __shared__ float s_l[2][kAttWaves];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int kCols = D / 4, kWays = kAttThreads / kCols;
+  __shared__ float s_f[512];                       // the parts' weights
+  __shared__ float s_red[3][kAttWaves];
+  __shared__ __attribute__((aligned(16))) f32x4 s_o[kWays][kCols];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   uint32_t w = blockIdx.x, d;
   d = fast_div(w, p.fd_rows);
   const int row = (int)(w - d * p.rows_max);
@@ -412,43 +420,67 @@ __global__ __launch_bounds__(kAttThreads) void attend_join_kernel(AttendParams) 
   const int i = (int)fast_div((uint32_t)row, p.fd_group);
   if (i >= rq.n) return;
   const int64_t at = (((int64_t)r * p.n_kv_heads + h) * p.rows_max + row) * p.n_splits;
+  const int col = tid % kCols, way = tid / kCols;
+  // the first loads of the sums leave together with those of the weights
+  constexpr int kFirst = 8;
+  f32x4 first[kFirst];
+#pragma unroll
+  for (int k = 0; k < kFirst; ++k) {
+    const int s = way + k * kWays;
+    first[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (s < p.n_splits) first[k] = *reinterpret_cast<const f32x4*>(p.part_o + (at + s) * D + col * 4);
+  }
+  f32x4 ml[2];
   float top = kLow;
-  for (int s = lane; s < p.n_splits; s += 64) top = fmaxf(top, p.part_ml[(at + s) * 4]);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int s = tid + k * kAttThreads;
+    ml[k] = f32x4{kLow, 0.f, 0.f, 0.f};
+    if (s < p.n_splits) ml[k] = *reinterpret_cast<const f32x4*>(p.part_ml + (at + s) * 4);
+    top = fmaxf(top, ml[k].x);
+  }
 #pragma unroll
   for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
-  float acc[C], l = 0.f, lx = 0.f;
+  if (lane == 0) s_red[0][wave] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
+  float l = 0.f, lx = 0.f;
 #pragma unroll
-  for (int c = 0; c < C; ++c) acc[c] = 0.f;
-  for (int s = wave; s < p.n_splits; s += kAttWaves) {
-    const f32x4 ml = *reinterpret_cast<const f32x4*>(p.part_ml + (at + s) * 4);
-    const float f = exp2_fast(ml.x - top);
-    l += ml.y * f;
-    lx += ml.z * f;
-#pragma unroll
-    for (int c = 0; c < C; ++c) acc[c] += p.part_o[(at + s) * D + lane * C + c] * f;
+  for (int k = 0; k < 2; ++k) {
+    const float f = exp2_fast(ml[k].x - top);
+    s_f[tid + k * kAttThreads] = f;
+    l += ml[k].y * f;
+    lx += ml[k].z * f;
   }
 #pragma unroll
-  for (int c = 0; c < C; ++c) s_o[wave][lane * C + c] = acc[c];
+  for (int x = 1; x < 64; x <<= 1) {
+    l += __shfl_xor(l, x);
+    lx += __shfl_xor(lx, x);
+  }
   if (lane == 0) {
-    s_l[0][wave] = l;
-    s_l[1][wave] = lx;
+    s_red[1][wave] = l;
+    s_red[2][wave] = lx;
   }
   __syncthreads();
-  const int t = threadIdx.x;
-  const float ll = (s_l[0][0] + s_l[0][1]) + (s_l[0][2] + s_l[0][3]);
-  const int64_t hq = (int64_t)h * p.group + (row - i * p.group);
-  if (t < D / 2) {
-    const float inv = ll == 0.f ? 0.f : 1.0f / ll;
-    float v[2];
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-      v[e] = ((s_o[0][2 * t + e] + s_o[1][2 * t + e]) + (s_o[2][2 * t + e] + s_o[3][2 * t + e])) * inv;
-    *reinterpret_cast<uint32_t*>(p.out + (rq.row0 + i) * p.out_s[0] + hq * p.out_s[1] + 2 * t) =
-        pack_bf16x2(v[0], v[1]);
+  for (int k = 0; k < kFirst; ++k)
+    if (way + k * kWays < p.n_splits) acc += first[k] * s_f[way + k * kWays];
+  for (int s = way + kFirst * kWays; s < p.n_splits; s += kWays)
+    acc += *reinterpret_cast<const f32x4*>(p.part_o + (at + s) * D + col * 4) * s_f[s];
+  s_o[way][col] = acc;
+  __syncthreads();
+  l = (s_red[1][0] + s_red[1][1]) + (s_red[1][2] + s_red[1][3]);
+  lx = (s_red[2][0] + s_red[2][1]) + (s_red[2][2] + s_red[2][3]);
+  const int64_t hq = (int64_t)h * p.group + (row - i * p.group);
+  if (tid < kCols) {
+#pragma unroll
+    for (int k = 1; k < kWays; ++k) acc += s_o[k][tid];
+    acc *= l == 0.f ? 0.f : 1.0f / l;
+    *reinterpret_cast<u32x2*>(p.out + (rq.row0 + i) * p.out_s[0] + hq * p.out_s[1] + 4 * tid) =
+        u32x2{pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w)};
   }
-  if (t == 0 && p.lse != nullptr)
-    p.lse[(rq.row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] =
-        row_lse(top, (s_l[1][0] + s_l[1][1]) + (s_l[1][2] + s_l[1][3]));
+  if (tid == 0 && p.lse != nullptr) p.lse[(rq.row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] = row_lse(top, lx);
 }
 
 namespace {

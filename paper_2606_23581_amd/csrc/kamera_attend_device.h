@@ -2,8 +2,7 @@
 // the bookkeeping of which keys a row sees.
 #pragma once
 
-#include "kamera_cache.h"
-#include "kamera_device.h"
+#include "kamera_cache_device.h"
 
 namespace kamera {
 
@@ -18,13 +17,6 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 template <bool HI>
 __device__ __forceinline__ uint32_t e4m3_to_bf16x2(uint32_t w, float scale) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI));
-}
-
-// Memory that no kernel writes while this one runs, at a wave-uniform address:
-// a scalar load.
-template <typename T>
-__device__ __forceinline__ T uniform_load(const T* p) {
-  return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
 }
 
 // The larger of two, NaN if one is: v_maximum3_f32 for two of these, with none of
@@ -86,11 +78,14 @@ struct Request {
 };
 
 __device__ __forceinline__ Request request_of(const AttendParams& p, int r) {
+  // all three at once, without a branch between them
+  const int n = load_or(p.q_tokens, r, p.n_queries, p.kv_tokens);
+  const int kv = load_or(p.kv_tokens, r, 0, p.kv_tokens);
+  const int base = load_or(p.q_base, r, 0, p.kv_tokens);
   Request q;
-  q.n = p.n_queries;
-  if (p.q_tokens != nullptr) q.n = min(max(uniform_load(p.q_tokens + r), 0), p.n_queries);
-  q.kv = min(max(uniform_load(p.kv_tokens + r), 0), p.n_keys);
-  q.row0 = p.q_base != nullptr ? (int64_t)uniform_load(p.q_base + r) : (int64_t)r * p.n_queries;
+  q.n = min(max(n, 0), p.n_queries);
+  q.kv = min(max(kv, 0), p.n_keys);
+  q.row0 = p.q_base != nullptr ? (int64_t)base : (int64_t)r * p.n_queries;
   return q;
 }
 

@@ -67,6 +67,7 @@ __global__ __launch_bounds__(kTabThreads) void tables_kernel(TablesParams) {
   const int per = (n + kTabThreads - 1) / kTabThreads;
   const int r0 = min(n, tid * per), r1 = min(n, r0 + per);
   const int cap = p.pt_stride * p.page_size;       // < 2^31
+  const int begin = p.free_begin != nullptr ? p.free_begin[0] : 0;
   int pages = 0, tokens = 0;
   uint32_t flags = 0;
   for (int r = r0; r < r1; ++r) {
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(kTabThreads) void tables_kernel(TablesParams) {
   }
   __syncthreads();
 
-  const int first = p.free_begin != nullptr ? min(max(p.free_begin[0], 0), p.n_free) : 0;
+  const int first = min(max(begin, 0), p.n_free);
   const int left = p.n_free - first;
   // page number k of the new ones, or -1
   auto new_page = [&](int k) -> int {

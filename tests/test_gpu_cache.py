@@ -253,6 +253,8 @@ SELECT_CASES = {
     "nonfinite_query": dict(kv=[900], keep=5, nonfinite=True),
     "bad_page": dict(kv=[900], keep=50, bad=True),
     "long": dict(kv=[40000], keep=100, H=1),
+    "most_pages": dict(kv=[140001, 16 * 8192 + 1], keep=77, H=1, G=2, D=64),
+    "most_pages_ties": dict(kv=[140001], keep=500, H=1, G=2, D=64, ties=True),
 }
 
 
