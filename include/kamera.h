@@ -565,6 +565,8 @@ typedef struct {
   int32_t n_last;                /* >= 1                                       */
   int32_t* sel;                  /* device [n_requests][n_kv_heads][n_keep]    */
   int32_t* sel_count;            /* device [n_requests][n_kv_heads]            */
+  void* workspace;               /* as in kamera_attend_args                   */
+  int64_t workspace_bytes;       /* at least kamera_select_workspace(args)     */
   uint32_t* status;
 } kamera_select_args;
 
@@ -647,10 +649,12 @@ int kamera_append_paged8(const kamera_append_args* args, void* stream);
 int kamera_select_pages(const kamera_select_args* args, void* stream);
 int kamera_attend_paged(const kamera_attend_args* args, void* stream);
 
-/* Bytes of workspace that kamera_attend_paged needs for `args` (its pointers
- * are not looked at, workspace and workspace_bytes included), 0 where the work
- * is not split; or the negative error code of a refused size. */
+/* Bytes of workspace that kamera_attend_paged and kamera_select_pages need for
+ * `args` (its pointers are not looked at, workspace and workspace_bytes
+ * included), 0 where the work is not split; or the negative error code of a
+ * refused size. */
 int64_t kamera_attend_workspace(const kamera_attend_args* args);
+int64_t kamera_select_workspace(const kamera_select_args* args);
 
 /* As kamera_validate, for the entry points above: 0 kamera_page_tables,
  * 1 kamera_append_paged8, 2 kamera_select_pages, 3 kamera_attend_paged. */

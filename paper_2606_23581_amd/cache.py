@@ -51,7 +51,8 @@ class CSelectArgs(ctypes.Structure):
                 ("page_size", _i32), ("pt_stride", _i32), ("n_pool_pages", _i32), ("kv_tokens", _vp),
                 ("page_table", _vp), ("q", _vp), ("q_stride", _i64 * 2), ("k_sum", _vp), ("k_sum_stride", _i64 * 2),
                 ("k_sum_scale", _vp), ("k_sum_scale_stride", _i64 * 2), ("n_keep", _i32), ("n_first", _i32),
-                ("n_last", _i32), ("sel", _vp), ("sel_count", _vp), ("status", _vp)]
+                ("n_last", _i32), ("sel", _vp), ("sel_count", _vp), ("workspace", _vp), ("workspace_bytes", _i64),
+                ("status", _vp)]
 
 
 class CAttendArgs(ctypes.Structure):
@@ -68,7 +69,7 @@ class CAttendArgs(ctypes.Structure):
 
 STRUCTS = {6: CPageTablesArgs, 7: CAppendArgs, 8: CSelectArgs, 9: CAttendArgs}
 EXPORTS = ("kamera_page_tables", "kamera_append_paged8", "kamera_select_pages", "kamera_attend_paged",
-           "kamera_attend_workspace", "kamera_validate_cache")
+           "kamera_attend_workspace", "kamera_select_workspace", "kamera_validate_cache")
 
 
 def declare(L) -> None:
@@ -80,6 +81,8 @@ def declare(L) -> None:
         fn.restype = _i32
     L.kamera_attend_workspace.argtypes = [ctypes.POINTER(CAttendArgs)]
     L.kamera_attend_workspace.restype = _i64
+    L.kamera_select_workspace.argtypes = [ctypes.POINTER(CSelectArgs)]
+    L.kamera_select_workspace.restype = _i64
     L.kamera_validate_cache.argtypes = [_i32, _vp]
     L.kamera_validate_cache.restype = _i32
 
@@ -124,6 +127,29 @@ def _device(*tensors):
 def _set(field, values):
     for i, x in enumerate(values):
         field[i] = int(x)
+
+
+def _workspace(a, need, workspace, device):
+    """The given workspace, or one of `need` bytes (or none), entered into the arguments."""
+    import torch
+
+    _check(min(need, 0))
+    if need > 0 and workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = _ptr(workspace), workspace.numel() * workspace.element_size()
+    return workspace
+
+
+def _launch_with_workspace(call, stream, given) -> None:
+    """Launches a call that may have a workspace of its own, which ends with it here."""
+    call.launch(stream)
+    if call.workspace is not None and given is None and stream is not None:
+        # the allocator learns that another stream than the current one uses the workspace
+        import torch
+
+        s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+        call.workspace.record_stream(s)
 
 
 def _is8(t):
@@ -291,17 +317,18 @@ def prepare_append_paged8(k, v, k_cache, v_cache, k_scale, v_scale, page_table, 
 
 def select_pages(*a, stream=None, **kw) -> None:
     """``kamera_select_pages``; see ``prepare_select_pages`` for the arguments."""
-    prepare_select_pages(*a, **kw).launch(stream)
+    _launch_with_workspace(prepare_select_pages(*a, **kw), stream, kw.get("workspace"))
 
 
 def prepare_select_pages(q, k_sum, k_sum_scale, page_table, kv_tokens, sel, sel_count, *, n_keys: int,
-                         page_size: int, n_first: int = 1, n_last: int = 1, status=None) -> Prepared:
+                         page_size: int, n_first: int = 1, n_last: int = 1, workspace=None,
+                         status=None) -> Prepared:
     """The sel.shape[-1] pages of each request that its query needs most, for every KV head.
 
     q: bf16 [R, heads, D], one query token a request; k_sum: int8 [pages, H, D] and k_sum_scale: fp32
     [pages, H], one layer's key sums; page_table: int32 [R, pages]; kv_tokens: int32 [R], at most n_keys.
     sel: int32 [R, H, keep], receives ascending page indices (-1 after them), sel_count: int32 [R, H].
-    The first n_first and the last n_last pages are always taken.
+    The first n_first and the last n_last pages are always taken.  workspace: as in ``prepare_attend_paged``.
     """
     import torch
 
@@ -318,7 +345,7 @@ def prepare_select_pages(q, k_sum, k_sum_scale, page_table, kv_tokens, sel, sel_
     _typed(sel, torch.int32, "sel", (R, H, keep))
     _typed(sel_count, torch.int32, "sel_count", (R, H))
     _typed(status, torch.int32, "status")
-    _device(q, k_sum, k_sum_scale, page_table, kv_tokens, sel, sel_count, status)
+    _device(q, k_sum, k_sum_scale, page_table, kv_tokens, sel, sel_count, workspace, status)
     a = CSelectArgs()
     a.n_requests, a.n_q_heads, a.n_kv_heads, a.head_dim, a.n_keys = R, HQ, H, D, int(n_keys)
     a.page_size, a.pt_stride, a.n_pool_pages = int(page_size), _table(page_table, R), n_pages
@@ -329,19 +356,16 @@ def prepare_select_pages(q, k_sum, k_sum_scale, page_table, kv_tokens, sel, sel_
     _set(a.k_sum_scale_stride, k_sum_scale.stride())
     a.n_keep, a.n_first, a.n_last = keep, int(n_first), int(n_last)
     a.sel, a.sel_count, a.status = _ptr(sel), _ptr(sel_count), _ptr(status)
-    return Prepared(L.kamera_select_pages, a, (q, k_sum, k_sum_scale, page_table, kv_tokens, sel, sel_count, status))
+    workspace = _workspace(a, L.kamera_select_workspace(ctypes.byref(a)), workspace, q.device)
+    call = Prepared(L.kamera_select_pages, a, (q, k_sum, k_sum_scale, page_table, kv_tokens, sel, sel_count,
+                                               workspace, status))
+    call.workspace = workspace
+    return call
 
 
 def attend_paged(*a, stream=None, **kw) -> None:
     """``kamera_attend_paged``; see ``prepare_attend_paged`` for the arguments."""
-    call = prepare_attend_paged(*a, **kw)
-    call.launch(stream)
-    if call.workspace is not None and kw.get("workspace") is None and stream is not None:
-        # the allocator learns that another stream than the current one uses the workspace
-        import torch
-
-        s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
-        call.workspace.record_stream(s)
+    _launch_with_workspace(prepare_attend_paged(*a, **kw), stream, kw.get("workspace"))
 
 
 def attend_workspace(prepared: Prepared) -> int:
@@ -419,12 +443,7 @@ def prepare_attend_paged(q, k_cache, v_cache, out, page_table, kv_tokens, *, n_q
     elif sel_count is not None:
         raise ValueError("sel_count without sel")
     a.status = _ptr(status)
-    need = L.kamera_attend_workspace(ctypes.byref(a))
-    _check(min(need, 0))
-    if need > 0:
-        if workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        a.workspace, a.workspace_bytes = _ptr(workspace), workspace.numel() * workspace.element_size()
+    workspace = _workspace(a, L.kamera_attend_workspace(ctypes.byref(a)), workspace, q.device)
     _device(q, k_cache, v_cache, out, page_table, kv_tokens, q_base, q_tokens, k_scale, v_scale, sel, sel_count, lse,
             workspace, status)
     call = Prepared(L.kamera_attend_paged, a, (q, k_cache, v_cache, out, page_table, kv_tokens, q_base, q_tokens,

@@ -418,7 +418,6 @@ __global__ __launch_bounds__(kAttThreads) void attend_join_kernel(AttendParams) 
   const int h = (int)(w - d * p.n_kv_heads), r = (int)d;
   const Request rq = request_of(p, r);
   const int i = (int)fast_div((uint32_t)row, p.fd_group);
-  if (i >= rq.n) return;
   const int64_t at = (((int64_t)r * p.n_kv_heads + h) * p.rows_max + row) * p.n_splits;
   const int col = tid % kCols, way = tid / kCols;
   // the first loads of the sums leave together with those of the weights
@@ -439,6 +438,7 @@ __global__ __launch_bounds__(kAttThreads) void attend_join_kernel(AttendParams) 
     if (s < p.n_splits) ml[k] = *reinterpret_cast<const f32x4*>(p.part_ml + (at + s) * 4);
     top = fmaxf(top, ml[k].x);
   }
+  if (i >= rq.n) return;                           // a row that no request has (its parts were not written)
 #pragma unroll
   for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
   if (lane == 0) s_red[0][wave] = top;
@@ -466,6 +466,7 @@ __global__ __launch_bounds__(kAttThreads) void attend_join_kernel(AttendParams) 
 #pragma unroll
   for (int k = 0; k < kFirst; ++k)
     if (way + k * kWays < p.n_splits) acc += first[k] * s_f[way + k * kWays];
+#pragma unroll 2
   for (int s = way + kFirst * kWays; s < p.n_splits; s += kWays)
     acc += *reinterpret_cast<const f32x4*>(p.part_o + (at + s) * D + col * 4) * s_f[s];
   s_o[way][col] = acc;

@@ -32,6 +32,10 @@ bool multiples(const int64_t* s, int n, int64_t of) {
   return true;
 }
 
+// Page selection: from so many pages a request on they are scored by workgroups of
+// their own (see kamera_select.hip).
+constexpr int64_t kSelectSplit = 2048;
+
 int check_head_dim(int32_t head_dim, const char* who) {
   if (head_dim != 64 && head_dim != 128)
     return fail(KAMERA_ERR_UNSUPPORTED, "%s: head_dim must be 64 or 128 (got %d)", who, head_dim);
@@ -54,6 +58,14 @@ int check_table(const int32_t* table, int32_t pt_stride, int32_t page_size, int3
   if (pt_stride < ceil_div(tokens, page_size))
     return fail(KAMERA_ERR_SHAPE, "%s: pt_stride %d < %lld pages needed for %lld tokens", who, pt_stride,
                 (long long)ceil_div(tokens, page_size), (long long)tokens);
+  return KAMERA_OK;
+}
+
+int check_workspace(const void* workspace, int64_t bytes, int64_t needed, const char* who) {
+  if (workspace == nullptr) return fail(KAMERA_ERR_NULL, "%s: workspace is NULL", who);
+  if (bytes < needed)
+    return fail(KAMERA_ERR_SHAPE, "%s: workspace of %lld bytes, %lld needed", who, (long long)bytes, (long long)needed);
+  if (!aligned16(workspace)) return fail(KAMERA_ERR_ALIGN, "%s: workspace must be 16-byte aligned", who);
   return KAMERA_OK;
 }
 
@@ -212,9 +224,12 @@ int build_append(const kamera_append_args* a, kamera::AppendParams& P, bool& lau
 
 // ---------------------------------------------------------------------------
 
-int build_select(const kamera_select_args* a, kamera::SelectParams& P, bool& launch) {
+// Sizes of a selection, and whether pages are scored apart.
+int size_select(const kamera_select_args* a, bool& work, int32_t& n_pieces, int64_t& workspace) {
   const char* who = "kamera_select_pages";
-  launch = false;
+  work = false;
+  n_pieces = 0;
+  workspace = 0;
   if (a == nullptr) return fail(KAMERA_ERR_NULL, "%s: args is NULL", who);
   if (a->n_requests < 0 || a->n_keys < 0) return fail(KAMERA_ERR_SHAPE, "%s: negative n_requests/n_keys", who);
   int rc = check_head_dim(a->head_dim, who);
@@ -229,28 +244,54 @@ int build_select(const kamera_select_args* a, kamera::SelectParams& P, bool& lau
     return fail(KAMERA_ERR_RANGE, "%s: %lld pages a request exceed %d", who, (long long)max_pages,
                 KAMERA_MAX_SELECT_PAGES);
   if (a->n_requests == 0) return KAMERA_OK;
+  const int64_t wgs = bounded_product({a->n_requests, a->n_kv_heads});
+  if (wgs < 0 || wgs * 1024 > 0xFFFFFFFFLL)
+    return fail(KAMERA_ERR_RANGE, "%s: too many requests and heads for one launch", who);
+  work = true;
+  const int64_t pieces = ceil_div(max_pages, 256);
+  if (max_pages > kSelectSplit && wgs <= 128 && max_pages > a->n_keep && wgs * pieces * 256 <= 0xFFFFFFFFLL) {
+    n_pieces = (int32_t)pieces;
+    workspace = wgs * max_pages * 4;
+  }
+  return KAMERA_OK;
+}
+
+int build_select(const kamera_select_args* a, kamera::SelectParams& P, bool& launch) {
+  const char* who = "kamera_select_pages";
+  bool work = false;
+  int32_t n_pieces = 0;
+  int64_t workspace = 0;
+  launch = false;
+  int rc = size_select(a, work, n_pieces, workspace);
+  if (rc || !work) return rc;
   if ((rc = check_table(a->page_table, a->pt_stride, a->page_size, a->n_pool_pages, a->n_keys, who))) return rc;
   if (a->kv_tokens == nullptr || a->q == nullptr || a->k_sum == nullptr || a->k_sum_scale == nullptr ||
       a->sel == nullptr || a->sel_count == nullptr)
     return fail(KAMERA_ERR_NULL, "%s: kv_tokens, q, k_sum, k_sum_scale, sel and sel_count are needed", who);
   if (!aligned16(a->k_sum) || !multiples(a->k_sum_stride, 2, 16))
     return fail(KAMERA_ERR_ALIGN, "%s: key sums must start at 16-byte boundaries", who);
-  const int64_t wgs = bounded_product({a->n_requests, a->n_kv_heads});
+  const int64_t wgs = (int64_t)a->n_requests * a->n_kv_heads;
   const int64_t entries = bounded_product({a->n_requests, a->n_kv_heads, a->n_keep});
-  if (wgs < 0 || entries < 0 || wgs * 1024 > 0xFFFFFFFFLL)
-    return fail(KAMERA_ERR_RANGE, "%s: too many requests and heads for one launch", who);
+  if (entries < 0) return fail(KAMERA_ERR_RANGE, "%s: n_keep too large", who);
   const int64_t ext_q[2] = {a->n_requests, a->n_q_heads}, ext_s[2] = {a->n_pool_pages, a->n_kv_heads};
-  Range in[3];
+  Range in[5] = {};
   if (!span(a->q, a->q_stride, ext_q, 2, a->head_dim, 2, in[0].lo, in[0].hi) ||
       !span(a->k_sum, a->k_sum_stride, ext_s, 2, a->head_dim, 1, in[1].lo, in[1].hi) ||
       !span(a->k_sum_scale, a->k_sum_scale_stride, ext_s, 2, 1, 4, in[2].lo, in[2].hi))
     return fail(KAMERA_ERR_RANGE, "%s: strides span more than the address space", who);
-  const Range out[2] = {flat(a->sel, entries, 4), flat(a->sel_count, wgs, 4)};
-  for (int k = 0; k < 3; ++k)
-    if (meet(out[0], in[k]) || meet(out[1], in[k])) return fail(KAMERA_ERR_ALIAS, "%s: an output overlaps an input", who);
-  const Range tab = flat(a->page_table, (int64_t)a->n_requests * a->pt_stride, 4), kvr = flat(a->kv_tokens, a->n_requests, 4);
-  if (meet(out[0], tab) || meet(out[1], tab) || meet(out[0], kvr) || meet(out[1], kvr) || meet(out[0], out[1]))
-    return fail(KAMERA_ERR_ALIAS, "%s: an output overlaps an input or the other output", who);
+  in[3] = flat(a->page_table, (int64_t)a->n_requests * a->pt_stride, 4);
+  in[4] = flat(a->kv_tokens, a->n_requests, 4);
+  Range out[3] = {flat(a->sel, entries, 4), flat(a->sel_count, wgs, 4), {0, 0}};
+  if (workspace > 0) {
+    if ((rc = check_workspace(a->workspace, a->workspace_bytes, workspace, who))) return rc;
+    out[2] = flat(a->workspace, workspace, 1);
+  }
+  for (int i = 0; i < 3; ++i) {
+    for (int k = 0; k < 5; ++k)
+      if (meet(out[i], in[k])) return fail(KAMERA_ERR_ALIAS, "%s: an output or the workspace overlaps an input", who);
+    for (int k = i + 1; k < 3; ++k)
+      if (meet(out[i], out[k])) return fail(KAMERA_ERR_ALIAS, "%s: sel, sel_count and workspace overlap", who);
+  }
   memset(&P, 0, sizeof(P));
   P.kv_tokens = a->kv_tokens;
   P.page_table = a->page_table;
@@ -274,7 +315,9 @@ int build_select(const kamera_select_args* a, kamera::SelectParams& P, bool& lau
   P.n_keep = a->n_keep;
   P.n_first = a->n_first;
   P.n_last = a->n_last;
-  P.max_pages = (int32_t)std::max<int64_t>(max_pages, 1);
+  P.max_pages = (int32_t)std::max<int64_t>(ceil_div(a->n_keys, a->page_size), 1);
+  P.n_pieces = n_pieces;
+  P.keys = static_cast<uint32_t*>(a->workspace);
   launch = true;
   return KAMERA_OK;
 }
@@ -392,11 +435,7 @@ int build_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& lau
     return fail(KAMERA_ERR_RANGE, "%s: strides span more than the address space", who);
   in[5] = flat(a->page_table, (int64_t)a->n_requests * a->pt_stride, 4);
   if (workspace > 0) {
-    if (a->workspace == nullptr) return fail(KAMERA_ERR_NULL, "%s: workspace is NULL", who);
-    if (a->workspace_bytes < workspace)
-      return fail(KAMERA_ERR_SHAPE, "%s: workspace of %lld bytes, %lld needed", who, (long long)a->workspace_bytes,
-                  (long long)workspace);
-    if (!aligned16(a->workspace)) return fail(KAMERA_ERR_ALIGN, "%s: workspace must be 16-byte aligned", who);
+    if ((rc = check_workspace(a->workspace, a->workspace_bytes, workspace, who))) return rc;
     out[2] = flat(a->workspace, workspace, 1);
   }
   for (int i = 0; i < 3; ++i) {
@@ -502,6 +541,16 @@ extern "C" int kamera_attend_paged(const kamera_attend_args* a, void* stream) {
   const int rc = build_attend(a, P, launch);
   if (rc) return rc;
   return finish(launch ? kamera::launch_attend(P, static_cast<hipStream_t>(stream)) : hipSuccess, "kamera_attend_paged");
+}
+
+extern "C" int64_t kamera_select_workspace(const kamera_select_args* a) {
+  bool work = false;
+  int32_t n_pieces = 0;
+  int64_t workspace = 0;
+  const int rc = size_select(a, work, n_pieces, workspace);
+  if (rc) return rc;
+  ok();
+  return workspace;
 }
 
 extern "C" int64_t kamera_attend_workspace(const kamera_attend_args* a) {

@@ -69,6 +69,8 @@ struct SelectParams {
   int32_t n_keys, page_size, pt_stride, n_pool_pages;
   int32_t n_keep, n_first, n_last;
   int32_t max_pages;                 // ceil(n_keys / page_size)
+  int32_t n_pieces;                  // > 0: scored by workgroups of their own, so many a (request, KV head)
+  uint32_t* keys;                    // [request][KV head][max_pages] of these
 };
 
 struct AttendParams {

@@ -1,7 +1,10 @@
 // kamera_select_pages: the pages a query needs most, by an integer score.
 //
-// One workgroup of 16 waves per (request, KV head).  The group's query rows
-// become int8 with one power-of-two scale; a page's score is the largest of
+// A workgroup of 16 waves per (request, KV head) selects; it also scores the pages
+// itself where these are few or the workgroups many, and otherwise 256-page pieces
+// are scored by workgroups of their own before (the keys in between in a
+// workspace): a CU takes in about 25 bytes of key sums a cycle, 2 ns a page, and a
+// second launch costs some 4 us.  The group's query rows become int8 with one power-of-two scale; a page's score is the largest of
 // the group's int8 products with the page's key sum, times the page's scale.
 // |product| <= 127 * 127 * 128 < 2^24, so the fp32 score is exact and the
 // selection one answer.
@@ -21,8 +24,7 @@
 // Bound by the latency of the page-table and sum loads (128 bytes a page) and of
 // the passes.
 
-#include "kamera_cache.h"
-#include "kamera_device.h"
+#include "kamera_cache_device.h"
 
 namespace kamera {
 
@@ -42,73 +44,66 @@ __device__ __forceinline__ uint32_t ordered(float x) {
 
 __device__ __forceinline__ int lane_of(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
+// Pages of request r.
+__device__ __forceinline__ int pages_of(const SelectParams& p, int r) {
+  return (min(max(uniform_load(p.kv_tokens + r), 0), p.n_keys) + p.page_size - 1) / p.page_size;
+}
+
 __device__ __forceinline__ int wave_max(int x) {
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) x = max(x, __shfl_xor(x, d));
   return x;
 }
 
-}  // namespace
-
-// D columns; RT tiles of 16 query rows (group <= 16 * RT); at most KPT * 1024 pages.
-template <int D, int RT, int KPT>
-__global__ __launch_bounds__(kSelThreads) void select_kernel(SelectParams) {
-  const SelectParams& p = kernel_params<SelectParams>();
-  extern __shared__ uint32_t s_key[];              // [max_pages]
-  __shared__ __attribute__((aligned(16))) int8_t s_q[RT * 16 * D];
-  __shared__ i32x4 s_turn[kSelWaves][64];
-  __shared__ int s_wave[kSelWaves];
-  __shared__ int s_cnt[3][3];
-  __shared__ int s_run[2][KPT * kSelWaves];
+// Keys of pages [first, end) of a request with n pages in all, by the workgroup's
+// WAVES waves; put(j, key) takes them.  D columns; RT tiles of 16 query rows
+// (group <= 16 * RT).  s_q: RT * 16 * D bytes, s_turn: 64 chunks a wave.
+template <int D, int RT, int WAVES, typename Put>
+__device__ __forceinline__ void score_pages(const SelectParams& p, int r, int h, int first, int end_most, int& n,
+                                            int8_t* s_q, i32x4* s_turn, int* s_wave, const Put& put) {
+  constexpr int kThreads = WAVES * 64;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c16 = lane & 15, g = lane >> 4;
-  const int r = blockIdx.x / p.n_kv_heads, h = blockIdx.x % p.n_kv_heads;
   const int32_t* table = p.page_table + (int64_t)r * p.pt_stride;
 
   // table entries, a turn ahead of their use; those past the request's pages are
   // not used, so its length is not waited for.  Lane i looks up page i / 4 of a tile.
-  constexpr int U = RT == 1 ? 8 : 4, kTurn = kSelWaves * 16 * U;
+  constexpr int U = RT == 1 && WAVES == 16 ? 8 : 4, kTurn = WAVES * 16 * U;
   int ahead[U];
   auto look_up = [&](int t0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int j = t0 + u * 16 + (lane >> 2);
-      ahead[u] = j < p.max_pages ? table[j] : 0;
+      ahead[u] = j < end_most ? table[j] : 0;
     }
   };
-  look_up(wave * 16 * U);
+  look_up(first + wave * 16 * U);
 
   // the group's queries in 8 bits
   const uint16_t* q = p.q + r * p.q_s[0] + (int64_t)h * p.group * p.q_s[1];
-  constexpr int QN = RT * 16 * D / kSelThreads;
+  constexpr int QN = RT * 16 * D / kThreads;
   uint32_t qv[QN];
   int amax = 0;
 #pragma unroll
   for (int k = 0; k < QN; ++k) {
-    const int i = tid + k * kSelThreads;
+    const int i = tid + k * kThreads;
     qv[k] = i < p.group * D ? q[(i / D) * p.q_s[1] + i % D] : 0;
     if ((qv[k] & 0x7fff) >= 0x7f80) qv[k] = 0;     // what is not finite
     amax = max(amax, (int)(qv[k] & 0x7fff));
   }
-  const int kv = min(max(p.kv_tokens[r], 0), p.n_keys);
-  const int n = (kv + p.page_size - 1) / p.page_size;
-  int32_t* sel = p.sel + ((int64_t)r * p.n_kv_heads + h) * p.n_keep;
-  const int keep = p.n_keep;
-  if (n <= keep) {                                 // every page
-    for (int j = tid; j < keep; j += kSelThreads) sel[j] = j < n ? j : -1;
-    if (tid == 0) p.sel_count[(int64_t)r * p.n_kv_heads + h] = n;
-    return;
-  }
+  n = pages_of(p, r);
+  const int end = min(end_most, n);
+  if (n <= p.n_keep || first >= end) return;
   amax = wave_max(amax);
   if (lane == 0) s_wave[wave] = amax;
   __syncthreads();
-  amax = wave_max(s_wave[c16]);
+  amax = wave_max(s_wave[c16 & (WAVES - 1)]);
   // 127 = (1 + 0x7e / 2^7) * 2^6
   int f = (amax >> 7) - 127 - 6 + ((amax & 0x7f) > 0x7e ? 1 : 0);
   f = f < kMinExp ? kMinExp : f;
   const float down = __uint_as_float((uint32_t)(127 - f) << 23);
 #pragma unroll
-  for (int k = 0; k < QN; ++k) s_q[tid + k * kSelThreads] = (int8_t)(int)rintf(bf_lo(qv[k]) * down);
+  for (int k = 0; k < QN; ++k) s_q[tid + k * kThreads] = (int8_t)(int)rintf(bf_lo(qv[k]) * down);
   __syncthreads();
 
   i32x4 qa[RT][D / 64];
@@ -118,18 +113,18 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectParams) {
     for (int k = 0; k < D / 64; ++k)
       qa[t][k] = *reinterpret_cast<const i32x4*>(s_q + (t * 16 + c16) * D + k * 64 + g * 16);
 
-  // Scores, U tiles of 16 pages in flight a wave.
+  // U tiles of 16 pages in flight a wave
   const int8_t* sums = p.k_sum + h * p.k_sum_s[1] + (lane & 3) * 16;
   const float* scales = p.k_sum_scale + h * p.k_sum_scale_s[1];
-  i32x4* turn = s_turn[wave];
-  for (int t0 = wave * 16 * U; t0 < n; t0 += kTurn) {
+  i32x4* turn = s_turn + wave * 64;
+  for (int t0 = first + wave * 16 * U; t0 < end; t0 += kTurn) {
     i32x4 b[U][D / 64];
     float sc[U];
     uint32_t in = 0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const bool ok = ahead[u] >= 0 && ahead[u] < p.n_pool_pages;
-      in |= ok || t0 + u * 16 + (lane >> 2) >= n ? 1u << u : 0u;
+      in |= ok || t0 + u * 16 + (lane >> 2) >= end ? 1u << u : 0u;
       const int pg = ok ? ahead[u] : 0;
 #pragma unroll
       for (int k = 0; k < D / 64; ++k) b[u][k] = *reinterpret_cast<const i32x4*>(sums + pg * p.k_sum_s[0] + k * 64);
@@ -163,19 +158,78 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectParams) {
       // page c16's maximum is in lane c16, its scale in lane 4 c16
       best = __shfl(best, lane >> 2);
       const int j = t0 + u * 16 + (lane >> 2);
-      if ((lane & 3) == 0 && j < n) {
+      if ((lane & 3) == 0 && j < end) {
         uint32_t key = ((in >> u) & 1) ? ordered((float)best * sc[u]) : kNever;
         if (j < p.n_first || j >= n - p.n_last) key = kAlways;
-        s_key[j] = key;
+        put(j, key);
       }
     }
+  }
+}
+
+constexpr int kPiece = 256, kPieceWaves = 4;
+
+}  // namespace
+
+// The keys of one 256-page piece of a (request, KV head) into the workspace.
+template <int D, int RT>
+__global__ __launch_bounds__(kPieceWaves * 64) void score_kernel(SelectParams) {
+  const SelectParams& p = kernel_params<SelectParams>();
+  __shared__ __attribute__((aligned(16))) int8_t s_q[RT * 16 * D];
+  __shared__ i32x4 s_turn[kPieceWaves * 64];
+  __shared__ int s_wave[kPieceWaves];
+  // the heads of a piece run at the same time: their sums lie together
+  uint32_t w = blockIdx.x, d;
+  d = w / p.n_kv_heads;
+  const int h = (int)(w - d * p.n_kv_heads);
+  w = d;
+  d = w / p.n_pieces;
+  const int piece = (int)(w - d * p.n_pieces), r = (int)d;
+  uint32_t* keys = p.keys + ((int64_t)r * p.n_kv_heads + h) * p.max_pages;
+  int n;
+  score_pages<D, RT, kPieceWaves>(p, r, h, piece * kPiece, min(p.max_pages, (piece + 1) * kPiece), n, s_q, s_turn, s_wave,
+                                  [&](int j, uint32_t key) { keys[j] = key; });
+}
+
+// Selection; at most KPT * 1024 pages.  SCORE: the workgroup makes the keys itself
+// (D, RT as in score_pages).
+template <int D, int RT, int KPT, bool SCORE>
+__global__ __launch_bounds__(kSelThreads) void select_kernel(SelectParams) {
+  const SelectParams& p = kernel_params<SelectParams>();
+  extern __shared__ uint32_t s_key[];              // [max_pages] (SCORE)
+  __shared__ __attribute__((aligned(16))) int8_t s_q[SCORE ? RT * 16 * D : 16];
+  __shared__ i32x4 s_turn[SCORE ? kSelWaves * 64 : 1];
+  __shared__ int s_wave[kSelWaves];
+  __shared__ int s_cnt[3][3];
+  __shared__ int s_run[2][KPT * kSelWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = blockIdx.x / p.n_kv_heads, h = blockIdx.x % p.n_kv_heads;
+  int n;
+  uint32_t key[KPT];                               // of pages k * 1024 + tid; 0: none
+  if (SCORE) {
+    score_pages<D, RT, kSelWaves>(p, r, h, 0, p.max_pages, n, s_q, s_turn, s_wave,
+                                  [&](int j, uint32_t k) { s_key[j] = k; });
+  } else {
+    const uint32_t* keys = p.keys + (int64_t)blockIdx.x * p.max_pages;
+#pragma unroll
+    for (int k = 0; k < KPT; ++k) key[k] = k * kSelThreads + tid < p.max_pages ? keys[k * kSelThreads + tid] : 0u;
+    n = pages_of(p, r);
+  }
+  int32_t* sel = p.sel + (int64_t)blockIdx.x * p.n_keep;
+  const int keep = p.n_keep;
+  if (n <= keep) {                                 // every page
+    for (int j = tid; j < keep; j += kSelThreads) sel[j] = j < n ? j : -1;
+    if (tid == 0) p.sel_count[blockIdx.x] = n;
+    return;
   }
   if (tid < 9) s_cnt[tid / 3][tid % 3] = 0;
   __syncthreads();
 
-  uint32_t key[KPT];                               // of pages k * 1024 + tid; 0: none
 #pragma unroll
-  for (int k = 0; k < KPT; ++k) key[k] = k * kSelThreads + tid < n ? s_key[k * kSelThreads + tid] : 0u;
+  for (int k = 0; k < KPT; ++k) {
+    if (SCORE) key[k] = k * kSelThreads + tid < n ? s_key[k * kSelThreads + tid] : 0u;
+    if (k * kSelThreads + tid >= n) key[k] = 0u;   // past the request's pages
+  }
 
   // The largest T with at least `keep` keys >= T, two bits a pass, or the first T
   // met with exactly that many: no smaller key can be taken then either.
@@ -257,35 +311,41 @@ __global__ __launch_bounds__(kSelThreads) void select_kernel(SelectParams) {
     const bool up = (gt[k] >> lane) & 1, level = (eq[k] >> lane) & 1;
     if (up || (level && e_rank < ties)) sel[place] = k * kSelThreads + tid;
   }
-  if (tid == 0) p.sel_count[(int64_t)r * p.n_kv_heads + h] = keep;
+  if (tid == 0) p.sel_count[blockIdx.x] = keep;
 }
 
 namespace {
 
-template <int D, int RT, int KPT>
+template <int D, int RT, int KPT, bool SCORE>
 hipError_t launch_one(const SelectParams& p, hipStream_t s) {
   static std::atomic<bool> done[kMaxDevices];
-  const size_t lds = (size_t)p.max_pages * sizeof(uint32_t);
-  if (KPT > 8) {
-    const hipError_t e = ensure_lds_limit((const void*)select_kernel<D, RT, KPT>,
+  const size_t lds = SCORE ? (size_t)p.max_pages * sizeof(uint32_t) : 0;
+  if (SCORE && KPT > 8) {
+    const hipError_t e = ensure_lds_limit((const void*)select_kernel<D, RT, KPT, SCORE>,
                                           KAMERA_MAX_SELECT_PAGES * (int)sizeof(uint32_t), done);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((select_kernel<D, RT, KPT>), dim3((uint32_t)p.n_requests * p.n_kv_heads), dim3(kSelThreads), lds, s,
-                     p);
+  hipLaunchKernelGGL((select_kernel<D, RT, KPT, SCORE>), dim3((uint32_t)p.n_requests * p.n_kv_heads), dim3(kSelThreads),
+                     lds, s, p);
   return hipGetLastError();
 }
 
 template <int D, int RT>
-hipError_t launch_kpt(const SelectParams& p, hipStream_t s) {
-  return p.max_pages <= 8 * kSelThreads ? launch_one<D, RT, 8>(p, s) : launch_one<D, RT, 32>(p, s);
+hipError_t launch_rt(const SelectParams& p, hipStream_t s) {
+  const bool small = p.max_pages <= 8 * kSelThreads;
+  if (p.n_pieces == 0) return small ? launch_one<D, RT, 8, true>(p, s) : launch_one<D, RT, 32, true>(p, s);
+  hipLaunchKernelGGL((score_kernel<D, RT>), dim3((uint32_t)p.n_requests * p.n_pieces * p.n_kv_heads),
+                     dim3(kPieceWaves * 64), 0, s, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  return small ? launch_one<64, 1, 8, false>(p, s) : launch_one<64, 1, 32, false>(p, s);
 }
 
 }  // namespace
 
 hipError_t launch_select(const SelectParams& p, hipStream_t s) {
-  if (p.head_dim == 128) return p.group <= 16 ? launch_kpt<128, 1>(p, s) : launch_kpt<128, 4>(p, s);
-  return p.group <= 16 ? launch_kpt<64, 1>(p, s) : launch_kpt<64, 4>(p, s);
+  if (p.head_dim == 128) return p.group <= 16 ? launch_rt<128, 1>(p, s) : launch_rt<128, 4>(p, s);
+  return p.group <= 16 ? launch_rt<64, 1>(p, s) : launch_rt<64, 4>(p, s);
 }
 
 }  // namespace kamera
