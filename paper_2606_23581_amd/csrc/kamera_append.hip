@@ -1,16 +1,19 @@
 // kamera_append_paged8: bf16 rows into the 8-bit paged cache.
 //
-// Unit = (chunk, layer, page of the chunk, plane, head), one wave each, four a
-// workgroup; the four are neighbouring heads of the same rows.  With A the
+// Unit = (chunk, layer, page of the chunk, plane, head); a wave takes 16 of its
+// tokens, so a unit is one, two or four waves of a 4-wave workgroup, whose units
+// are neighbouring heads of the same rows.  With A the
 // largest finite |x| of the page's new rows, e = min { e : A <= 448 * 2^e } is
 // read off A's bf16 bits: 448 = 1.75 * 2^8, so e = exponent(A) - 8, one more
 // where the fraction of A passes 1.75.  Scaling by 2^-e is exact, so one
 // rounding (v_cvt_pk_fp8_f32, to nearest even) stands between the row and its
 // byte, and any correct implementation stores the same bytes.
 //
-// Bound by HBM: 2 bytes read and 1 written for each element.  A wave keeps the
-// page in registers between the maximum and the conversion, so rows are read
-// once; the page's key sums come from the converted bytes that it still holds.
+// Bound by HBM: 2 bytes read and 1 written for each element.  Waves keep their
+// rows in registers between the maximum and the conversion, so rows are read
+// once; the page's key sums come from the converted bytes that they still hold.
+// (One wave for a whole 64-token page: 1024-token chunks of 8 requests, one layer
+// of 8 heads, took 20.3 us.)
 
 #include "kamera_cache_device.h"
 
@@ -51,18 +54,23 @@ __device__ __forceinline__ void from_e4m3(u32x2 w, float (&f)[8]) {
 
 }  // namespace
 
-// D columns, SUB 16-token parts a page.  A row takes D / 8 lanes of 8 columns.
+// D columns, SUB 16-token parts (and waves) a page.  A row takes D / 8 lanes of 8 columns.
 template <int D, int SUB>
 __global__ __launch_bounds__(kAppThreads) void append_kernel(AppendParams) {
   constexpr int LPR = D / 8;                       // lanes a row
   constexpr int TPI = 64 / LPR;                    // tokens a step of the wave
-  constexpr int IT = SUB * 16 / TPI;               // steps a page
+  constexpr int IT = 16 / TPI;                     // steps
   constexpr int P = SUB * 16;
+  constexpr int kWaves = kAppThreads / 64, kUnits = kWaves / SUB;
   const AppendParams& p = kernel_params<AppendParams>();
-  const int lane = threadIdx.x & 63;
-  const uint32_t unit = blockIdx.x * (kAppThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (unit >= (uint32_t)p.n_units) return;
-  uint32_t u = unit, q;
+  __shared__ uint32_t s_top[kWaves];
+  __shared__ float s_sum[SUB > 1 ? kWaves : 1][D];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int sub = wave % SUB, wave0 = wave - sub;  // this wave's part, the unit's first wave
+  const uint32_t unit = blockIdx.x * kUnits + wave / SUB;
+  bool live = unit < (uint32_t)p.n_units;
+  if (SUB == 1 && !live) return;
+  uint32_t u = live ? unit : 0u, q;
   q = fast_div(u, p.fd_heads);
   const int h = (int)(u - q * p.n_heads);
   const int pl = (int)(q & 1);
@@ -79,18 +87,22 @@ __global__ __launch_bounds__(kAppThreads) void append_kernel(AppendParams) {
   const int64_t j = before / P + jp;               // page of the chunk
   const int64_t p0 = j * P;
   const int64_t lo64 = max((int64_t)before, p0) - p0, hi64 = min((int64_t)before + n, p0 + P) - p0;
-  if (hi64 <= lo64) return;
+  live = live && hi64 > lo64;
+  if (SUB == 1 && !live) return;
   const int lo = (int)lo64, hi = (int)hi64;        // new tokens of the page: [lo, hi)
   int page = -1;
-  if (j < p.pt_stride) page = uniform_load(p.page_table + (int64_t)c * p.pt_stride + j);
-  if (page < 0 || page >= p.n_pool_pages) {
+  if (live && j < p.pt_stride) page = uniform_load(p.page_table + (int64_t)c * p.pt_stride + j);
+  if (live && (page < 0 || page >= p.n_pool_pages)) {
     if (lane == 0 && p.status != nullptr)
       atomicOr(p.status, j < p.pt_stride ? KAMERA_STATUS_BAD_PAGE : KAMERA_STATUS_BAD_LENGTH);
-    return;
+    live = false;
   }
+  if (SUB == 1 && !live) return;
+  // with several waves a unit, all of the workgroup's waves go on to the barriers
+  if (!live) page = 0;
 
   const AppendPlane& pp = p.plane[pl];
-  const int t_lane = lane / LPR, col = (lane % LPR) * 8;
+  const int t_lane = sub * 16 + lane / LPR, col = (lane % LPR) * 8;
   const int64_t row0 = p0 - before + base;         // row of the page's token 0
   const uint16_t* rows = pp.rows + c * pp.rows_s[0] + l * pp.rows_s[1] + h * pp.rows_s[3] + col;
   u32x4 x[IT];
@@ -99,7 +111,7 @@ __global__ __launch_bounds__(kAppThreads) void append_kernel(AppendParams) {
   for (int i = 0; i < IT; ++i) {
     const int t = i * TPI + t_lane;
     x[i] = u32x4{0u, 0u, 0u, 0u};
-    if (t >= lo && t < hi) x[i] = ld16(rows + (row0 + t) * pp.rows_s[2]);
+    if (live && t >= lo && t < hi) x[i] = ld16(rows + (row0 + t) * pp.rows_s[2]);
   }
 #pragma unroll
   for (int i = 0; i < IT; ++i)
@@ -121,16 +133,24 @@ __global__ __launch_bounds__(kAppThreads) void append_kernel(AppendParams) {
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, d));
   }
+  if (SUB > 1) {
+    if (lane == 0) s_top[wave] = amax;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < SUB; ++k) amax = max(amax, s_top[wave0 + k]);
+  }
   int e = clamp_exp((int)(amax >> 7) - 127 - 8 + ((amax & 0x7fu) > 0x60u ? 1 : 0));
 
   float* scale = pp.scale + l * pp.scale_s[0] + page * pp.scale_s[1] + h * pp.scale_s[2];
   uint8_t* cache = pp.cache + l * pp.cache_s[0] + page * pp.cache_s[1] + h * pp.cache_s[3] + col;
-  const bool sums = pl == 0 && p.k_sum != nullptr && hi == P;
+  const bool sums = live && pl == 0 && p.k_sum != nullptr && hi == P;
   u32x2 old[IT];
 #pragma unroll
   for (int i = 0; i < IT; ++i) old[i] = u32x2{0u, 0u};
-  if (lo > 0) {                                    // tokens [0, lo) are there already
-    const int e_old = clamp_exp((int)((__float_as_uint(*scale) >> 23) & 0xffu) - 127);
+  int e_old = kMinExp;
+  if (live && lo > 0) e_old = clamp_exp((int)((__float_as_uint(*scale) >> 23) & 0xffu) - 127);
+  if (SUB > 1) __syncthreads();                    // every wave of the unit has the old scale
+  if (live && lo > 0) {                            // tokens [0, lo) are there already
     const bool lift = e > e_old;
     if (lift || sums) {
 #pragma unroll
@@ -161,13 +181,13 @@ __global__ __launch_bounds__(kAppThreads) void append_kernel(AppendParams) {
     }
   }
   const float inv = pow2(-e);
-  if (lane == 0) *scale = pow2(e);
+  if (live && lane == 0 && sub == 0) *scale = pow2(e);
   float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < IT; ++i) {
     const int t = i * TPI + t_lane;
     const u32x2 r = to_e4m3(x[i], inv);
-    if (t >= lo && t < hi) *reinterpret_cast<u32x2*>(cache + t * pp.cache_s[2]) = r;
+    if (live && t >= lo && t < hi) *reinterpret_cast<u32x2*>(cache + t * pp.cache_s[2]) = r;
     if (sums) {
       float f[8];
       from_e4m3(t < lo ? old[i] : r, f);
@@ -175,23 +195,34 @@ __global__ __launch_bounds__(kAppThreads) void append_kernel(AppendParams) {
       for (int k = 0; k < 8; ++k) sum[k] += f[k] == f[k] ? f[k] : 0.0f;
     }
   }
-  if (!sums) return;
+  if (SUB == 1 && !sums) return;
   // Multiples of 2^-9 below 64 * 448 < 2^15: every partial sum is exact in 24
   // bits, so the order does not matter.
-  float big = 0.f;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
+  for (int k = 0; k < 8; ++k)
 #pragma unroll
     for (int d = LPR; d < 64; d <<= 1) sum[k] += __shfl_xor(sum[k], d);
-    big = fmaxf(big, fabsf(sum[k]));
+  if (SUB > 1) {
+    if (lane < LPR)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s_sum[wave][col + k] = sum[k];
+    __syncthreads();
+    if (!sums || sub != 0) return;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int w = 1; w < SUB; ++w) sum[k] += s_sum[wave + w][col + k];
   }
+  float big = 0.f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) big = fmaxf(big, fabsf(sum[k]));
 #pragma unroll
   for (int d = 1; d < LPR; d <<= 1) big = fmaxf(big, __shfl_xor(big, d));
   // 127 = (1 + 0x7e0000 / 2^23) * 2^6
   const uint32_t bits = __float_as_uint(big);
   const int f = clamp_exp(big > 0.f ? (int)(bits >> 23) - 127 - 6 + ((bits & 0x7fffffu) > 0x7e0000u ? 1 : 0) : kMinExp);
   const float down = pow2(-f);
-  if (t_lane == 0) {
+  if (lane < LPR) {
     u32x2 w = {0u, 0u};
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -206,7 +237,8 @@ __global__ __launch_bounds__(kAppThreads) void append_kernel(AppendParams) {
 }
 
 hipError_t launch_append(const AppendParams& p, hipStream_t s) {
-  const dim3 grid((uint32_t)((p.n_units + kAppThreads / 64 - 1) / (kAppThreads / 64))), block(kAppThreads);
+  const int per = kAppThreads / 64 / (p.page_size / 16);   // units a workgroup
+  const dim3 grid((uint32_t)((p.n_units + per - 1) / per)), block(kAppThreads);
 #define KAMERA_APPEND(D, SUB) hipLaunchKernelGGL((append_kernel<D, SUB>), grid, block, 0, s, p)
   if (p.head_dim == 128) {
     switch (p.page_size) {

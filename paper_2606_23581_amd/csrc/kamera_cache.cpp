@@ -118,6 +118,7 @@ int build_tables(const kamera_page_tables_args* a, kamera::TablesParams& P, bool
   P.token_base = a->token_base;
   P.slots = a->n_slots > 0 ? a->slots : nullptr;
   P.n_slots = a->n_slots;
+  P.slots_aligned = aligned16(a->slots) ? 1 : 0;
   P.status = a->status;
   P.n_requests = a->n_requests;
   P.page_size = a->page_size;

@@ -24,7 +24,7 @@ struct TablesParams {
   int64_t n_slots;
   uint32_t* status;
   int32_t n_requests, page_size, pt_stride, n_pool_pages, n_free;
-  int32_t pad_;
+  int32_t slots_aligned;             // to 16 bytes
   FastDiv fd_page;
 };
 

@@ -130,11 +130,11 @@ __global__ __launch_bounds__(kTabThreads) void tables_kernel(TablesParams) {
     for (int64_t i0 = self * 4; i0 < p.n_slots; i0 += stride * 4) {
       int r = i0 < total_tokens ? owner(s_tokens, n, (int)i0) : n;
       int last_k = -1, pg = -1;
+      int64_t slot[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int64_t i = i0 + e;
-        if (i >= p.n_slots) break;
-        int64_t slot = -1;
+        slot[e] = -1;
         if (i < total_tokens) {
           while (i >= s_tokens[r + 1]) {
             ++r;
@@ -156,9 +156,16 @@ __global__ __launch_bounds__(kTabThreads) void tables_kernel(TablesParams) {
             }
             last_k = k;
           }
-          if (pg >= 0) slot = (int64_t)pg * p.page_size + (tok - (uint32_t)k * p.page_size);
+          if (pg >= 0) slot[e] = (int64_t)pg * p.page_size + (tok - (uint32_t)k * p.page_size);
         }
-        p.slots[i] = slot;
+      }
+      if (i0 + 4 <= p.n_slots && p.slots_aligned) {
+        reinterpret_cast<longlong2*>(p.slots + i0)[0] = make_longlong2(slot[0], slot[1]);
+        reinterpret_cast<longlong2*>(p.slots + i0)[1] = make_longlong2(slot[2], slot[3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (i0 + e < p.n_slots) p.slots[i0 + e] = slot[e];
       }
     }
   }
@@ -173,10 +180,11 @@ hipError_t launch_page_tables(const TablesParams& p, hipStream_t s) {
                                           (int)((3 * (size_t)KAMERA_MAX_REQUESTS + 2) * sizeof(int)), done);
     if (e != hipSuccess) return e;
   }
-  // four slots a thread; a workgroup repeats the sums, so no more than one a CU
+  // Four slots a thread.  Every workgroup repeats the sums: one a CU where these are
+  // long, four where a thread has one request at most.
   const int64_t items = p.slots != nullptr ? (p.n_slots + 3) / 4 : 0;
-  const int64_t want = std::max<int64_t>(items, p.n_requests + 1);
-  const int grid = (int)std::min<int64_t>((want + kTabThreads - 1) / kTabThreads, 256);
+  const int64_t want = std::max<int64_t>(items, p.n_requests + 1), most = p.n_requests <= kTabThreads ? 1024 : 256;
+  const int grid = (int)std::min<int64_t>((want + kTabThreads - 1) / kTabThreads, most);
   hipLaunchKernelGGL(tables_kernel, dim3(grid), dim3(kTabThreads), lds, s, p);
   return hipGetLastError();
 }
