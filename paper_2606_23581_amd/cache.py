@@ -91,9 +91,9 @@ def _typed(t, dtype, name, shape=None, contiguous=True):
     """t (or None) checked for its type, shape and, by default, dense layout."""
     if t is None:
         return None
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {str(dtype).replace('torch.', '')} (got {t.dtype})")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
     if contiguous and not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
@@ -103,30 +103,25 @@ def _typed(t, dtype, name, shape=None, contiguous=True):
 def _table(page_table, n):
     """The row stride of an int32 [n, pages] table whose rows are dense."""
     _i32_dev(page_table, "page_table")
-    if page_table.dim() != 2 or int(page_table.shape[0]) != n:
-        raise ValueError(f"page_table must be [{n}, pages] (got {tuple(page_table.shape)})")
-    if page_table.numel() > 0 and page_table.shape[1] > 1 and page_table.stride(1) != 1:
+    shape = page_table.shape
+    if len(shape) != 2 or shape[0] != n:
+        raise ValueError(f"page_table must be [{n}, pages] (got {tuple(shape)})")
+    s0, s1 = page_table.stride()
+    if s1 != 1 and shape[1] > 1 and n > 0:
         raise ValueError("the rows of page_table must be contiguous")
-    return int(page_table.stride(0)) if n > 1 else max(int(page_table.shape[1]), 1)
+    return s0 if n > 1 else max(shape[1], 1)
 
 
 def _device(*tensors):
     """All tensors on one GPU."""
     dev = None
     for t in tensors:
-        if t is None:
-            continue
-        if t.device.type != "cuda":
-            raise ValueError("tensors must be in device memory")
-        if dev is None:
+        if t is not None and t.device != dev:
+            if dev is not None:
+                raise ValueError(f"tensors on {dev} and {t.device} in one call")
             dev = t.device
-        elif t.device != dev:
-            raise ValueError(f"tensors on {dev} and {t.device} in one call")
-
-
-def _set(field, values):
-    for i, x in enumerate(values):
-        field[i] = int(x)
+            if dev.type != "cuda":
+                raise ValueError("tensors must be in device memory")
 
 
 def _workspace(a, need, workspace, device):
@@ -155,11 +150,11 @@ def _launch_with_workspace(call, stream, given) -> None:
 def _is8(t):
     import torch
 
-    return t.dtype in (torch.uint8, torch.float8_e4m3fn)
+    return t.dtype is torch.float8_e4m3fn or t.dtype is torch.uint8
 
 
 def _inner(t, name):
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError(f"the innermost dimension of {name} must be contiguous")
     return t
 
@@ -214,17 +209,18 @@ def prepare_page_tables(tokens_before, tokens_after, free_pages, page_table, *, 
     import torch
 
     L = lib()
-    R = int(tokens_after.shape[0])
+    R = tokens_after.shape[0]
     a = CPageTablesArgs()
     a.n_requests, a.page_size, a.n_pool_pages = R, int(page_size), int(n_pool_pages)
-    for t, nm, shape in ((tokens_before, "tokens_before", (R,)), (tokens_after, "tokens_after", (R,)),
-                         (free_pages, "free_pages", None), (free_begin, "free_begin", (1,)),
-                         (free_end, "free_end", (1,)), (token_base, "token_base", (R + 1,)), (status, "status", None)):
-        _typed(t, torch.int32, nm, shape)
+    i32 = torch.int32
+    _typed(tokens_before, i32, "tokens_before", (R,)), _typed(tokens_after, i32, "tokens_after", (R,))
+    _typed(free_pages, i32, "free_pages"), _typed(free_begin, i32, "free_begin", (1,))
+    _typed(free_end, i32, "free_end", (1,)), _typed(token_base, i32, "token_base", (R + 1,))
+    _typed(status, i32, "status")
     _typed(slots, torch.int64, "slots")
     _device(tokens_before, tokens_after, free_pages, page_table, free_begin, free_end, token_base, slots, status)
     a.pt_stride = _table(page_table, R)
-    if R > 1 and a.pt_stride != int(page_table.shape[1]):
+    if R > 1 and a.pt_stride != page_table.shape[1]:
         raise ValueError("page_table must be contiguous")
     a.tokens_before, a.tokens_after = _ptr(tokens_before), _ptr(tokens_after)
     a.free_pages, a.n_free = _ptr(free_pages), int(free_pages.numel())
@@ -258,29 +254,29 @@ def prepare_append_paged8(k, v, k_cache, v_cache, k_scale, v_scale, page_table, 
     L = lib()
     _inner(_bf16(k, "k"), "k"), _inner(_bf16(v, "v"), "v")
     a = CAppendArgs()
-    if tuple(k.shape) != tuple(v.shape):
+    if k.shape != v.shape:
         raise ValueError("k and v must have one shape")
-    C = int(page_table.shape[0])
+    C = page_table.shape[0]
     if row_base is not None:
         if k.dim() != 4 or n_tokens is None:
             raise ValueError("with row_base, k and v are [L, rows, H, D] and n_tokens is given")
-        Ln, _, H, D = (int(x) for x in k.shape)
-        _set(a.k_stride, (0, *k.stride()[:3]))
-        _set(a.v_stride, (0, *v.stride()[:3]))
+        Ln, _, H, D = k.shape
+        a.k_stride[0:4] = (0, *k.stride()[:3])
+        a.v_stride[0:4] = (0, *v.stride()[:3])
         n = int(n_tokens)
     else:
-        if k.dim() != 5 or int(k.shape[0]) != C:
+        if k.dim() != 5 or k.shape[0] != C:
             raise ValueError("k and v must be [C, L, n, H, D], C the rows of page_table")
-        _, Ln, rows, H, D = (int(x) for x in k.shape)
-        _set(a.k_stride, k.stride()[:4])
-        _set(a.v_stride, v.stride()[:4])
+        _, Ln, rows, H, D = k.shape
+        a.k_stride[0:4] = k.stride()[:4]
+        a.v_stride[0:4] = v.stride()[:4]
         n = rows if n_tokens is None else int(n_tokens)
         if n > rows:
             raise ValueError(f"n_tokens {n} exceeds the {rows} rows of a chunk")
-    if k_cache.dim() != 5 or tuple(k_cache.shape) != tuple(v_cache.shape):
+    if k_cache.dim() != 5 or k_cache.shape != v_cache.shape:
         raise ValueError("k_cache and v_cache must be [L, pages, page_size, H, D]")
-    _, n_pages, page_size = (int(x) for x in k_cache.shape[:3])
-    if tuple(k_cache.shape) != (Ln, n_pages, page_size, H, D):
+    _, n_pages, page_size = k_cache.shape[:3]
+    if k_cache.shape != (Ln, n_pages, page_size, H, D):
         raise ValueError(f"the caches must be [{Ln}, pages, page_size, {H}, {D}] (got {tuple(k_cache.shape)})")
     for t, nm in ((k_cache, "k_cache"), (v_cache, "v_cache")):
         if not _is8(t):
@@ -299,17 +295,17 @@ def prepare_append_paged8(k, v, k_cache, v_cache, k_scale, v_scale, page_table, 
     a.chunk_tokens, a.tokens_before, a.row_base = _ptr(chunk_tokens), _ptr(tokens_before), _ptr(row_base)
     a.page_table, a.k, a.v = _ptr(page_table), _ptr(k), _ptr(v)
     a.k_cache, a.v_cache, a.k_scale, a.v_scale = _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale)
-    _set(a.k_cache_stride, k_cache.stride()[:4])
-    _set(a.v_cache_stride, v_cache.stride()[:4])
-    _set(a.k_scale_stride, k_scale.stride())
-    _set(a.v_scale_stride, v_scale.stride())
+    a.k_cache_stride[0:4] = k_cache.stride()[:4]
+    a.v_cache_stride[0:4] = v_cache.stride()[:4]
+    a.k_scale_stride[:] = k_scale.stride()
+    a.v_scale_stride[:] = v_scale.stride()
     if k_sum is not None:
         _inner(k_sum, "k_sum")
         a.k_sum = _ptr(k_sum)
-        _set(a.k_sum_stride, k_sum.stride()[:3])
+        a.k_sum_stride[0:3] = k_sum.stride()[:3]
     if k_sum_scale is not None:
         a.k_sum_scale = _ptr(k_sum_scale)
-        _set(a.k_sum_scale_stride, k_sum_scale.stride())
+        a.k_sum_scale_stride[:] = k_sum_scale.stride()
     a.status = _ptr(status)
     return Prepared(L.kamera_append_paged8, a, (k, v, k_cache, v_cache, k_scale, v_scale, page_table, tokens_before,
                                                 chunk_tokens, row_base, k_sum, k_sum_scale, status))
@@ -334,14 +330,14 @@ def prepare_select_pages(q, k_sum, k_sum_scale, page_table, kv_tokens, sel, sel_
 
     L = lib()
     _inner(_bf16(q, "q"), "q")
-    R, HQ, D = (int(x) for x in q.shape)
+    R, HQ, D = q.shape
     _inner(_typed(k_sum, torch.int8, "k_sum", contiguous=False), "k_sum")
-    n_pages, H = (int(x) for x in k_sum.shape[:2])
-    if int(k_sum.shape[2]) != D:
+    n_pages, H = k_sum.shape[:2]
+    if k_sum.shape[2] != D:
         raise ValueError("q and k_sum must have one head size")
     _typed(k_sum_scale, torch.float32, "k_sum_scale", (n_pages, H), contiguous=False)
     _typed(kv_tokens, torch.int32, "kv_tokens", (R,))
-    keep = int(sel.shape[-1])
+    keep = sel.shape[-1]
     _typed(sel, torch.int32, "sel", (R, H, keep))
     _typed(sel_count, torch.int32, "sel_count", (R, H))
     _typed(status, torch.int32, "status")
@@ -350,10 +346,10 @@ def prepare_select_pages(q, k_sum, k_sum_scale, page_table, kv_tokens, sel, sel_
     a.n_requests, a.n_q_heads, a.n_kv_heads, a.head_dim, a.n_keys = R, HQ, H, D, int(n_keys)
     a.page_size, a.pt_stride, a.n_pool_pages = int(page_size), _table(page_table, R), n_pages
     a.kv_tokens, a.page_table, a.q = _ptr(kv_tokens), _ptr(page_table), _ptr(q)
-    _set(a.q_stride, q.stride()[:2])
+    a.q_stride[0:2] = q.stride()[:2]
     a.k_sum, a.k_sum_scale = _ptr(k_sum), _ptr(k_sum_scale)
-    _set(a.k_sum_stride, k_sum.stride()[:2])
-    _set(a.k_sum_scale_stride, k_sum_scale.stride())
+    a.k_sum_stride[0:2] = k_sum.stride()[:2]
+    a.k_sum_scale_stride[:] = k_sum_scale.stride()
     a.n_keep, a.n_first, a.n_last = keep, int(n_first), int(n_last)
     a.sel, a.sel_count, a.status = _ptr(sel), _ptr(sel_count), _ptr(status)
     workspace = _workspace(a, L.kamera_select_workspace(ctypes.byref(a)), workspace, q.device)
@@ -394,19 +390,19 @@ def prepare_attend_paged(q, k_cache, v_cache, out, page_table, kv_tokens, *, n_q
 
     L = lib()
     _inner(_bf16(q, "q"), "q"), _inner(_bf16(out, "out"), "out")
-    rows, HQ, D = (int(x) for x in q.shape)
-    if tuple(out.shape) != (rows, HQ, D):
+    rows, HQ, D = q.shape
+    if out.shape != q.shape:
         raise ValueError("out must have q's shape")
-    if k_cache.dim() != 4 or tuple(k_cache.shape) != tuple(v_cache.shape) or k_cache.dtype != v_cache.dtype:
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.dtype != v_cache.dtype:
         raise ValueError("k_cache and v_cache must be [pages, page_size, H, D] of one type")
-    n_pages, page_size, H, Dc = (int(x) for x in k_cache.shape)
+    n_pages, page_size, H, Dc = k_cache.shape
     if Dc != D:
         raise ValueError("q and the caches must have one head size")
     eight = _is8(k_cache)
     if not eight:
         _bf16(k_cache, "k_cache")
     _inner(k_cache, "k_cache"), _inner(v_cache, "v_cache")
-    R = int(kv_tokens.shape[0])
+    R = kv_tokens.shape[0]
     n_queries = int(n_queries)
     if q_base is None and R * n_queries > rows:
         raise ValueError(f"{R} requests of {n_queries} queries exceed the {rows} rows of q")
@@ -424,19 +420,19 @@ def prepare_attend_paged(q, k_cache, v_cache, out, page_table, kv_tokens, *, n_q
     a.scale = D ** -0.5 if scale is None else float(scale)
     a.q_tokens, a.q_base, a.kv_tokens, a.page_table = _ptr(q_tokens), _ptr(q_base), _ptr(kv_tokens), _ptr(page_table)
     a.q, a.out, a.lse = _ptr(q), _ptr(out), _ptr(lse)
-    _set(a.q_stride, q.stride()[:2])
-    _set(a.out_stride, out.stride()[:2])
+    a.q_stride[0:2] = q.stride()[:2]
+    a.out_stride[0:2] = out.stride()[:2]
     if lse is not None:
-        _set(a.lse_stride, lse.stride())
+        a.lse_stride[:] = lse.stride()
     a.k_cache, a.v_cache, a.k_scale, a.v_scale = _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale)
-    _set(a.k_cache_stride, k_cache.stride()[:3])
-    _set(a.v_cache_stride, v_cache.stride()[:3])
+    a.k_cache_stride[0:3] = k_cache.stride()[:3]
+    a.v_cache_stride[0:3] = v_cache.stride()[:3]
     if k_scale is not None:
-        _set(a.k_scale_stride, k_scale.stride())
+        a.k_scale_stride[:] = k_scale.stride()
     if v_scale is not None:
-        _set(a.v_scale_stride, v_scale.stride())
+        a.v_scale_stride[:] = v_scale.stride()
     if sel is not None:
-        keep = int(sel.shape[-1])
+        keep = sel.shape[-1]
         _typed(sel, torch.int32, "sel", (R, H, keep))
         _typed(sel_count, torch.int32, "sel_count", (R, H))
         a.sel, a.sel_count, a.sel_stride = _ptr(sel), _ptr(sel_count), keep

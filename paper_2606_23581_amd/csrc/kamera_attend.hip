@@ -400,88 +400,89 @@ __global__ __launch_bounds__(kAttThreads, 2) void attend_rows_kernel(AttendParam
 }
 
 // Joins the parts of each row: with M the largest of the parts' maxima m_s,
-// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.  One workgroup a row: a
-// thread takes four columns of every eighth (or 16th) part, all loads in flight.
-template <int D>
+// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.  A thread takes four columns
+// of every WAYS-th part, eight parts at a time with all their loads in flight; the
+// ways of a row meet in LDS.  Up to 8 parts one way a row and several rows a
+// workgroup (a workgroup a row took 88 us for 16384 rows of 2 parts), else 8 ways.
+template <int D, int WAYS>
 __global__ __launch_bounds__(kAttThreads) void attend_join_kernel(AttendParams) {
   const AttendParams& p = kernel_params<AttendParams>();
-  constexpr int kCols = D / 4, kWays = kAttThreads / kCols;
-  __shared__ float s_f[512];                       // the parts' weights
-  __shared__ float s_red[3][kAttWaves];
-  __shared__ __attribute__((aligned(16))) f32x4 s_o[kWays][kCols];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  uint32_t w = blockIdx.x, d;
+  constexpr int kCols = D / 4, kRows = kAttThreads / (kCols * WAYS), kChunk = 8;
+  static_assert(WAYS == 1 || kRows == 1 || D == 64, "");
+  __shared__ f32x4 s_o[WAYS > 1 ? kRows * WAYS : 1][kCols];
+  __shared__ float s_ml[WAYS > 1 ? kRows * WAYS : 1][3];
+  const int tid = threadIdx.x, col = tid % kCols, way = tid / kCols % WAYS, slot = tid / kCols;
+  const uint32_t task = blockIdx.x * kRows + tid / (kCols * WAYS);
+  if (WAYS == 1 && task >= (uint32_t)p.n_join) return;
+  uint32_t w = min(task, (uint32_t)p.n_join - 1), d;
   d = fast_div(w, p.fd_rows);
   const int row = (int)(w - d * p.rows_max);
   w = d;
   d = fast_div(w, p.fd_heads);
   const int h = (int)(w - d * p.n_kv_heads), r = (int)d;
-  const Request rq = request_of(p, r);
   const int i = (int)fast_div((uint32_t)row, p.fd_group);
+  int n = p.n_queries;
+  if (p.q_tokens != nullptr) n = min(max(p.q_tokens[r], 0), p.n_queries);
+  const int64_t row0 = p.q_base != nullptr ? (int64_t)p.q_base[r] : (int64_t)r * p.n_queries;
   const int64_t at = (((int64_t)r * p.n_kv_heads + h) * p.rows_max + row) * p.n_splits;
-  const int col = tid % kCols, way = tid / kCols;
-  // the first loads of the sums leave together with those of the weights
-  constexpr int kFirst = 8;
-  f32x4 first[kFirst];
-#pragma unroll
-  for (int k = 0; k < kFirst; ++k) {
-    const int s = way + k * kWays;
-    first[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (s < p.n_splits) first[k] = *reinterpret_cast<const f32x4*>(p.part_o + (at + s) * D + col * 4);
-  }
-  f32x4 ml[2];
-  float top = kLow;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int s = tid + k * kAttThreads;
-    ml[k] = f32x4{kLow, 0.f, 0.f, 0.f};
-    if (s < p.n_splits) ml[k] = *reinterpret_cast<const f32x4*>(p.part_ml + (at + s) * 4);
-    top = fmaxf(top, ml[k].x);
-  }
-  if (i >= rq.n) return;                           // a row that no request has (its parts were not written)
-#pragma unroll
-  for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x));
-  if (lane == 0) s_red[0][wave] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
-  float l = 0.f, lx = 0.f;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const float f = exp2_fast(ml[k].x - top);
-    s_f[tid + k * kAttThreads] = f;
-    l += ml[k].y * f;
-    lx += ml[k].z * f;
-  }
-#pragma unroll
-  for (int x = 1; x < 64; x <<= 1) {
-    l += __shfl_xor(l, x);
-    lx += __shfl_xor(lx, x);
-  }
-  if (lane == 0) {
-    s_red[1][wave] = l;
-    s_red[2][wave] = lx;
-  }
-  __syncthreads();
+
+  float top = kLow, l = 0.f, lx = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = way; s0 < p.n_splits; s0 += kChunk * WAYS) {
+    f32x4 ml[kChunk], o[kChunk];
 #pragma unroll
-  for (int k = 0; k < kFirst; ++k)
-    if (way + k * kWays < p.n_splits) acc += first[k] * s_f[way + k * kWays];
-#pragma unroll 2
-  for (int s = way + kFirst * kWays; s < p.n_splits; s += kWays)
-    acc += *reinterpret_cast<const f32x4*>(p.part_o + (at + s) * D + col * 4) * s_f[s];
-  s_o[way][col] = acc;
-  __syncthreads();
-  l = (s_red[1][0] + s_red[1][1]) + (s_red[1][2] + s_red[1][3]);
-  lx = (s_red[2][0] + s_red[2][1]) + (s_red[2][2] + s_red[2][3]);
-  const int64_t hq = (int64_t)h * p.group + (row - i * p.group);
-  if (tid < kCols) {
+    for (int k = 0; k < kChunk; ++k) {
+      const int s = min(s0 + k * WAYS, p.n_splits - 1);     // one past the end is read again and left out
+      ml[k] = *reinterpret_cast<const f32x4*>(p.part_ml + (at + s) * 4);
+      o[k] = *reinterpret_cast<const f32x4*>(p.part_o + (at + s) * D + col * 4);
+    }
+    float m = top;
 #pragma unroll
-    for (int k = 1; k < kWays; ++k) acc += s_o[k][tid];
-    acc *= l == 0.f ? 0.f : 1.0f / l;
-    *reinterpret_cast<u32x2*>(p.out + (rq.row0 + i) * p.out_s[0] + hq * p.out_s[1] + 4 * tid) =
-        u32x2{pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w)};
+    for (int k = 0; k < kChunk; ++k) m = fmaxf(m, ml[k].x);
+    const float down = exp2_fast(top - m);
+    top = m;
+    l *= down;
+    lx *= down;
+    acc *= down;
+#pragma unroll
+    for (int k = 0; k < kChunk; ++k)
+      if (s0 + k * WAYS < p.n_splits) {
+        const float f = exp2_fast(ml[k].x - top);
+        l += ml[k].y * f;
+        lx += ml[k].z * f;
+        acc += o[k] * f;
+      }
   }
-  if (tid == 0 && p.lse != nullptr) p.lse[(rq.row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] = row_lse(top, lx);
+  if (WAYS > 1) {
+    s_o[WAYS > 1 ? slot : 0][col] = acc;
+    if (col == 0) {
+      s_ml[WAYS > 1 ? slot : 0][0] = top;
+      s_ml[WAYS > 1 ? slot : 0][1] = l;
+      s_ml[WAYS > 1 ? slot : 0][2] = lx;
+    }
+    __syncthreads();
+    if (way != 0) return;
+    const float own = top;
+#pragma unroll
+    for (int k = 1; k < WAYS; ++k) top = fmaxf(top, s_ml[WAYS > 1 ? slot + k : 0][0]);
+    const float down = exp2_fast(own - top);
+    l *= down;
+    lx *= down;
+    acc *= down;
+#pragma unroll
+    for (int k = 1; k < WAYS; ++k) {
+      const float f = exp2_fast(s_ml[WAYS > 1 ? slot + k : 0][0] - top);
+      l += s_ml[WAYS > 1 ? slot + k : 0][1] * f;
+      lx += s_ml[WAYS > 1 ? slot + k : 0][2] * f;
+      acc += s_o[WAYS > 1 ? slot + k : 0][col] * f;
+    }
+  }
+  if (i >= n || task >= (uint32_t)p.n_join) return;   // a row that no request has (its parts were not written)
+  const int64_t hq = (int64_t)h * p.group + (row - i * p.group);
+  acc *= l == 0.f ? 0.f : 1.0f / l;
+  *reinterpret_cast<u32x2*>(p.out + (row0 + i) * p.out_s[0] + hq * p.out_s[1] + 4 * col) =
+      u32x2{pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w)};
+  if (col == 0 && p.lse != nullptr) p.lse[(row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] = row_lse(top, lx);
 }
 
 namespace {
@@ -496,6 +497,15 @@ hipError_t launch_rows(const AttendParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int D>
+hipError_t launch_join(const AttendParams& p, hipStream_t s) {
+  const int ways = p.n_splits <= 8 ? 1 : 8, rows = kAttThreads / (D / 4 * ways);
+  const dim3 grid((uint32_t)((p.n_join + rows - 1) / rows)), block(kAttThreads);
+  if (ways == 1) hipLaunchKernelGGL((attend_join_kernel<D, 1>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((attend_join_kernel<D, 8>), grid, block, 0, s, p);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_attend(const AttendParams& p, hipStream_t s) {
@@ -507,10 +517,7 @@ hipError_t launch_attend(const AttendParams& p, hipStream_t s) {
   else
     e = p.head_dim == 128 ? launch_rows<128, KAMERA_CACHE_BF16>(p, s) : launch_rows<64, KAMERA_CACHE_BF16>(p, s);
   if (e != hipSuccess || p.n_splits == 1) return e;
-  const dim3 grid((uint32_t)p.n_requests * p.n_kv_heads * p.rows_max), block(kAttThreads);
-  if (p.head_dim == 128) hipLaunchKernelGGL(attend_join_kernel<128>, grid, block, 0, s, p);
-  else hipLaunchKernelGGL(attend_join_kernel<64>, grid, block, 0, s, p);
-  return hipGetLastError();
+  return p.head_dim == 128 ? launch_join<128>(p, s) : launch_join<64>(p, s);
 }
 
 }  // namespace kamera

@@ -372,10 +372,18 @@ int size_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& laun
   if (a->n_splits > 0) {
     P.n_splits = a->n_splits;
   } else {
-    // parts of at least 256 keys, until there are two workgroups a CU
+    // Few rows: one workgroup a CU, parts of at least 128 keys; up to 768 keys in 8
+    // bits (384 in bf16) one part is as fast as many, which a second kernel joins (one
+    // request of 8 KV heads, 8 bits, 1 / 8 / 16 / 32 parts: 512 keys 8.1 / 9.8 / 9.8 /
+    // 10.0 us, 1024 keys 10.8 / 10.2 / 10.0 / 10.1, 4096 keys 26.8 / 12.4 / 11.2 / 10.8,
+    // 16384 keys 94.9 / 22.2 / 17.1 / 15.4).  Many rows: two workgroups a CU, parts of
+    // at least 512 keys.
     int64_t span_keys = a->sel_stride > 0 ? (int64_t)a->sel_stride * a->page_size : a->n_keys;
     if (a->window > 0) span_keys = std::min<int64_t>(span_keys, (int64_t)a->window + a->n_queries);
-    P.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(512 / tasks, span_keys / 256), 512));
+    const int64_t one = a->cache_type == KAMERA_CACHE_E4M3 ? 768 : 384;
+    const int64_t most = P.tiles ? std::min<int64_t>(512 / tasks, span_keys / 512)
+                                 : (span_keys <= one ? 1 : std::min<int64_t>(256 / tasks, span_keys / 128));
+    P.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(most, 512));
   }
   int64_t wgs = bounded_product({tasks, P.n_splits});
   const int64_t join = bounded_product({a->n_requests, a->n_kv_heads, rows});
@@ -390,6 +398,7 @@ int size_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& laun
   if (wgs < 0 || join < 0 || std::max(wgs, join) * 256 > 0xFFFFFFFFLL)
     return fail(KAMERA_ERR_RANGE, "%s: too many workgroups for one launch", who);
   P.n_tasks = (int32_t)wgs;
+  P.n_join = (int32_t)join;
   if (P.n_splits > 1) {
     workspace = bounded_product({join, P.n_splits, a->head_dim + 4, 4});
     if (workspace < 0) return fail(KAMERA_ERR_RANGE, "%s: workspace too large", who);

@@ -105,6 +105,7 @@ struct AttendParams {
   int32_t row_tiles;                 // tiles of 16 (few-rows) or 32 (many-rows kernel) rows a wave
   int32_t n_row_blocks;
   int32_t n_tasks;                   // workgroups
+  int32_t n_join;                    // rows of all requests and KV heads (n_splits > 1)
   int32_t deal;                      // many-rows kernel: shares that a (request, KV head) pair's row blocks
   int32_t n_shares;                  // are dealt into, shares on an XCD, row blocks of a share
   int32_t blocks_share;
