@@ -34,7 +34,7 @@ bool multiples(const int64_t* s, int n, int64_t of) {
 
 // Page selection: from so many pages a request on they are scored by workgroups of
 // their own (see kamera_select.hip).
-constexpr int64_t kSelectSplit = 2048;
+constexpr int64_t kSelectSplit = 1024;
 
 int check_head_dim(int32_t head_dim, const char* who) {
   if (head_dim != 64 && head_dim != 128)

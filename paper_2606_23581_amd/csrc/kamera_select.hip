@@ -3,8 +3,9 @@
 // A workgroup of 16 waves per (request, KV head) selects; it also scores the pages
 // itself where these are few or the workgroups many, and otherwise 256-page pieces
 // are scored by workgroups of their own before (the keys in between in a
-// workspace): a CU takes in about 25 bytes of key sums a cycle, 2 ns a page, and a
-// second launch costs some 4 us.  The group's query rows become int8 with one power-of-two scale; a page's score is the largest of
+// workspace): a CU takes in about 25 bytes of key sums a cycle, 2 ns a page (one
+// request of 8 KV heads, one kernel / two: 1000 pages 11.8 / 12.2 us, 2048 pages
+// 14.1 / 12.4, 8192 pages 29.0 / 13.8; 32 requests, 4096 pages: 50.1 / 54.4).  The group's query rows become int8 with one power-of-two scale; a page's score is the largest of
 // the group's int8 products with the page's key sum, times the page's scale.
 // |product| <= 127 * 127 * 128 < 2^24, so the fp32 score is exact and the
 // selection one answer.
