@@ -2,7 +2,7 @@
 // matrix products are the work (prompt chunks).
 //
 // Rows as in the few-rows kernel: (query token, head of the group) of one KV
-// head.  A wave takes RT tiles of 32 rows, a workgroup four waves, all over the
+// head.  A wave takes 32 rows, a workgroup four waves, all over the
 // same 64-token tiles of K and V, which the workgroup stages in LDS as bf16: K as
 // [token][D], V transposed, [D][token].  e4m3 becomes bf16 on the way, once for
 // all rows.
@@ -34,6 +34,7 @@ namespace {
 
 constexpr int kTileThreads = 256;
 constexpr int kTileKeys = 64;
+constexpr int kMfma = 0x8, kDsRead = 0x100;   // instruction groups of the scheduler
 constexpr float kLow = -3.402823466e38f;
 constexpr float kSlack = 8.0f;
 
@@ -157,11 +158,11 @@ __device__ __forceinline__ bool store_tile(Stage<D, FMT>& s, uint8_t* buf, const
 
 }  // namespace
 
-template <int D, int FMT, int RT>
-__global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_kernel(AttendParams) {
+template <int D, int FMT, bool LSE>
+__global__ __launch_bounds__(kTileThreads, 2) void attend_tiles_kernel(AttendParams) {
   const AttendParams& p = kernel_params<AttendParams>();
   constexpr int KC = D / 8, KS = D / 16, DT = D / 32;
-  constexpr int kRows = 4 * RT * 32;
+  constexpr int kRows = 4 * 32;
   constexpr int kVAt = kTileKeys * D * 2;          // a buffer holds K, then V^T: bytes to V^T, and of both
   constexpr int kBuf = 2 * kVAt;
   using S = Stage<D, FMT>;
@@ -210,37 +211,34 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_ke
   const int per = (max(tile1 - tile0, 0) + p.n_splits - 1) / p.n_splits;
   const int t_begin = tile0 + split * per, t_end = min(tile1, t_begin + per);
 
-  // this wave's rows
-  const int wave_row = row_first + wave * RT * 32;
-  bf16x8 qf[RT][KS];
-  int row_hi[RT], row_lo[RT];
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int row = wave_row + t * 32 + c32;
+  // this wave's rows; lane l has row l % 32
+  const int wave_row = row_first + wave * 32, row = wave_row + c32;
+  bf16x8 qf[KS];
+  int row_lo = 0x3fffffff;                         // sees the keys row_lo .. row_lo + row_span; none past the end
+  uint32_t row_span = 0;
+  {
     const int i = (int)fast_div((uint32_t)row, p.fd_group), hq = row - i * p.group;
     const bool there = row < row_end;
-    row_hi[t] = there ? min(last_key(p, rq, i), rq.kv - 1) : -1;
-    row_lo[t] = there ? first_key(p, last_key(p, rq, i)) : 0;
+    const int last = last_key(p, rq, i);
+    if (there && last >= 0) {
+      row_lo = first_key(p, last);
+      row_span = (uint32_t)(min(last, rq.kv - 1) - row_lo);
+    }
     const uint16_t* src = p.q + (rq.row0 + i) * p.q_s[0] + ((int64_t)h * p.group + hq) * p.q_s[1] + hf * 8;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       u32x4 x = {0u, 0u, 0u, 0u};
       if (there) x = *reinterpret_cast<const u32x4*>(src + ks * 16) ^ p.q_sign;
-      qf[t][ks] = __builtin_bit_cast(bf16x8, x);
+      qf[ks] = __builtin_bit_cast(bf16x8, x);
     }
   }
 
-  f32x16 o[RT][DT];
-  float m[RT], l[RT], lx[RT];
+  f32x16 o[DT];
+  float m = kLow, l = 0.f, lx = 0.f;
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    m[t] = kLow;
-    l[t] = lx[t] = 0.f;
+  for (int b = 0; b < DT; ++b)
 #pragma unroll
-    for (int b = 0; b < DT; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[t][b][i] = 0.f;
-  }
+    for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
 
   // this thread's places in global memory and in LDS
   const int tid = threadIdx.x, q4 = (tid >> 4) & 3, cg = tid & 15;
@@ -296,78 +294,95 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_ke
     }
     const bool partial = is_partial(tile, bad);
 
-    f32x16 sc[RT][2];
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sc[t][u][i] = 0.f;
+    // S^T.  The chunks of the first 32 tokens are read together and those of the
+    // second one by one behind the products, so that no product waits for its own
+    // read: with reads two products ahead a third of the time went into such waits.
+    __builtin_amdgcn_s_setprio(1);
+    f32x16 sc[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const bf16x8 a = *reinterpret_cast<const bf16x8*>(lds + k_at[ks] + (B + u * 32 * D * 2));
+      for (int i = 0; i < 16; ++i) sc[u][i] = 0.f;
+    constexpr int kAhead = FMT == KAMERA_CACHE_BF16 ? KS / 2 : KS;
+    bf16x8 kf[2][KS];
 #pragma unroll
-        for (int t = 0; t < RT; ++t) sc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[t][ks], sc[t][u], 0, 0, 0);
-      }
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) kf[u][ks] = *reinterpret_cast<const bf16x8*>(lds + k_at[ks] + (B + u * 32 * D * 2));
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u][ks], qf[ks], sc[u], 0, 0, 0);
+    __builtin_amdgcn_sched_group_barrier(kDsRead, kAhead, 0);
+#pragma unroll
+    for (int ks = 0; ks < 2 * KS - kAhead; ++ks) {
+      __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kMfma, kAhead, 0);
+    __builtin_amdgcn_s_setprio(0);
 
-    bf16x8 pf[RT][4];
+    if (partial) {
+      const int row_at = tile * kTileKeys + 4 * hf - row_lo;
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      if (partial) {
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t from_lo = (uint32_t)(row_at + (u * 32 + 8 * (i >> 2) + (i & 3)));
+          sc[u][i] = from_lo <= row_span ? sc[u][i] : -INFINITY;
+        }
+      if (bad != 0) {                              // parts that are not in the pool
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int off = u * 32 + 8 * (i >> 2) + 4 * hf + (i & 3), pos = tile * kTileKeys + off;
-            const bool seen = pos >= row_lo[t] && pos <= row_hi[t] && ((bad >> (u * 2 + (i >> 3))) & 1) == 0;
-            sc[t][u][i] = seen ? sc[t][u][i] : -INFINITY;
-          }
-      }
-      float top = max2(sc[t][0][0], sc[t][1][0]);
-#pragma unroll
-      for (int i = 1; i < 16; ++i) top = max2(max2(top, sc[t][0][i]), sc[t][1][i]);
-      top *= p.scale2;
-      if (__ballot(top > m[t] + kSlack) != 0) {
-        const float m_new = fmaxf(m[t], max_x32(top));
-        const float down = exp2_fast(m[t] - m_new);
-        m[t] = m_new;
-        l[t] *= down;
-        lx[t] *= down;
-#pragma unroll
-        for (int b = 0; b < DT; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[t][b][i] *= down;
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float x[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = exp2_fast(__builtin_fmaf(sc[t][u][i], p.scale2, -m[t]));
-        if (p.lse != nullptr) {
-#pragma unroll
-          for (int i = 0; i < 16; i += 4) lx[t] += (x[i] + x[i + 1]) + (x[i + 2] + x[i + 3]);
-        }
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const u32x4 w = {pack_bf16x2(x[8 * s], x[8 * s + 1]), pack_bf16x2(x[8 * s + 2], x[8 * s + 3]),
-                           pack_bf16x2(x[8 * s + 4], x[8 * s + 5]), pack_bf16x2(x[8 * s + 6], x[8 * s + 7])};
-          l[t] = add_pair(w.w, add_pair(w.z, add_pair(w.y, add_pair(w.x, l[t]))));
-          pf[t][u * 2 + s] = __builtin_bit_cast(bf16x8, w);
-        }
+          for (int i = 0; i < 16; ++i) sc[u][i] = (bad >> (u * 2 + (i >> 3))) & 1 ? -INFINITY : sc[u][i];
       }
     }
+    float top = max2(sc[0][0], sc[1][0]);
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = max2(max2(top, sc[0][i]), sc[1][i]);
+    top *= p.scale2;
+    if (__ballot(top > m + kSlack) != 0) {
+      const float m_new = fmaxf(m, max_x32(top));
+      const float down = exp2_fast(m - m_new);
+      m = m_new;
+      l *= down;
+      lx *= down;
+#pragma unroll
+      for (int b = 0; b < DT; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] *= down;
+    }
 
+    // P^T of the first 32 tokens, then their products with V^T between the steps of
+    // the other half's exponentials.
+    __builtin_amdgcn_s_setprio(1);
+    bf16x8 vf[4][DT];
 #pragma unroll
-    for (int b = 0; b < DT; ++b)
+    for (int s = 0; s < 4; ++s)
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const bf16x8 a = *reinterpret_cast<const bf16x8*>(lds + v_at[b][s] + B);
+      for (int b = 0; b < DT; ++b) vf[s][b] = *reinterpret_cast<const bf16x8*>(lds + v_at[b][s] + B);
 #pragma unroll
-        for (int t = 0; t < RT; ++t) o[t][b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pf[t][s], o[t][b], 0, 0, 0);
+    for (int u = 0; u < 2; ++u) {
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = exp2_fast(__builtin_fmaf(sc[u][i], p.scale2, -m));
+      if (LSE) {
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) lx += (x[i] + x[i + 1]) + (x[i + 2] + x[i + 3]);
       }
-
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const u32x4 w = {pack_bf16x2(x[8 * s], x[8 * s + 1]), pack_bf16x2(x[8 * s + 2], x[8 * s + 3]),
+                         pack_bf16x2(x[8 * s + 4], x[8 * s + 5]), pack_bf16x2(x[8 * s + 6], x[8 * s + 7])};
+        l = add_pair(w.w, add_pair(w.z, add_pair(w.y, add_pair(w.x, l))));
+        const bf16x8 pf = __builtin_bit_cast(bf16x8, w);
+#pragma unroll
+        for (int b = 0; b < DT; ++b)
+          o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * u + s][b], pf, o[b], 0, 0, 0);
+      }
+    }
+    __builtin_amdgcn_s_setprio(0);
     bad = bad_next;
     if (tile + 1 < t_end) store(tile + 1, bad, lds + kOther);
     __syncthreads();
@@ -377,36 +392,30 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_ke
     if (tile + 1 < t_end) step(std::integral_constant<int, 1>{}, tile + 1);
   }
 
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const int row = wave_row + t * 32 + c32;
-    const float ll = sum_x32(l[t]), lxx = sum_x32(lx[t]);
-    if (row >= row_end) continue;
+  l = sum_x32(l);
+  if (LSE) lx = sum_x32(lx);
+  if (row < row_end) {
     if (p.n_splits > 1) {
-      const int64_t at = (((int64_t)r * p.n_kv_heads + h) * p.rows_max + row) * p.n_splits + split;
+      const int64_t part = (((int64_t)r * p.n_kv_heads + h) * p.rows_max + row) * p.n_splits + split;
 #pragma unroll
       for (int b = 0; b < DT; ++b)
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
-          *reinterpret_cast<f32x4*>(p.part_o + at * D + b * 32 + 2 * i + 4 * hf) =
-              f32x4{o[t][b][i], o[t][b][i + 1], o[t][b][i + 2], o[t][b][i + 3]};
-      if (hf == 0) {
-        *reinterpret_cast<f32x4*>(p.part_ml + at * 4) = f32x4{m[t], ll, lxx, 0.f};
-      }
+          *reinterpret_cast<f32x4*>(p.part_o + part * D + b * 32 + 2 * i + 4 * hf) =
+              f32x4{o[b][i], o[b][i + 1], o[b][i + 2], o[b][i + 3]};
+      if (hf == 0) *reinterpret_cast<f32x4*>(p.part_ml + part * 4) = f32x4{m, l, lx, 0.f};
     } else {
       const int i = (int)fast_div((uint32_t)row, p.fd_group);
       const int64_t hq = (int64_t)h * p.group + (row - i * p.group);
-      const float inv = ll == 0.f ? 0.f : 1.0f / ll;
+      const float inv = l == 0.f ? 0.f : 1.0f / l;
       uint16_t* dst = p.out + (rq.row0 + i) * p.out_s[0] + hq * p.out_s[1] + 4 * hf;
 #pragma unroll
       for (int b = 0; b < DT; ++b)
 #pragma unroll
         for (int e = 0; e < 16; e += 4)
           *reinterpret_cast<u32x2*>(dst + b * 32 + 2 * e) =
-              u32x2{pack_bf16x2(o[t][b][e] * inv, o[t][b][e + 1] * inv),
-                    pack_bf16x2(o[t][b][e + 2] * inv, o[t][b][e + 3] * inv)};
-      if (p.lse != nullptr && hf == 0)
-        p.lse[(rq.row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] = row_lse(m[t], lxx);
+              u32x2{pack_bf16x2(o[b][e] * inv, o[b][e + 1] * inv), pack_bf16x2(o[b][e + 2] * inv, o[b][e + 3] * inv)};
+      if (LSE && hf == 0) p.lse[(rq.row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] = row_lse(m, lx);
     }
   }
   if (s_odd)
@@ -415,27 +424,27 @@ __global__ __launch_bounds__(kTileThreads, RT == 1 ? 2 : 1) void attend_tiles_ke
 
 namespace {
 
-template <int D, int FMT, int RT>
+template <int D, int FMT, bool LSE>
 hipError_t launch_one(const AttendParams& p, hipStream_t s) {
   static std::atomic<bool> done[kMaxDevices];
   const int lds = 4 * kTileKeys * D * 2;
-  const hipError_t e = ensure_lds_limit((const void*)attend_tiles_kernel<D, FMT, RT>, lds, done);
+  const hipError_t e = ensure_lds_limit((const void*)attend_tiles_kernel<D, FMT, LSE>, lds, done);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((attend_tiles_kernel<D, FMT, RT>), dim3((uint32_t)p.n_tasks), dim3(kTileThreads), lds, s, p);
+  hipLaunchKernelGGL((attend_tiles_kernel<D, FMT, LSE>), dim3((uint32_t)p.n_tasks), dim3(kTileThreads), lds, s, p);
   return hipGetLastError();
 }
 
-template <int RT>
-hipError_t launch_rt(const AttendParams& p, hipStream_t s) {
-  if (p.cache_type == KAMERA_CACHE_E4M3)
-    return p.head_dim == 128 ? launch_one<128, KAMERA_CACHE_E4M3, RT>(p, s) : launch_one<64, KAMERA_CACHE_E4M3, RT>(p, s);
-  return p.head_dim == 128 ? launch_one<128, KAMERA_CACHE_BF16, RT>(p, s) : launch_one<64, KAMERA_CACHE_BF16, RT>(p, s);
+template <int D, int FMT>
+hipError_t launch_lse(const AttendParams& p, hipStream_t s) {
+  return p.lse != nullptr ? launch_one<D, FMT, true>(p, s) : launch_one<D, FMT, false>(p, s);
 }
 
 }  // namespace
 
 hipError_t launch_attend_tiles(const AttendParams& p, hipStream_t s) {
-  return p.row_tiles == 1 ? launch_rt<1>(p, s) : launch_rt<2>(p, s);
+  if (p.cache_type == KAMERA_CACHE_E4M3)
+    return p.head_dim == 128 ? launch_lse<128, KAMERA_CACHE_E4M3>(p, s) : launch_lse<64, KAMERA_CACHE_E4M3>(p, s);
+  return p.head_dim == 128 ? launch_lse<128, KAMERA_CACHE_BF16>(p, s) : launch_lse<64, KAMERA_CACHE_BF16>(p, s);
 }
 
 }  // namespace kamera
