@@ -3,8 +3,8 @@
 //
 // Rows.  The query rows that share a KV head -- every query token's `group`
 // heads -- are one matrix of rows (token, head), taken 16 at a time as the N
-// side of the 16x16x32 bf16 MFMA, NR such tiles a workgroup, so a key is
-// fetched and converted once for all of them.
+// side of the 16x16x32 bf16 MFMA, NR such tiles a workgroup (one, or two of an
+// 8-bit cache), so a key is fetched and converted once for all of them.
 //
 // A step of a wave is 32 tokens, two 16-token parts that each lie in one page.
 //   S^T = K Q^T: K's rows are the A operand; a lane takes 16 bytes of one
@@ -487,14 +487,16 @@ __global__ __launch_bounds__(kAttThreads) void attend_join_kernel(AttendParams) 
 
 namespace {
 
-template <int D, int FMT>
+template <int D, int FMT, int NR>
 hipError_t launch_rows(const AttendParams& p, hipStream_t s) {
-  const dim3 grid((uint32_t)p.n_tasks), block(kAttThreads);
-  switch (p.row_tiles) {
-    case 1: hipLaunchKernelGGL((attend_rows_kernel<D, FMT, 1>), grid, block, 0, s, p); break;
-    default: hipLaunchKernelGGL((attend_rows_kernel<D, FMT, 2>), grid, block, 0, s, p); break;
-  }
+  hipLaunchKernelGGL((attend_rows_kernel<D, FMT, NR>), dim3((uint32_t)p.n_tasks), dim3(kAttThreads), 0, s, p);
   return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_few(const AttendParams& p, hipStream_t s) {
+  if (p.cache_type == KAMERA_CACHE_BF16) return launch_rows<D, KAMERA_CACHE_BF16, 1>(p, s);
+  return p.row_tiles == 1 ? launch_rows<D, KAMERA_CACHE_E4M3, 1>(p, s) : launch_rows<D, KAMERA_CACHE_E4M3, 2>(p, s);
 }
 
 template <int D>
@@ -509,13 +511,8 @@ hipError_t launch_join(const AttendParams& p, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_attend(const AttendParams& p, hipStream_t s) {
-  hipError_t e;
-  if (p.tiles)
-    e = launch_attend_tiles(p, s);
-  else if (p.cache_type == KAMERA_CACHE_E4M3)
-    e = p.head_dim == 128 ? launch_rows<128, KAMERA_CACHE_E4M3>(p, s) : launch_rows<64, KAMERA_CACHE_E4M3>(p, s);
-  else
-    e = p.head_dim == 128 ? launch_rows<128, KAMERA_CACHE_BF16>(p, s) : launch_rows<64, KAMERA_CACHE_BF16>(p, s);
+  const hipError_t e =
+      p.tiles ? launch_attend_tiles(p, s) : (p.head_dim == 128 ? launch_few<128>(p, s) : launch_few<64>(p, s));
   if (e != hipSuccess || p.n_splits == 1) return e;
   return p.head_dim == 128 ? launch_join<128>(p, s) : launch_join<64>(p, s);
 }

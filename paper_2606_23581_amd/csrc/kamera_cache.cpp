@@ -359,14 +359,14 @@ int size_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& laun
   if (rows > INT32_MAX / 2) return fail(KAMERA_ERR_RANGE, "%s: too many query rows", who);
   memset(&P, 0, sizeof(P));
   P.rows_max = (int32_t)rows;
-  P.tiles = rows > 32 && a->sel_stride == 0 ? 1 : 0;
-  if (P.tiles) {
-    P.row_tiles = 1;
-    P.n_row_blocks = (int32_t)ceil_div(rows, 128 * P.row_tiles);
-  } else {
-    P.row_tiles = rows <= 16 ? 1 : 2;
-    P.n_row_blocks = (int32_t)ceil_div(rows, 16 * P.row_tiles);
-  }
+  // Few rows or many.  The few-rows kernel takes 32 rows of an 8-bit cache at once
+  // (4 queries of 8 heads, 32 requests of 8192 keys: 101 us, with the other kernel
+  // 152), and 16 of a bf16 one, whose loads leave no registers for more (202 us with
+  // the many-rows kernel, 324 with two tiles a wave here).
+  const bool e4m3 = a->cache_type == KAMERA_CACHE_E4M3;
+  P.tiles = rows > (e4m3 ? 32 : 16) && a->sel_stride == 0 ? 1 : 0;
+  P.row_tiles = !P.tiles && e4m3 && rows > 16 ? 2 : 1;
+  P.n_row_blocks = (int32_t)ceil_div(rows, P.tiles ? 128 : 16 * P.row_tiles);
   const int64_t tasks = bounded_product({a->n_requests, a->n_kv_heads, P.n_row_blocks});
   if (tasks < 0) return fail(KAMERA_ERR_RANGE, "%s: too many requests, heads and rows", who);
   if (a->n_splits > 0) {
@@ -380,7 +380,7 @@ int size_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& laun
     // at least 512 keys.
     int64_t span_keys = a->sel_stride > 0 ? (int64_t)a->sel_stride * a->page_size : a->n_keys;
     if (a->window > 0) span_keys = std::min<int64_t>(span_keys, (int64_t)a->window + a->n_queries);
-    const int64_t one = a->cache_type == KAMERA_CACHE_E4M3 ? 768 : 384;
+    const int64_t one = e4m3 ? 768 : 384;
     const int64_t most = P.tiles ? std::min<int64_t>(512 / tasks, span_keys / 512)
                                  : (span_keys <= one ? 1 : std::min<int64_t>(256 / tasks, span_keys / 128));
     P.n_splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(most, 512));
@@ -509,7 +509,6 @@ int build_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& lau
   P.fd_shares = kamera::make_fast_div((uint32_t)std::max(P.n_shares, 1));
   P.fd_deal = kamera::make_fast_div((uint32_t)std::max(P.deal, 1));
   P.fd_page16 = kamera::make_fast_div((uint32_t)a->page_size / 16);
-  P.fd_page = kamera::make_fast_div((uint32_t)a->page_size);
   launch = true;
   return KAMERA_OK;
 }

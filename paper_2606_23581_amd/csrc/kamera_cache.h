@@ -102,7 +102,7 @@ struct AttendParams {
   int32_t n_splits;
   int32_t rows_max;                  // n_queries * group: rows of one (request, KV head)
   int32_t tiles;                     // 1: the many-rows kernel
-  int32_t row_tiles;                 // tiles of 16 (few-rows) or 32 (many-rows kernel) rows a wave
+  int32_t row_tiles;                 // few-rows kernel: tiles of 16 rows a wave, 1 or 2
   int32_t n_row_blocks;
   int32_t n_tasks;                   // workgroups
   int32_t n_join;                    // rows of all requests and KV heads (n_splits > 1)
@@ -110,7 +110,7 @@ struct AttendParams {
   int32_t n_shares;                  // are dealt into, shares on an XCD, row blocks of a share
   int32_t blocks_share;
   FastDiv fd_group, fd_heads, fd_blocks, fd_splits, fd_rows, fd_shares, fd_deal;
-  FastDiv fd_page16, fd_page;        // by page_size / 16 and page_size
+  FastDiv fd_page16;                 // by page_size / 16
 };
 
 hipError_t launch_page_tables(const TablesParams& p, hipStream_t s);

@@ -706,3 +706,52 @@ def test_decode_loop_on_a_stream_and_in_a_graph():
                 assert torch.equal(x, y)
     # the full attention of the last step differs from the selected pages' (pages were left out)
     assert not torch.equal(eager[-1][5], eager[-1][6])
+
+
+def test_example_answers_from_recalled_chunks():
+    """The example's steps from its graph equal the eager ones, and its last answer token the plain form over
+    the cache that it leaves."""
+    from examples.answer_from_recall import answer
+
+    kw = dict(chunks=3, tokens=64, layers=2, question=20, steps=3, keep=6, seed=9)
+    torch.manual_seed(1)
+    out_q, answers, r = answer(**kw)
+    torch.manual_seed(1)
+    out_q2, answers2, _ = answer(graph=False, **kw)
+    assert torch.equal(out_q, out_q2) and torch.equal(answers, answers2)
+    n = int(r.tokens)
+    assert n == 3 * 64 + 20 + 3 and int(r.count.min()) == 6
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(9)
+    # the last layer's query of the last step, drawn again in the example's order
+    q = last_query(gen, kw)
+    bytes_ = r.cache.k[1].contiguous().view(torch.uint8).cpu().numpy()
+    v_bytes = r.cache.v[1].contiguous().view(torch.uint8).cpu().numpy()
+    ks, vs = r.cache.k_scale[1].cpu().double().numpy(), r.cache.v_scale[1].cpu().double().numpy()
+    k, v = ref.decode(bytes_) * ks[:, None, :, None], ref.decode(v_bytes) * vs[:, None, :, None]
+    table = r.table.cpu().numpy()
+    sel = [[int(x) for x in r.sel[0, h].cpu() if x >= 0] for h in range(8)]
+    k_sum, k_sum_scale = r.cache.k_sum[1].cpu().numpy(), r.cache.k_sum_scale[1].cpu().double().numpy()
+    qv = q.double().cpu().numpy()
+    assert sel == ref.select(qv, k_sum, k_sum_scale, table, [n], 16, 6, 1, 2)
+    a = (table, [n], [1], [0], 16, 128 ** -0.5, True, 0, sel)
+    want, _ = ref.attend(qv, k, v, *a)
+    size, _ = ref.attend(qv, k, np.abs(v), *a)
+    got = answers[-1, 1].double().cpu().numpy()
+    assert (np.abs(got - want) <= BOUND * size).all()
+
+
+def last_query(gen, kw):
+    def rows(*shape):
+        return torch.randn(shape, generator=gen, device=DEV).to(torch.bfloat16)
+
+    c, n, layers = kw["chunks"], kw["tokens"], kw["layers"]
+    rows(c, layers, n, 8, 128), rows(c, layers, n, 8, 128)
+    rows(2, c, layers, 8, n, 16), rows(2, c, layers, 8, 16, 128)
+    rows(2, 1, layers, kw["question"], 8, 128)
+    for _ in range(layers):
+        rows(kw["question"], 64, 128)
+    for _ in range(kw["steps"]):
+        rows(2, 1, layers, 1, 8, 128)
+        q = rows(layers, 1, 64, 128)
+    return q[-1]
