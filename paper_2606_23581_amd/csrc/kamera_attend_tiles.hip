@@ -214,7 +214,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void attend_tiles_kernel(AttendPar
   // this wave's rows; lane l has row l % 32
   const int wave_row = row_first + wave * 32, row = wave_row + c32;
   bf16x8 qf[KS];
-  int row_lo = 0x3fffffff;                         // sees the keys row_lo .. row_lo + row_span; none past the end
+  int row_lo = INT32_MAX;                          // sees the keys row_lo .. row_lo + row_span; none past the end
   uint32_t row_span = 0;
   {
     const int i = (int)fast_div((uint32_t)row, p.fd_group), hq = row - i * p.group;

@@ -755,3 +755,66 @@ def last_query(gen, kw):
         rows(2, 1, layers, 1, 8, 128)
         q = rows(layers, 1, 64, 128)
     return q[-1]
+
+
+def test_calls_on_a_given_stream():
+    """Calls handed a stream (an object or a raw handle) run there, after what that stream holds already, and a
+    workspace of their own outlives the call."""
+    s = attend_case(dict(kv=[3000, 700], H=2, G=4))
+    table, kv = i32(s["table"]), i32(s["kv"])
+    want = torch.zeros_like(s["q"])
+    km.attend_paged(s["q"], s["kt"], s["vt"], want, table, kv, n_queries=1, n_keys=3000, **s["scales"])
+    torch.cuda.synchronize()
+    for raw in (False, True):
+        side = torch.cuda.Stream()
+        q = torch.zeros_like(s["q"])
+        out = torch.zeros_like(s["q"])
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(2_000_000)
+            q.copy_(s["q"])
+        km.attend_paged(q, s["kt"], s["vt"], out, table, kv, n_queries=1, n_keys=3000, n_splits=4,
+                        stream=side.cuda_stream if raw else side, **s["scales"])
+        # memory that the current stream takes meanwhile is not the call's workspace
+        noise = [torch.full((1 << 20,), float("nan"), device=DEV) for _ in range(4)]
+        side.synchronize()
+        assert len(noise) == 4
+        assert float((out.float() - want.float()).abs().max()) <= 2.0 ** -6
+
+
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+@pytest.mark.parametrize("queries", [1, 3, 40])
+def test_a_query_that_is_not_finite_stays_in_its_row(cache, queries):
+    s = attend_case(dict(kv=[150], nq=[queries], H=2, G=4, cache=cache))
+    clean, out = torch.zeros_like(s["q"]), torch.zeros_like(s["q"])
+    table, kv = i32(s["table"]), i32(s["kv"])
+    km.attend_paged(s["q"], s["kt"], s["vt"], clean, table, kv, n_queries=queries, n_keys=150, **s["scales"])
+    q = s["q"].clone()
+    q[queries // 2, 5, 9] = float("nan")
+    km.attend_paged(q, s["kt"], s["vt"], out, table, kv, n_queries=queries, n_keys=150, **s["scales"])
+    torch.cuda.synchronize()
+    hit = torch.zeros(s["q"].shape[:2], dtype=torch.bool, device=DEV)
+    hit[queries // 2, 5] = True
+    assert torch.isnan(out[hit].float()).all()
+    assert torch.equal(out[~hit], clean[~hit])
+
+
+def test_parts_of_a_context_join_by_lse():
+    """Attention over two halves of the pages, joined by their lse, is the attention over all of them."""
+    s = attend_case(dict(kv=[640, 640], H=2, G=4, page=32))
+    table, n = i32(s["table"]), 640
+    outs, lses = [], []
+    for a, b in ((0, 20), (0, 7), (7, 20)):
+        out, lse = torch.zeros_like(s["q"]), torch.zeros(s["q"].shape[:2], device=DEV)
+        km.attend_paged(s["q"], s["kt"], s["vt"], out, table[:, a:b], i32([(b - a) * 32] * 2), n_queries=1,
+                        n_keys=(b - a) * 32, causal=False, lse=lse, **s["scales"])
+        outs.append(out.double())
+        lses.append(lse.double())
+    torch.cuda.synchronize()
+    w = torch.softmax(torch.stack(lses[1:]), 0)[..., None]
+    joined = w[0] * outs[1] + w[1] * outs[2]
+    size, _ = ref.attend(s["qv"], s["k"], np.abs(s["v"]), s["table"], s["kv"], s["nq"], s["base"], 32, 128 ** -0.5,
+                         False)
+    # each side within BOUND of the exact one
+    assert (np.abs((joined - outs[0]).cpu().numpy()) <= 2 * BOUND * size).all()
+    assert float((torch.logsumexp(torch.stack(lses[1:]), 0) - lses[0]).abs().max()) <= 2.0 ** -10
