@@ -75,21 +75,21 @@ __device__ __forceinline__ void load_step(const AttendParams& p, const Parts& a,
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     s.pos[u] = lane_int(a.pos, lane + u);
-    const uint8_t* kb = lane_address(a.k, lane + u);
-    const uint8_t* vb = lane_address(a.v, lane + u);
+    const GlobalBytes kb = lane_address(a.k, lane + u);
+    const GlobalBytes vb = lane_address(a.v, lane + u);
 #pragma unroll
-    for (int i = 0; i < T::kLoads; ++i) s.k[u][i] = *reinterpret_cast<const u32x4*>(kb + k_lane + i * 64);
+    for (int i = 0; i < T::kLoads; ++i) s.k[u][i] = load_global<u32x4>(kb + k_lane + i * 64);
     const uint32_t vt = (uint32_t)p.v_s[1];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint8_t* at = vb + v_lane + j * vt;
-      if (T::kVW == 1) s.v[u][j][0] = *reinterpret_cast<const uint32_t*>(at);
+      const GlobalBytes at = vb + v_lane + j * vt;
+      if (T::kVW == 1) s.v[u][j][0] = load_global<uint32_t>(at);
       else if (T::kVW == 2) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(at);
+        const u32x2 w = load_global<u32x2>(at);
         s.v[u][j][0] = w.x;
         s.v[u][j][T::kVW > 1 ? 1 : 0] = w.y;
       } else {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(at);
+        const u32x4 w = load_global<u32x4>(at);
 #pragma unroll
         for (int e = 0; e < T::kVW; ++e) s.v[u][j][e] = u4_get(w, e);
       }

@@ -148,10 +148,17 @@ __device__ __forceinline__ Parts fetch_parts(const AttendParams& p, const Walk& 
 }
 
 __device__ __forceinline__ int lane_int(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
-__device__ __forceinline__ const uint8_t* lane_address(uint64_t x, int lane) {
+// An address that was a number is said to be global memory: a generic (flat) load
+// would count as an LDS access too, and every wait for LDS then wait for it.
+typedef const __attribute__((address_space(1))) uint8_t* GlobalBytes;
+template <typename T>
+__device__ __forceinline__ T load_global(GlobalBytes p) {
+  return *reinterpret_cast<const __attribute__((address_space(1))) T*>(p);
+}
+__device__ __forceinline__ GlobalBytes lane_address(uint64_t x, int lane) {
   const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, lane);
   const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(x >> 32), lane);
-  return reinterpret_cast<const uint8_t*>(((uint64_t)hi << 32) | lo);
+  return (GlobalBytes)(((uint64_t)hi << 32) | lo);
 }
 __device__ __forceinline__ float lane_float(float x, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
@@ -184,11 +191,11 @@ __device__ __forceinline__ void add_nonfinite(const AttendParams& p, const Reque
     for (int u = 0; u < group; ++u) {
       if (((a.ok >> u) & 1) == 0) continue;
       const int pos = lane_int(a.pos, u);
-      const uint8_t* vb = lane_address(a.v, u) + col * kEl;
+      const GlobalBytes vb = lane_address(a.v, u) + col * kEl;
       for (int t = 0; t < 16 && pos + t < rq.kv; ++t) {
         float v;
         if (FMT == KAMERA_CACHE_BF16) {
-          const uint32_t x = *reinterpret_cast<const uint16_t*>(vb + t * p.v_s[1]);
+          const uint32_t x = load_global<uint16_t>(vb + t * p.v_s[1]);
           if ((x & 0x7f80u) != 0x7f80u) continue;
           v = bf_lo(x);
         } else {

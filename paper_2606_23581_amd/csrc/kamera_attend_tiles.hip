@@ -76,20 +76,20 @@ __device__ __forceinline__ void load_tile(const Parts& a, int tile, int wave, ui
   for (int i = 0; i < S::KN; ++i) {
     // a wave's tokens of one load lie in one part
     const int u = lane0 + (wave * 64 + i * kTileThreads) / S::kRowLoads / 16;
-    s.k[i] = *reinterpret_cast<const u32x4*>(lane_address(a.k, u) + k_off);
+    s.k[i] = load_global<u32x4>(lane_address(a.k, u) + k_off);
     s.ks[i] = lane_float(a.ks, u);
   }
-  const uint8_t* vb = lane_address(a.v, lane0 + wave);
+  GlobalBytes vb = lane_address(a.v, lane0 + wave);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const uint8_t* at = vb + v_off;
-    if (S::VW == 1) s.v[j][0] = *reinterpret_cast<const uint32_t*>(at);
+    const GlobalBytes at = vb + v_off;
+    if (S::VW == 1) s.v[j][0] = load_global<uint32_t>(at);
     else if (S::VW == 2) {
-      const u32x2 x = *reinterpret_cast<const u32x2*>(at);
+      const u32x2 x = load_global<u32x2>(at);
       s.v[j][0] = x.x;
       s.v[j][S::VW > 1 ? 1 : 0] = x.y;
     } else {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(at);
+      const u32x4 x = load_global<u32x4>(at);
 #pragma unroll
       for (int e = 0; e < S::VW; ++e) s.v[j][e] = u4_get(x, e);
     }
