@@ -240,7 +240,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void attend_tiles_kernel(AttendPar
   }
 
   f32x16 o[DT];
-  float m = kLow, l = 0.f, lx = 0.f;
+  float m = kLow, l = 0.f, l1 = 0.f, lx = 0.f;
 #pragma unroll
   for (int b = 0; b < DT; ++b)
 #pragma unroll
@@ -344,15 +344,17 @@ __global__ __launch_bounds__(kTileThreads, 2) void attend_tiles_kernel(AttendPar
           for (int i = 0; i < 16; ++i) sc[u][i] = (bad >> (u * 2 + (i >> 3))) & 1 ? -INFINITY : sc[u][i];
       }
     }
-    float top = max2(sc[0][0], sc[1][0]);
+    float top = sc[0][0];                          // the first half's are there before the second's
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = max2(max2(top, sc[0][i]), sc[1][i]);
+    for (int i = 1; i < 31; i += 2) top = max2(max2(top, sc[i >> 4][i & 15]), sc[(i + 1) >> 4][(i + 1) & 15]);
+    top = max2(top, sc[1][15]);
     top *= p.scale2;
     if (__ballot(top > m + kSlack) != 0) {
       const float m_new = fmaxf(m, max_x32(top));
       const float down = exp2_fast(m - m_new);
       m = m_new;
       l *= down;
+      l1 *= down;
       lx *= down;
 #pragma unroll
       for (int b = 0; b < DT; ++b)
@@ -381,13 +383,15 @@ __global__ __launch_bounds__(kTileThreads, 2) void attend_tiles_kernel(AttendPar
       for (int s = 0; s < 2; ++s) {
         const u32x4 w = {pack_bf16x2(x[8 * s], x[8 * s + 1]), pack_bf16x2(x[8 * s + 2], x[8 * s + 3]),
                          pack_bf16x2(x[8 * s + 4], x[8 * s + 5]), pack_bf16x2(x[8 * s + 6], x[8 * s + 7])};
-        l = add_pair(w.w, add_pair(w.z, add_pair(w.y, add_pair(w.x, l))));
+        l = add_pair(w.y, add_pair(w.x, l));
+        l1 = add_pair(w.w, add_pair(w.z, l1));
         const bf16x8 pf = __builtin_bit_cast(bf16x8, w);
 #pragma unroll
         for (int b = 0; b < DT; ++b)
           o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[2 * u + s][b], pf, o[b], 0, 0, 0);
       }
     }
+    asm volatile("" : "+v"(l), "+v"(l1));         // or the sums sink behind the next tile's stores
     __builtin_amdgcn_s_setprio(0);
     bad = bad_next;
     if (tile + 1 < t_end) store(tile + 1, bad, lds + kOther);
@@ -398,7 +402,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void attend_tiles_kernel(AttendPar
     if (tile + 1 < t_end) step(std::integral_constant<int, 1>{}, tile + 1);
   }
 
-  l = sum_x32(l);
+  l = sum_x32(l + l1);
   if (LSE) lx = sum_x32(lx);
   if (row < row_end) {
     if (p.n_splits > 1) {
