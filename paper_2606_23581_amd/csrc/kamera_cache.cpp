@@ -494,7 +494,7 @@ int build_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& lau
   P.n_pool_pages = a->n_pool_pages;
   P.cache_type = a->cache_type;
   P.causal = a->causal;
-  P.window = a->window;
+  P.window = std::min(a->window, std::max(a->n_keys, 1));   // a longer one sees no more, and positions less it could wrap
   P.sel_stride = a->sel_stride;
   if (workspace > 0) {
     const int64_t parts = (int64_t)a->n_requests * a->n_kv_heads * P.rows_max * P.n_splits;

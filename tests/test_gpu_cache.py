@@ -445,6 +445,21 @@ def test_attend(name):
     assert int(status) == (km.STATUS_BAD_PAGE if c.get("bad") else 0)
 
 
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+@pytest.mark.parametrize("kv,nq", [([10, 3, 70], [16, 12, 16]), ([10, 70], [50, 90])])
+def test_attend_longest_window(cache, kv, nq):
+    """A window of the type's largest value is no window, also for queries before the first key."""
+    s = attend_case(dict(kv=kv, nq=nq, H=2, G=1 if max(nq) <= 16 else 4, cache=cache))
+    outs = []
+    for window in (0, 2 ** 31 - 1):
+        out = torch.full_like(s["q"], -7.0)
+        km.attend_paged(s["q"], s["kt"], s["vt"], out, i32(s["table"]), i32(kv), n_queries=s["n_max"], n_keys=max(kv),
+                        q_tokens=i32(nq), window=window, **s["scales"])
+        outs.append(out)
+    torch.cuda.synchronize()
+    assert torch.equal(*outs)
+
+
 POISON_CASES = {
     "spec": dict(kv=[40, 70], nq=[4, 6], H=2, G=2),
     "spec_bf16": dict(kv=[40, 70], nq=[4, 6], H=2, G=2, cache="bf16"),
