@@ -395,10 +395,11 @@ int size_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& laun
     wgs = bounded_product({pairs * P.deal, P.blocks_share, P.n_splits});
     P.n_shares = (int32_t)std::min<int64_t>(pairs * P.deal / 8, INT32_MAX);
   }
-  if (wgs < 0 || join < 0 || std::max(wgs, join) * 256 > 0xFFFFFFFFLL)
+  // rows count only where a second kernel joins them
+  if (wgs < 0 || wgs * 256 > 0xFFFFFFFFLL || (P.n_splits > 1 && (join < 0 || join * 256 > 0xFFFFFFFFLL)))
     return fail(KAMERA_ERR_RANGE, "%s: too many workgroups for one launch", who);
   P.n_tasks = (int32_t)wgs;
-  P.n_join = (int32_t)join;
+  P.n_join = P.n_splits > 1 ? (int32_t)join : 0;
   if (P.n_splits > 1) {
     workspace = bounded_product({join, P.n_splits, a->head_dim + 4, 4});
     if (workspace < 0) return fail(KAMERA_ERR_RANGE, "%s: workspace too large", who);

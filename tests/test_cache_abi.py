@@ -196,6 +196,9 @@ CASES = [
     (3, dict(workspace=0x21000000), km.ERR_ALIAS),
     (3, dict(lse=0x21000000), km.ERR_ALIAS),
     (3, dict(n_requests=1 << 28, n_splits=1), km.ERR_RANGE),
+    # 2^25 rows of long prompts in one part each; joined parts of as many are past one launch
+    (3, dict(n_queries=1 << 20, out=0x2000000000, k_cache=0x4000000000, v_cache=0x5000000000), km.OK),
+    (3, dict(n_queries=1 << 20, out=0x2000000000, k_cache=0x4000000000, v_cache=0x5000000000, n_splits=2), km.ERR_RANGE),
 ]
 
 
