@@ -136,15 +136,19 @@ def _workspace(a, need, workspace, device):
     return workspace
 
 
-def _launch_with_workspace(call, stream, given) -> None:
-    """Launches a call that may have a workspace of its own, which ends with it here."""
-    call.launch(stream)
-    if call.workspace is not None and given is None and stream is not None:
-        # the allocator learns that another stream than the current one uses the workspace
-        import torch
+def _launch_on(stream, prepare, a, kw) -> None:
+    """Prepares and launches a call that may have a workspace of its own: memory of the stream that it runs on,
+    which other work of the current stream may still use otherwise."""
+    if stream is None:
+        prepare(*a, **kw).launch()
+        return
+    import torch
 
-        s = torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
-        call.workspace.record_stream(s)
+    s = stream
+    if isinstance(stream, int):
+        s = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    with torch.cuda.stream(s):
+        prepare(*a, **kw).launch(s)
 
 
 def _is8(t):
@@ -313,7 +317,7 @@ def prepare_append_paged8(k, v, k_cache, v_cache, k_scale, v_scale, page_table, 
 
 def select_pages(*a, stream=None, **kw) -> None:
     """``kamera_select_pages``; see ``prepare_select_pages`` for the arguments."""
-    _launch_with_workspace(prepare_select_pages(*a, **kw), stream, kw.get("workspace"))
+    _launch_on(stream, prepare_select_pages, a, kw)
 
 
 def prepare_select_pages(q, k_sum, k_sum_scale, page_table, kv_tokens, sel, sel_count, *, n_keys: int,
@@ -361,7 +365,7 @@ def prepare_select_pages(q, k_sum, k_sum_scale, page_table, kv_tokens, sel, sel_
 
 def attend_paged(*a, stream=None, **kw) -> None:
     """``kamera_attend_paged``; see ``prepare_attend_paged`` for the arguments."""
-    _launch_with_workspace(prepare_attend_paged(*a, **kw), stream, kw.get("workspace"))
+    _launch_on(stream, prepare_attend_paged, a, kw)
 
 
 def attend_workspace(prepared: Prepared) -> int:
@@ -384,7 +388,8 @@ def prepare_attend_paged(q, k_cache, v_cache, out, page_table, kv_tokens, *, n_q
     scale: of the scores, default D ** -0.5.  window > 0: only the last `window` keys up to a query's own.
     sel, sel_count: int32 [R, H, keep] and [R, H] from ``select_pages``, for one query token a request.
     lse: fp32 [rows, heads], receives the log of the softmax sums.  workspace: device bytes for split work;
-    allocated with the call where None, and then its own for as long as the prepared call lives.
+    allocated with the call where None, and then its own for as long as the prepared call lives (memory of the
+    stream that is current then, on which other streams wait before its first launch there).
     """
     import torch
 

@@ -797,6 +797,28 @@ def test_calls_on_a_given_stream():
         assert float((out.float() - want.float()).abs().max()) <= 2.0 ** -6
 
 
+@pytest.mark.parametrize("raw", ["object", "raw", "null"])
+def test_own_workspace_is_memory_of_the_given_stream(raw, monkeypatch):
+    """Memory of another stream may still be read there when this call writes it."""
+    s = attend_case(dict(kv=[3000, 700], H=2, G=4))
+    table, kv, out = i32(s["table"]), i32(s["kv"]), torch.zeros_like(s["q"])
+    side = torch.cuda.default_stream() if raw == "null" else torch.cuda.Stream()
+    torch.cuda.synchronize()
+    taken, empty = [], torch.empty
+
+    def seen(*a, **kw):
+        taken.append(torch.cuda.current_stream().cuda_stream)
+        return empty(*a, **kw)
+
+    monkeypatch.setattr(torch, "empty", seen)
+    km.attend_paged(s["q"], s["kt"], s["vt"], out, table, kv, n_queries=1, n_keys=3000, n_splits=4,
+                    stream=side if raw == "object" else side.cuda_stream, **s["scales"])
+    monkeypatch.undo()
+    torch.cuda.synchronize()
+    assert taken == [side.cuda_stream]
+    check_attend(out, None, s, 128 ** -0.5)
+
+
 @pytest.mark.parametrize("cache", ["e4m3", "bf16"])
 @pytest.mark.parametrize("queries", [1, 3, 40])
 def test_a_query_that_is_not_finite_stays_in_its_row(cache, queries):
