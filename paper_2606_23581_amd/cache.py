@@ -100,8 +100,13 @@ def _typed(t, dtype, name, shape=None, contiguous=True):
     return t
 
 
-def _table(page_table, n):
-    """The row stride of an int32 [n, pages] table whose rows are dense."""
+def _table(page_table, n, tokens=None, page_size=1):
+    """The row stride of an int32 [n, pages] table whose rows are dense.
+
+    The library takes the stride for the pages of a row.  Where that is more than the rows of this view hold, a
+    call says how many tokens a request has at most, and none of the rest is looked up; a call that cannot say
+    (tokens None) needs the rest of the last row to be there too.
+    """
     _i32_dev(page_table, "page_table")
     shape = page_table.shape
     if len(shape) != 2 or shape[0] != n:
@@ -109,7 +114,15 @@ def _table(page_table, n):
     s0, s1 = page_table.stride()
     if s1 != 1 and shape[1] > 1 and n > 0:
         raise ValueError("the rows of page_table must be contiguous")
-    return s0 if n > 1 else max(shape[1], 1)
+    if n <= 1:
+        return max(shape[1], 1)
+    if s0 > shape[1]:
+        if tokens is not None and tokens > shape[1] * page_size:
+            raise ValueError(f"the {shape[1]} pages of a row of page_table hold less than {tokens} tokens")
+        there = page_table.untyped_storage().nbytes() // 4 - page_table.storage_offset()
+        if tokens is None and n * s0 > there:
+            raise ValueError("the rows of page_table must be whole")
+    return s0
 
 
 def _device(*tensors):
@@ -348,7 +361,8 @@ def prepare_select_pages(q, k_sum, k_sum_scale, page_table, kv_tokens, sel, sel_
     _device(q, k_sum, k_sum_scale, page_table, kv_tokens, sel, sel_count, workspace, status)
     a = CSelectArgs()
     a.n_requests, a.n_q_heads, a.n_kv_heads, a.head_dim, a.n_keys = R, HQ, H, D, int(n_keys)
-    a.page_size, a.pt_stride, a.n_pool_pages = int(page_size), _table(page_table, R), n_pages
+    a.page_size, a.n_pool_pages = int(page_size), n_pages
+    a.pt_stride = _table(page_table, R, int(n_keys), int(page_size))
     a.kv_tokens, a.page_table, a.q = _ptr(kv_tokens), _ptr(page_table), _ptr(q)
     a.q_stride[0:2] = q.stride()[:2]
     a.k_sum, a.k_sum_scale = _ptr(k_sum), _ptr(k_sum_scale)
@@ -419,7 +433,9 @@ def prepare_attend_paged(q, k_cache, v_cache, out, page_table, kv_tokens, *, n_q
     _typed(status, torch.int32, "status")
     a = CAttendArgs()
     a.n_requests, a.n_q_heads, a.n_kv_heads, a.head_dim, a.n_queries, a.n_keys = R, HQ, H, D, n_queries, int(n_keys)
-    a.page_size, a.pt_stride, a.n_pool_pages = page_size, _table(page_table, R), n_pages
+    a.page_size, a.n_pool_pages = page_size, n_pages
+    # selected pages are whatever sel holds
+    a.pt_stride = _table(page_table, R, int(n_keys) if sel is None else None, page_size)
     a.cache_type = CACHE_E4M3 if eight else CACHE_BF16
     a.causal, a.window, a.n_splits = int(causal), int(window), int(n_splits)
     a.scale = D ** -0.5 if scale is None else float(scale)

@@ -14,6 +14,7 @@ import pytest
 import torch
 
 import paper_2606_23581_amd as km
+from paper_2606_23581_amd import cache
 from tests import cache_ref as ref
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -277,6 +278,22 @@ def test_binding_refuses():
     with pytest.raises(TypeError):
         km.prepare_select_pages(q, cache[:, 0], scale, table, kv, torch.zeros((2, 2, 4), dtype=i4),
                                 torch.zeros((2, 2), dtype=i4), n_keys=32, page_size=16)
+
+
+def test_binding_takes_views_of_page_tables():
+    """Rows with a stride: what a call may look up has to be there."""
+    i4 = torch.int32
+    whole = torch.zeros((3, 20), dtype=i4)
+    for view, tokens, ok in ((whole, None, True), (whole[:, :8], 128, True), (whole[:, 12:], 128, True),
+                             (whole[:, 12:], 129, False), (whole[:, :8], 129, False), (whole[:, :8], None, True),
+                             (whole[:, 12:], None, False), (whole[1:, 12:], None, False), (whole[:2, 12:], None, True),
+                             (whole[:1, 12:], None, True)):
+        n = view.shape[0]
+        if ok:
+            assert cache._table(view, n, tokens, 16) == (20 if n > 1 else view.shape[1])
+        else:
+            with pytest.raises(ValueError):
+                cache._table(view, n, tokens, 16)
 
 
 def test_reference_e4m3_agrees_with_torch():
