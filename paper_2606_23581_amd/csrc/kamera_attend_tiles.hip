@@ -25,8 +25,8 @@
 // Bound by the softmax's vector instructions beside the matrix pipe: 64 keys cost a
 // wave 1024 cycles of MFMA and about as many of exponentials, maxima and
 // conversions, which two waves a SIMD (two workgroups a CU) overlap in part.  1024
-// queries of 8 x 8 heads over 16384 keys in 8 bits: 507 us, 1050 TFLOP/s (at 531 us
-// the matrix pipe was busy 43%).  64 rows a wave, one wave a SIMD: 522 against 755
+// queries of 8 x 8 heads over 16384 keys in 8 bits: 507 us, 1050 TFLOP/s, matrix pipe
+// busy 46%.  64 rows a wave, one wave a SIMD: 522 against 755
 // TFLOP/s in an earlier form, for want of a second wave to overlap with.
 
 #include <algorithm>
@@ -194,7 +194,12 @@ __global__ __launch_bounds__(kTileThreads, 2) void attend_tiles_kernel(AttendPar
   w = d;
   d = fast_div(w, p.fd_splits);
   const int split = (int)(w - d * p.n_splits);
-  const int rb = (p.blocks_share - 1 - (int)d) * p.deal + (int)(share - pair * p.deal);
+  // which of `deal` neighbouring blocks an XCD takes turns from pair to pair and split to
+  // split too, or where the blocks are no multiple of `deal` the same XCDs would go without
+  // (37 requests of 3 queries of 16 heads over one bf16 KV head, up to 10040 keys: one XCD
+  // had all the work, 222 us, now 72)
+  const int rb = (p.blocks_share - 1 - (int)d) * p.deal +
+                 (int)((share - pair * p.deal + local + (uint32_t)split) & (uint32_t)(p.deal - 1));
   d = fast_div(pair, p.fd_heads);
   const int h = (int)(pair - d * p.n_kv_heads), r = (int)d;
   if (rb >= p.n_row_blocks) return;
