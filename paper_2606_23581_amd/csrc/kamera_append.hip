@@ -24,8 +24,6 @@ namespace {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kAppThreads = 256;
-
 __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
   typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
   const u16x2 x = __builtin_bit_cast(u16x2, a), y = __builtin_bit_cast(u16x2, b);
@@ -57,12 +55,12 @@ __device__ __forceinline__ void from_e4m3(u32x2 w, float (&f)[8]) {
 
 // D columns, SUB 16-token parts (and waves) a page.  A row takes D / 8 lanes of 8 columns.
 template <int D, int SUB>
-__global__ __launch_bounds__(kAppThreads) void append_kernel(AppendParams) {
+__global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendParams) {
   constexpr int LPR = D / 8;                       // lanes a row
   constexpr int TPI = 64 / LPR;                    // tokens a step of the wave
   constexpr int IT = 16 / TPI;                     // steps
   constexpr int P = SUB * 16;
-  constexpr int kWaves = kAppThreads / 64, kUnits = kWaves / SUB;
+  constexpr int kWaves = kAppendThreads / 64, kUnits = kWaves / SUB;
   const AppendParams& p = kernel_params<AppendParams>();
   __shared__ uint32_t s_top[kWaves];
   __shared__ float s_sum[SUB > 1 ? kWaves : 1][D];
@@ -238,8 +236,8 @@ __global__ __launch_bounds__(kAppThreads) void append_kernel(AppendParams) {
 }
 
 hipError_t launch_append(const AppendParams& p, hipStream_t s) {
-  const int per = kAppThreads / 64 / (p.page_size / 16);   // units a workgroup
-  const dim3 grid((uint32_t)((p.n_units + per - 1) / per)), block(kAppThreads);
+  const int per = append_units_wg(p.page_size);
+  const dim3 grid((uint32_t)((p.n_units + per - 1) / per)), block(kAppendThreads);
 #define KAMERA_APPEND(D, SUB) hipLaunchKernelGGL((append_kernel<D, SUB>), grid, block, 0, s, p)
   if (p.head_dim == 128) {
     switch (p.page_size) {

@@ -158,7 +158,7 @@ int build_append(const kamera_append_args* a, kamera::AppendParams& P, bool& lau
   // the page that holds the first new token may hold page_size - 1 others
   const int64_t pages = ((int64_t)a->n_tokens + a->page_size - 2) / a->page_size + 1;
   const int64_t units = bounded_product({a->n_chunks, a->n_layers, a->n_heads, 2, pages});
-  if (units < 0 || units > (int64_t)0xFFFFFFFF / 64 - 8)
+  if (units < 0 || ceil_div(units, kamera::append_units_wg(a->page_size)) * kamera::kAppendThreads > 0xFFFFFFFFLL)
     return fail(KAMERA_ERR_RANGE, "%s: too many (chunk, layer, page, head) units for one launch", who);
   const int64_t ext[4] = {a->n_layers, a->n_pool_pages, a->page_size, a->n_heads};
   const int64_t ext_s[3] = {a->n_layers, a->n_pool_pages, a->n_heads};

@@ -10,6 +10,8 @@
 
 namespace kamera {
 
+constexpr int kAppendThreads = 256;              // a workgroup of the append: a wave for each 16 tokens of a page
+constexpr int append_units_wg(int page_size) { return kAppendThreads / 64 / (page_size / 16); }
 constexpr int kMinExp = -100, kMaxExp = 120;     // exponents of the 8-bit cache's scales
 
 struct TablesParams {
@@ -50,7 +52,7 @@ struct AppendParams {
   uint32_t* status;
   int32_t n_chunks, n_layers, n_heads, n_tokens;
   int32_t head_dim, page_size, pt_stride, n_pool_pages;
-  int32_t n_units;                   // (chunk, layer, page of the chunk, plane, head): one wave each
+  int32_t n_units;                   // (chunk, layer, page of the chunk, plane, head): page_size / 16 waves each
   int32_t pages;                     // most pages that a chunk's new tokens touch
   FastDiv fd_heads, fd_pages, fd_layers;
 };

@@ -210,6 +210,21 @@ def test_validation(which, change, code):
     assert (km.last_error() == "") == (code == km.OK)
 
 
+@pytest.mark.parametrize("page_size,units_a_workgroup", [(16, 4), (32, 2), (64, 1)])
+def test_append_fits_one_launch(page_size, units_a_workgroup):
+    """A page of 64 tokens takes the four waves of a workgroup, one of 16 tokens one of them: a launch has at most
+    2^32 - 1 work-items, 256 a workgroup.  One token a chunk, one head: two units a chunk (keys, values)."""
+    most = ((1 << 32) - 1) // 256 * units_a_workgroup // 2
+    for n, code in ((most, km.OK), (most + 1, km.ERR_RANGE)):
+        a = append_args(n_chunks=n, n_layers=1, n_heads=1, n_tokens=1, page_size=page_size, k_stride=(0,), v_stride=(0,))
+        assert km.lib().kamera_validate_cache(1, ctypes.byref(a)) == code, km.last_error()
+    # a batch of ragged prompts of which only the longest is known on the host
+    a = append_args(n_chunks=256, n_layers=80, n_heads=8, n_tokens=8192, page_size=page_size, pt_stride=512)
+    for f in (a.k_stride, a.v_stride, a.k_cache_stride, a.v_cache_stride):
+        strides(f, (0, 0))
+    assert km.lib().kamera_validate_cache(1, ctypes.byref(a)) == km.ERR_RANGE
+
+
 def test_validation_of_nothing():
     L = km.lib()
     for which in range(4):
