@@ -487,7 +487,8 @@ typedef struct {
  * is larger, and is otherwise brought to the new one (bytes rounded to
  * nearest even where they leave the normal range).  Elements are rounded to
  * the nearest e4m3 value, ties to even; infinities and NaN are stored as NaN
- * and take no part in e.  Slots past the last token are not written.
+ * and take no part in e.  Slots past the last token are not written.  Tokens
+ * past the pages of a row (pt_pages) are left out (KAMERA_STATUS_BAD_LENGTH).
  *
  * k_sum (with k_sum_scale; both or neither): when a page is filled, the sum
  * of its page_size keys, column by column, as int8 with one power-of-two
@@ -509,7 +510,8 @@ typedef struct {
   const int32_t* chunk_tokens;   /* device [n_chunks], or NULL                 */
   const int32_t* tokens_before;  /* device [n_chunks], or NULL                 */
   const int32_t* row_base;       /* device [n_chunks], or NULL                 */
-  const int32_t* page_table;     /* device [n_chunks][pt_stride]               */
+  const int32_t* page_table;     /* device [n_chunks][pt_stride], pt_pages of  */
+                                 /*   each row in use                          */
   const void* k;
   int64_t k_stride[4];           /* chunk, layer, row, head                    */
   const void* v;
@@ -527,6 +529,7 @@ typedef struct {
   float* k_sum_scale;
   int64_t k_sum_scale_stride[3];
   uint32_t* status;
+  int32_t pt_pages;              /* entries of a page-table row (0: pt_stride) */
 } kamera_append_args;
 
 /* kamera_select_pages -- for one query token a request and every KV head, the
@@ -597,7 +600,8 @@ typedef enum {
  * sel (optional; n_queries must be 1): only the pages sel[r][h][0 ..
  * sel_count[r][h]) (indices into the page-table row, as kamera_select_pages
  * writes them) are read.
- * Keys in pages whose number is outside the pool are not seen (and flagged).
+ * Keys in pages whose number is outside the pool are not seen (and flagged),
+ * nor are selected pages past the pages of a row (pt_pages).
  *
  * Work is split over the keys where there are few rows: n_splits parts a row
  * (0: chosen from the sizes), joined by a second kernel on the same stream.
@@ -623,7 +627,8 @@ typedef struct {
   const int32_t* q_tokens;       /* device [n_requests], or NULL               */
   const int32_t* q_base;         /* device [n_requests], or NULL               */
   const int32_t* kv_tokens;      /* device [n_requests], at most n_keys        */
-  const int32_t* page_table;     /* device [n_requests][pt_stride]             */
+  const int32_t* page_table;     /* device [n_requests][pt_stride], pt_pages   */
+                                 /*   of each row in use                       */
   const void* q;                 /* bf16                                       */
   int64_t q_stride[2];           /* row, head                                  */
   void* out;                     /* bf16                                       */
@@ -641,6 +646,7 @@ typedef struct {
   const int32_t* sel;            /* optional: device [n_requests][n_kv_heads]  */
   const int32_t* sel_count;      /*   [sel_stride], and their counts           */
   int32_t sel_stride;
+  int32_t pt_pages;              /* entries of a page-table row (0: pt_stride) */
   void* workspace;
   int64_t workspace_bytes;
   uint32_t* status;

@@ -43,7 +43,7 @@ class CAppendArgs(ctypes.Structure):
                 ("v", _vp), ("v_stride", _i64 * 4), ("k_cache", _vp), ("k_cache_stride", _i64 * 4), ("v_cache", _vp),
                 ("v_cache_stride", _i64 * 4), ("k_scale", _vp), ("k_scale_stride", _i64 * 3), ("v_scale", _vp),
                 ("v_scale_stride", _i64 * 3), ("k_sum", _vp), ("k_sum_stride", _i64 * 3), ("k_sum_scale", _vp),
-                ("k_sum_scale_stride", _i64 * 3), ("status", _vp)]
+                ("k_sum_scale_stride", _i64 * 3), ("status", _vp), ("pt_pages", _i32)]
 
 
 class CSelectArgs(ctypes.Structure):
@@ -64,7 +64,7 @@ class CAttendArgs(ctypes.Structure):
                 ("lse", _vp), ("lse_stride", _i64 * 2), ("k_cache", _vp), ("k_cache_stride", _i64 * 3),
                 ("v_cache", _vp), ("v_cache_stride", _i64 * 3), ("k_scale", _vp), ("k_scale_stride", _i64 * 2),
                 ("v_scale", _vp), ("v_scale_stride", _i64 * 2), ("sel", _vp), ("sel_count", _vp), ("sel_stride", _i32),
-                ("workspace", _vp), ("workspace_bytes", _i64), ("status", _vp)]
+                ("pt_pages", _i32), ("workspace", _vp), ("workspace_bytes", _i64), ("status", _vp)]
 
 
 STRUCTS = {6: CPageTablesArgs, 7: CAppendArgs, 8: CSelectArgs, 9: CAttendArgs}
@@ -103,8 +103,8 @@ def _typed(t, dtype, name, shape=None, contiguous=True):
 def _table(page_table, n, tokens=None, page_size=1):
     """The row stride of an int32 [n, pages] table whose rows are dense.
 
-    The library takes the stride for the pages of a row.  Where that is more than the rows of this view hold, a
-    call says how many tokens a request has at most, and none of the rest is looked up; a call that cannot say
+    Where that is more than the rows of this view hold, a call says how many tokens a request has at most, and none
+    of the rest is looked up (0 where the library is told the pages of a row itself); a call that cannot say
     (tokens None) needs the rest of the last row to be there too.
     """
     _i32_dev(page_table, "page_table")
@@ -308,7 +308,9 @@ def prepare_append_paged8(k, v, k_cache, v_cache, k_scale, v_scale, page_table, 
     _device(k, v, k_cache, v_cache, k_scale, v_scale, page_table, tokens_before, chunk_tokens, row_base, k_sum,
             k_sum_scale, status)
     a.n_chunks, a.n_layers, a.n_heads, a.head_dim, a.n_tokens = C, Ln, H, D, n
-    a.page_size, a.pt_stride, a.n_pool_pages = page_size, _table(page_table, C), n_pages
+    # chunks may outgrow the rows of a view: they end where the view does
+    a.page_size, a.pt_stride, a.n_pool_pages = page_size, _table(page_table, C, 0), n_pages
+    a.pt_pages = page_table.shape[1]
     a.chunk_tokens, a.tokens_before, a.row_base = _ptr(chunk_tokens), _ptr(tokens_before), _ptr(row_base)
     a.page_table, a.k, a.v = _ptr(page_table), _ptr(k), _ptr(v)
     a.k_cache, a.v_cache, a.k_scale, a.v_scale = _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale)
@@ -434,8 +436,9 @@ def prepare_attend_paged(q, k_cache, v_cache, out, page_table, kv_tokens, *, n_q
     a = CAttendArgs()
     a.n_requests, a.n_q_heads, a.n_kv_heads, a.head_dim, a.n_queries, a.n_keys = R, HQ, H, D, n_queries, int(n_keys)
     a.page_size, a.n_pool_pages = page_size, n_pages
-    # selected pages are whatever sel holds
-    a.pt_stride = _table(page_table, R, int(n_keys) if sel is None else None, page_size)
+    # selected pages are whatever sel holds: one past the rows of a view is not seen
+    a.pt_stride = _table(page_table, R, int(n_keys) if sel is None else 0, page_size)
+    a.pt_pages = page_table.shape[1]
     a.cache_type = CACHE_E4M3 if eight else CACHE_BF16
     a.causal, a.window, a.n_splits = int(causal), int(window), int(n_splits)
     a.scale = D ** -0.5 if scale is None else float(scale)

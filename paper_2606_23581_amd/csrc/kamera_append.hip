@@ -90,10 +90,10 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(AppendParams) {
   if (SUB == 1 && !live) return;
   const int lo = (int)lo64, hi = (int)hi64;        // new tokens of the page: [lo, hi)
   int page = -1;
-  if (live && j < p.pt_stride) page = uniform_load(p.page_table + (int64_t)c * p.pt_stride + j);
+  if (live && j < p.pt_pages) page = uniform_load(p.page_table + (int64_t)c * p.pt_stride + j);
   if (live && (page < 0 || page >= p.n_pool_pages)) {
     if (lane == 0 && p.status != nullptr)
-      atomicOr(p.status, j < p.pt_stride ? KAMERA_STATUS_BAD_PAGE : KAMERA_STATUS_BAD_LENGTH);
+      atomicOr(p.status, j < p.pt_pages ? KAMERA_STATUS_BAD_PAGE : KAMERA_STATUS_BAD_LENGTH);
     live = false;
   }
   if (SUB == 1 && !live) return;

@@ -131,7 +131,7 @@ __device__ __forceinline__ Parts fetch_parts(const AttendParams& p, const Walk& 
       idx = w.sel[k];
       a.pos = (int)((uint32_t)idx * (uint32_t)p.page_size) + in_page;
     }
-    if (idx >= 0 && idx < p.pt_stride) page = w.table[idx];
+    if (idx >= 0 && idx < p.pt_pages) page = w.table[idx];
   }
   const bool ok = page >= 0 && page < p.n_pool_pages;
   a.ok = __ballot(ok);

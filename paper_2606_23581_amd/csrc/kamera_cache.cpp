@@ -51,14 +51,23 @@ int check_heads(int32_t q_heads, int32_t kv_heads, const char* who) {
   return KAMERA_OK;
 }
 
-int check_table(const int32_t* table, int32_t pt_stride, int32_t page_size, int32_t n_pool_pages, int64_t tokens,
-                const char* who) {
+// `pages`: the entries of a row.
+int check_table(const int32_t* table, int32_t pt_stride, int32_t pages, int32_t page_size, int32_t n_pool_pages,
+                int64_t tokens, const char* who) {
   if (table == nullptr) return fail(KAMERA_ERR_NULL, "%s: page_table is NULL", who);
   if (n_pool_pages <= 0) return fail(KAMERA_ERR_SHAPE, "%s: n_pool_pages must be positive", who);
-  if (pt_stride < ceil_div(tokens, page_size))
-    return fail(KAMERA_ERR_SHAPE, "%s: pt_stride %d < %lld pages needed for %lld tokens", who, pt_stride,
-                (long long)ceil_div(tokens, page_size), (long long)tokens);
+  if (pt_stride < 0 || pages < ceil_div(tokens, page_size))
+    return fail(KAMERA_ERR_SHAPE, "%s: %d pages a row (stride %d) < %lld pages needed for %lld tokens", who, pages,
+                pt_stride, (long long)ceil_div(tokens, page_size), (long long)tokens);
   return KAMERA_OK;
+}
+
+// Entries that a row of a page table has.
+int32_t row_pages(int32_t pt_stride, int32_t pt_pages) { return pt_pages != 0 ? pt_pages : pt_stride; }
+
+// Bytes of a table of n rows.
+Range table_range(const int32_t* table, int64_t n, int32_t pt_stride, int32_t pages) {
+  return flat(table, n > 0 && pages > 0 ? (n - 1) * pt_stride + pages : 0, 4);
 }
 
 int check_workspace(const void* workspace, int64_t bytes, int64_t needed, const char* who) {
@@ -142,7 +151,8 @@ int build_append(const kamera_append_args* a, kamera::AppendParams& P, bool& lau
   if (rc) return rc;
   if ((rc = check_page8(a->page_size, who))) return rc;
   if (a->n_chunks == 0 || a->n_layers == 0 || a->n_heads == 0 || a->n_tokens == 0) return KAMERA_OK;
-  if ((rc = check_table(a->page_table, a->pt_stride, a->page_size, a->n_pool_pages, a->n_tokens, who))) return rc;
+  const int32_t row = row_pages(a->pt_stride, a->pt_pages);
+  if ((rc = check_table(a->page_table, a->pt_stride, row, a->page_size, a->n_pool_pages, a->n_tokens, who))) return rc;
   if (a->k == nullptr || a->v == nullptr || a->k_cache == nullptr || a->v_cache == nullptr || a->k_scale == nullptr ||
       a->v_scale == nullptr)
     return fail(KAMERA_ERR_NULL, "%s: k, v, their caches and scales are needed", who);
@@ -213,6 +223,7 @@ int build_append(const kamera_append_args* a, kamera::AppendParams& P, bool& lau
   P.head_dim = a->head_dim;
   P.page_size = a->page_size;
   P.pt_stride = a->pt_stride;
+  P.pt_pages = row;
   P.n_pool_pages = a->n_pool_pages;
   P.n_units = (int32_t)units;
   P.pages = (int32_t)pages;
@@ -265,7 +276,8 @@ int build_select(const kamera_select_args* a, kamera::SelectParams& P, bool& lau
   launch = false;
   int rc = size_select(a, work, n_pieces, workspace);
   if (rc || !work) return rc;
-  if ((rc = check_table(a->page_table, a->pt_stride, a->page_size, a->n_pool_pages, a->n_keys, who))) return rc;
+  if ((rc = check_table(a->page_table, a->pt_stride, a->pt_stride, a->page_size, a->n_pool_pages, a->n_keys, who)))
+    return rc;
   if (a->kv_tokens == nullptr || a->q == nullptr || a->k_sum == nullptr || a->k_sum_scale == nullptr ||
       a->sel == nullptr || a->sel_count == nullptr)
     return fail(KAMERA_ERR_NULL, "%s: kv_tokens, q, k_sum, k_sum_scale, sel and sel_count are needed", who);
@@ -280,7 +292,7 @@ int build_select(const kamera_select_args* a, kamera::SelectParams& P, bool& lau
       !span(a->k_sum, a->k_sum_stride, ext_s, 2, a->head_dim, 1, in[1].lo, in[1].hi) ||
       !span(a->k_sum_scale, a->k_sum_scale_stride, ext_s, 2, 1, 4, in[2].lo, in[2].hi))
     return fail(KAMERA_ERR_RANGE, "%s: strides span more than the address space", who);
-  in[3] = flat(a->page_table, (int64_t)a->n_requests * a->pt_stride, 4);
+  in[3] = table_range(a->page_table, a->n_requests, a->pt_stride, (int32_t)ceil_div(a->n_keys, a->page_size));
   in[4] = flat(a->kv_tokens, a->n_requests, 4);
   Range out[3] = {flat(a->sel, entries, 4), flat(a->sel_count, wgs, 4), {0, 0}};
   if (workspace > 0) {
@@ -415,7 +427,10 @@ int build_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& lau
   if (rc || !launch) return rc;
   launch = false;
   const bool e4m3 = a->cache_type == KAMERA_CACHE_E4M3;
-  if ((rc = check_table(a->page_table, a->pt_stride, a->page_size, a->n_pool_pages, a->n_keys, who))) return rc;
+  const int32_t row = row_pages(a->pt_stride, a->pt_pages);
+  // selected pages are whatever sel holds: one past the row is not seen
+  const int64_t tokens = a->sel_stride > 0 ? 0 : a->n_keys;
+  if ((rc = check_table(a->page_table, a->pt_stride, row, a->page_size, a->n_pool_pages, tokens, who))) return rc;
   if (a->kv_tokens == nullptr || a->q == nullptr || a->out == nullptr || a->k_cache == nullptr || a->v_cache == nullptr)
     return fail(KAMERA_ERR_NULL, "%s: kv_tokens, q, out and the caches are needed", who);
   if (e4m3 && (a->k_scale == nullptr || a->v_scale == nullptr))
@@ -444,7 +459,7 @@ int build_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& lau
       (e4m3 && (!span(a->k_scale, a->k_scale_stride, ext_s, 2, 1, 4, in[3].lo, in[3].hi) ||
                 !span(a->v_scale, a->v_scale_stride, ext_s, 2, 1, 4, in[4].lo, in[4].hi))))
     return fail(KAMERA_ERR_RANGE, "%s: strides span more than the address space", who);
-  in[5] = flat(a->page_table, (int64_t)a->n_requests * a->pt_stride, 4);
+  in[5] = table_range(a->page_table, a->n_requests, a->pt_stride, row);
   if (workspace > 0) {
     if ((rc = check_workspace(a->workspace, a->workspace_bytes, workspace, who))) return rc;
     out[2] = flat(a->workspace, workspace, 1);
@@ -492,6 +507,7 @@ int build_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& lau
   P.n_keys = a->n_keys;
   P.page_size = a->page_size;
   P.pt_stride = a->pt_stride;
+  P.pt_pages = row;
   P.n_pool_pages = a->n_pool_pages;
   P.cache_type = a->cache_type;
   P.causal = a->causal;

@@ -52,6 +52,7 @@ struct AppendParams {
   uint32_t* status;
   int32_t n_chunks, n_layers, n_heads, n_tokens;
   int32_t head_dim, page_size, pt_stride, n_pool_pages;
+  int32_t pt_pages;                  // entries of a table row
   int32_t n_units;                   // (chunk, layer, page of the chunk, plane, head): page_size / 16 waves each
   int32_t pages;                     // most pages that a chunk's new tokens touch
   FastDiv fd_heads, fd_pages, fd_layers;
@@ -100,6 +101,7 @@ struct AttendParams {
   uint32_t q_sign;                   // 0x80008000 where the scale is negative: q's signs are turned
   int32_t n_requests, n_kv_heads, group, head_dim;
   int32_t n_queries, n_keys, page_size, pt_stride, n_pool_pages;
+  int32_t pt_pages;                  // entries of a table row
   int32_t cache_type, causal, window, sel_stride;
   int32_t n_splits;
   int32_t rows_max;                  // n_queries * group: rows of one (request, KV head)

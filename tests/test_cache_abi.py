@@ -311,6 +311,42 @@ def test_binding_takes_views_of_page_tables():
                 cache._table(view, n, tokens, 16)
 
 
+@pytest.mark.parametrize("which,change,code", [
+    (1, dict(pt_stride=20, pt_pages=3), km.OK),
+    (1, dict(pt_stride=20, pt_pages=2), km.ERR_SHAPE),
+    (1, dict(pt_stride=20, pt_pages=-1), km.ERR_SHAPE),
+    (3, dict(pt_stride=500, pt_pages=256), km.OK),
+    (3, dict(pt_stride=500, pt_pages=255), km.ERR_SHAPE),
+    (3, dict(pt_stride=500, pt_pages=-1), km.ERR_SHAPE),
+    # selected pages are whatever sel holds
+    (3, dict(pt_stride=500, pt_pages=8, sel=P, sel_count=P, sel_stride=8), km.OK),
+    # the last row ends with its own pages: what lies behind them is not the table's
+    (1, dict(pt_stride=20, pt_pages=3, page_table=0x30000000 - 4 * 23), km.OK),
+    (3, dict(pt_stride=500, pt_pages=256, page_table=0x21000000 - 4 * 756), km.OK),
+])
+def test_rows_of_a_page_table_narrower_than_their_stride(which, change, code):
+    a = MAKE[which](**change)
+    assert km.lib().kamera_validate_cache(which, ctypes.byref(a)) == code, km.last_error()
+
+
+def test_views_of_page_tables_end_where_the_view_does(monkeypatch):
+    """A call is told the pages of its view, not those of the tensor behind it."""
+    monkeypatch.setattr(cache, "_device", lambda *t: None)
+    whole = torch.zeros((3, 20), dtype=torch.int32)
+    rows = torch.zeros((3, 1, 24, 2, 128), dtype=torch.bfloat16)
+    planes = [torch.zeros((1, 4, 16, 2, 128), dtype=torch.uint8) for _ in range(2)]
+    scales = [torch.ones((1, 4, 2)) for _ in range(2)]
+    q = torch.zeros((3, 8, 128), dtype=torch.bfloat16)
+    kv, sel = torch.zeros(3, dtype=torch.int32), torch.zeros((3, 2, 2), dtype=torch.int32)
+    for view in (whole[:, :2], whole[:, 18:], whole[:, 5:9], whole):
+        a = km.prepare_append_paged8(rows, rows, *planes, *scales, view).args
+        assert (a.pt_stride, a.pt_pages) == (20, view.shape[1])
+        for kw in (dict(sel=sel, sel_count=sel[:, :, 0].contiguous()), {}):
+            a = km.prepare_attend_paged(q, planes[0][0], planes[1][0], torch.zeros_like(q), view, kv, n_queries=1,
+                                        n_keys=32, k_scale=scales[0][0], v_scale=scales[1][0], **kw).args
+            assert (a.pt_stride, a.pt_pages) == (20, view.shape[1])
+
+
 def test_reference_e4m3_agrees_with_torch():
     """The tests' own e4m3 rounding against torch's cast, at every value, midpoint and many others."""
     pos = ref.e4m3_values()[:127]

@@ -212,6 +212,32 @@ def test_append(name):
     assert int(status) == (km.STATUS_BAD_PAGE if c.get("bad") else km.STATUS_BAD_LENGTH if c.get("cut") else 0)
 
 
+@pytest.mark.parametrize("first", [0, 3, 6])
+def test_append_ends_where_a_view_of_the_table_does(first):
+    """Two columns of a wider table: chunks that outgrow them are cut and flagged, as with a copy of the columns,
+    and no page that only the other columns name is written."""
+    rng = np.random.default_rng(23)
+    before, tokens, page, H, D = [20, 5, 10], [32, 30, 6], 16, 2, 128
+    pool = 3 * 8 + 1
+    whole = i32(rng.permutation(pool)[:24].reshape(3, 8))
+    xt, _ = bf16(rng.standard_normal((2, 3, 1, 32, H, D)))
+    kept = [new_cache(rng, 1, pool, page, H, D, "heads") for _ in range(2)]
+    got = []
+    for view in (whole[:, first:first + 2], whole[:, first:first + 2].contiguous()):
+        (kc, ks), (vc, vs) = [(k[0].clone(), k[2].clone()) for k in kept]
+        status = i32([0])
+        km.append_paged8(xt[0], xt[1], kc, vc, ks, vs, view, tokens_before=i32(before), chunk_tokens=i32(tokens),
+                         status=status)
+        got.append((kc, vc, ks, vs))
+        assert int(status) == km.STATUS_BAD_LENGTH
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    mine = set(whole[:, first:first + 2].flatten().tolist())
+    others = [p for p in range(pool) if p not in mine]
+    for (kc, _, ks, _), (now, now_scale) in zip(kept, (got[0][0::2], got[0][1::2])):
+        assert torch.equal(now[:, others], kc[:, others]) and torch.equal(now_scale[:, others], ks[:, others])
+
+
 def test_append_in_steps_equals_append_at_once():
     """One token at a time and all at once leave the same bytes where the largest magnitude comes first, and
     the same values up to the roundings of a lift otherwise."""
@@ -563,6 +589,24 @@ def test_attend_selected_pages(cache, page):
                         sel=i32(sel), sel_count=i32(count), lse=lse, n_splits=splits, **s["scales"])
         torch.cuda.synchronize()
         check_attend(out, lse, s, 128 ** -0.5, sel=sel_list)
+
+
+def test_selected_pages_end_where_a_view_of_the_table_does():
+    """An index past the view's columns names no page, whatever the tensor behind it holds there."""
+    s = attend_case(dict(kv=[300, 300], H=2, G=4))
+    whole, kv = i32(s["table"]), i32(s["kv"])
+    sel, count = i32(np.tile([0, 3, 9, 12], (2, 2, 1))), i32(np.full((2, 2), 4))
+    inside = [[0, 3]] * 4
+    for first in (0, 5):
+        view = whole[:, first:first + 9]
+        part = dict(s, table=s["table"][:, first:first + 9])
+        for table in (view, view.contiguous()):
+            out, status = torch.full_like(s["q"], -7.0), i32([0])
+            km.attend_paged(s["q"], s["kt"], s["vt"], out, table, kv, n_queries=1, n_keys=300, sel=sel,
+                            sel_count=count, status=status, **s["scales"])
+            torch.cuda.synchronize()
+            assert int(status) == km.STATUS_BAD_PAGE
+            check_attend(out, None, part, 128 ** -0.5, sel=inside)
 
 
 def test_attend_strided_rows_and_lse():
