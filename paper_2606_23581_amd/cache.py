@@ -145,6 +145,8 @@ def _workspace(a, need, workspace, device):
     if need > 0 and workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
     if workspace is not None:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
         a.workspace, a.workspace_bytes = _ptr(workspace), workspace.numel() * workspace.element_size()
     return workspace
 

@@ -347,6 +347,32 @@ def test_views_of_page_tables_end_where_the_view_does(monkeypatch):
             assert (a.pt_stride, a.pt_pages) == (20, view.shape[1])
 
 
+def test_a_given_workspace_is_as_long_as_it_says(monkeypatch):
+    """A view's elements may be many more than the memory behind it holds, or lie apart."""
+    monkeypatch.setattr(cache, "_device", lambda *t: None)
+    q, kv = torch.zeros((2, 8, 128), dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    planes = [torch.zeros((4, 16, 2, 128), dtype=torch.uint8) for _ in range(2)]
+    scale, table = torch.ones((4, 2)), torch.zeros((2, 300), dtype=torch.int32)
+
+    def attend(workspace):
+        return km.prepare_attend_paged(q, *planes, torch.zeros_like(q), table, kv, n_queries=1, n_keys=4096,
+                                       k_scale=scale, v_scale=scale, n_splits=4, workspace=workspace)
+
+    def select(workspace):
+        return km.prepare_select_pages(q, torch.zeros((4, 2, 128), dtype=torch.int8), scale,
+                                       torch.zeros((2, 3000), dtype=torch.int32), kv,
+                                       torch.zeros((2, 2, 4), dtype=torch.int32), torch.zeros((2, 2), dtype=torch.int32),
+                                       n_keys=40000, page_size=16, workspace=workspace)
+
+    for call in (attend, select):
+        need = call(None).args.workspace_bytes
+        assert need > 0
+        assert call(torch.zeros(need // 4)).args.workspace_bytes == need
+        for bad in (torch.zeros(16).expand(need, 16), torch.zeros(1).expand(need), torch.zeros((need, 2))[:, 0]):
+            with pytest.raises(ValueError, match="contiguous"):
+                call(bad)
+
+
 def test_reference_e4m3_agrees_with_torch():
     """The tests' own e4m3 rounding against torch's cast, at every value, midpoint and many others."""
     pos = ref.e4m3_values()[:127]
