@@ -546,8 +546,9 @@ typedef struct {
  * (>= -100) at which the group's largest finite magnitude is at most 127 * 2^f;
  * what is not finite counts as 0.  The integer sums are exact, so the
  * selection is one answer, whatever computes it.  A page number outside the
- * pool is flagged and its page ranked last; a request of at most n_keep pages
- * keeps them all, without a look at their numbers. */
+ * pool is flagged and its page ranked last, as is a page whose score is not a
+ * number; a request of at most n_keep pages keeps them all, without a look at
+ * their numbers. */
 typedef struct {
   int32_t n_requests;
   int32_t n_q_heads;             /* a multiple of n_kv_heads; group <= 64      */

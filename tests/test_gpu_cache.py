@@ -325,6 +325,33 @@ def test_select(name):
     assert int(status) == (km.STATUS_BAD_PAGE if c.get("bad") else 0)
 
 
+@pytest.mark.parametrize("pages", [60, 300, 1100])
+def test_select_scores_that_are_not_numbers(pages):
+    """Pages whose sums were never formed: any NaN as their scale (with any bits) ranks them last, and neither
+    adds to the selection nor leaves a place of it open.  300 pages in one kernel, 1100 in two."""
+    rng = np.random.default_rng(29)
+    kv, keep, H, G, D = [16 * pages, 16 * pages - 9], 9, 2, 4, 128
+    table, pool = table_for(rng, kv, 16)
+    k_sum = rng.integers(-127, 128, size=(pool, H, D)).astype(np.int8)
+    scale = (2.0 ** rng.integers(-3, 3, size=(pool, H))).astype(np.float32)
+    qt, qv = bf16(rng.standard_normal((2, H * G, D)))
+    for share in (0.3, 1.0):
+        bits = scale.copy().view(np.uint32)
+        lost = rng.random(pool) < share
+        bits[lost] = rng.choice(np.array([0x7FFFFFFF, 0xFFFFFFFF, 0x7FC00000, 0xFFC00000, 0x7F800001], dtype=np.uint32),
+                                size=bits[lost].shape)
+        sel = torch.full((4, H, keep), -9, dtype=torch.int32, device=DEV)      # two rows more than the call's
+        count = i32(np.full((2, H), -9))
+        km.select_pages(qt, torch.tensor(k_sum, device=DEV), torch.tensor(bits.view(np.int32), device=DEV).view(torch.float32),
+                        i32(table), i32(kv), sel[1:3], count, n_keys=max(kv), page_size=16)
+        torch.cuda.synchronize()
+        # ranked as a page that is not in the pool
+        known = np.where(lost[np.maximum(table, 0)], -1, table)
+        want = ref.select(qv, k_sum, scale.astype(float), known, kv, 16, keep, 1, 1)
+        assert sel[1:3].reshape(2 * H, keep).tolist() == want
+        assert (count == keep).all() and (sel[0] == -9).all() and (sel[3] == -9).all()
+
+
 # ---------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------
