@@ -166,7 +166,7 @@ __device__ __forceinline__ void score_pages(const SelectParams& p, int r, int h,
       const int j = t0 + u * 16 + (lane >> 2);
       if ((lane & 3) == 0 && j < end) {
         // one that is not a number would pass for another key: a page always taken, or none
-        const float score = (float)best * sc[u];
+        const float score = (float)best * sc[u] + 0.0f;   // -0 becomes 0, which it ties with
         uint32_t key = ((in >> u) & 1) && score == score ? ordered(score) : kNever;
         if (j < p.n_first || j >= n - p.n_last) key = kAlways;
         put(j, key);

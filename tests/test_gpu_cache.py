@@ -352,6 +352,19 @@ def test_select_scores_that_are_not_numbers(pages):
         assert (count == keep).all() and (sel[0] == -9).all() and (sel[3] == -9).all()
 
 
+def test_select_zeros_of_either_sign_tie():
+    """A negative sum under a scale of zero is a score of -0, which is no less than 0."""
+    k_sum = np.full((40, 1, 64), 1, dtype=np.int8)
+    k_sum[::2] = -1
+    scale, table = np.zeros((40, 1)), np.arange(40)[None].astype(np.int32)
+    qt, qv = bf16(np.ones((1, 4, 64)))
+    sel, count = i32(np.full((1, 1, 10), -9)), i32([[-9]])
+    km.select_pages(qt, torch.tensor(k_sum, device=DEV), torch.tensor(scale, dtype=torch.float32, device=DEV),
+                    i32(table), i32([640]), sel, count, n_keys=640, page_size=16)
+    torch.cuda.synchronize()
+    assert sel.flatten().tolist() == ref.select(qv, k_sum, scale, table, [640], 16, 10, 1, 1)[0] == [*range(9), 39]
+
+
 # ---------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------
