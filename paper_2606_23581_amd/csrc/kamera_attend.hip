@@ -145,9 +145,13 @@ __device__ __forceinline__ bf16x8 v_frag(const Step<D, FMT>& s, int b) {
 
 // Zero the V rows of this lane's tokens outside [lo, hi], and what is not finite
 // in the others (the result says whether there was any; see add_nonfinite).
+// A part that is not there has been read from the pool's first page: its scale,
+// which may be no number, goes too.
 template <int D, int FMT>
 __device__ __forceinline__ bool clear_unseen(Step<D, FMT>& s, int g, int lo, int hi) {
   uint32_t odd = 0;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) s.vs[u] = (s.ok >> u) & 1 ? s.vs[u] : 1.0f;
 #pragma unroll
   for (int u = 0; u < 2; ++u)
 #pragma unroll

@@ -108,7 +108,8 @@ struct Places {
 
 // Registers -> LDS.  With `clear`, V rows that no row of the block sees become
 // zero, and so does what is not finite in the others (the result says whether
-// there was any; see add_nonfinite).
+// there was any; see add_nonfinite).  A part that is not there has been read from
+// the pool's first page: its scale, which may be no number, goes too.
 template <int D, int FMT>
 __device__ __forceinline__ bool store_tile(Stage<D, FMT>& s, uint8_t* buf, const Places<D, FMT>& at, bool clear,
                                            uint32_t bad, int wave, int v_pos, int lo, int hi) {
@@ -131,6 +132,7 @@ __device__ __forceinline__ bool store_tile(Stage<D, FMT>& s, uint8_t* buf, const
   uint32_t odd = 0;
   if (clear) {
     const bool missing = (bad >> wave) & 1;
+    s.vs = missing ? 1.0f : s.vs;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const bool keep = !missing && v_pos + j >= lo && v_pos + j <= hi;

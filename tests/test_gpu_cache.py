@@ -574,6 +574,26 @@ def test_attend_values_that_a_row_does_not_see(name):
                 assert (np.abs(got[row] - want[row]) <= BOUND * size[row]).all(), (r, i)
 
 
+@pytest.mark.parametrize("nq,window", [([1, 1, 1], 0), ([4, 5, 2], 20), ([70, 40, 70], 0), ([70, 40, 70], 40)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attend_scales_of_pages_that_no_request_has(nq, window, D):
+    """The scales of a page that is nobody's, the pool's first, may hold anything."""
+    s = attend_case(dict(kv=[100, 45, 190], nq=nq, H=2, G=2, D=D, bad=[(0, 2)]))
+    first = {k: torch.cat([torch.full_like(t[:1], 0x7F if t.dtype is torch.uint8 else 1.0), t])
+             for k, t in dict(k_cache=s["kt"], v_cache=s["vt"], **s["scales"]).items()}
+    table, outs = i32(np.where(s["table"] >= 0, s["table"] + 1, -1)), []
+    for scale in (1.0, float("nan"), float("inf"), 0.0, -float("inf")):
+        first["k_scale"][0] = first["v_scale"][0] = scale
+        out, lse = torch.full_like(s["q"], -7.0), torch.full(s["q"].shape[:2], -7.0, device=DEV)
+        km.attend_paged(s["q"], out=out, page_table=table, kv_tokens=i32(s["kv"]), n_queries=max(nq), n_keys=190,
+                        q_tokens=i32(nq), window=window, lse=lse, **first)
+        outs.append((out, lse))
+    torch.cuda.synchronize()
+    check_attend(*outs[0], s, D ** -0.5, True, window)
+    for out, lse in outs[1:]:
+        assert torch.equal(out, outs[0][0]) and torch.equal(lse, outs[0][1])
+
+
 def test_attend_clean_keys_poisoned_values():
     """A value that is not finite, under finite scores: only its columns, only in the rows that see it."""
     for cache in ("e4m3", "bf16"):
