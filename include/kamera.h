@@ -497,7 +497,8 @@ typedef struct {
  *   k_sum[j] = round(t[j] * 2^-f) (ties to even), k_sum_scale = scale * 2^f
  * (fp32: 0 for a page of zeros).
  * kamera_select_pages scores pages by it.
- * A page may receive rows of one chunk only. */
+ * A page may receive rows of one chunk only.  No output may overlap an input
+ * (checked on the extents that the sizes imply) or another output. */
 typedef struct {
   int32_t n_chunks;
   int32_t n_layers;

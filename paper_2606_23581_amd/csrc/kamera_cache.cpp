@@ -24,6 +24,9 @@ Range flat(const void* p, int64_t n, int bytes) {
   return {a, a + (uintptr_t)n * bytes};
 }
 
+// The same of an optional array.
+Range flat_or(const void* p, int64_t n, int bytes) { return flat(p, p != nullptr ? n : 0, bytes); }
+
 bool meet(const Range& a, const Range& b) { return a.lo < a.hi && b.lo < b.hi && overlap(a.lo, a.hi, b.lo, b.hi); }
 
 bool multiples(const int64_t* s, int n, int64_t of) {
@@ -108,9 +111,9 @@ int build_tables(const kamera_page_tables_args* a, kamera::TablesParams& P, bool
   if (a->n_slots > 0 && a->slots == nullptr) return fail(KAMERA_ERR_NULL, "%s: slots is NULL", who);
   const int64_t n = a->n_requests;
   const Range outs[4] = {flat(a->page_table, n * a->pt_stride, 4), flat(a->token_base, n + 1, 4),
-                         flat(a->free_end, 1, 4), flat(a->slots, a->slots != nullptr ? a->n_slots : 0, 8)};
-  const Range ins[4] = {flat(a->tokens_before, a->tokens_before != nullptr ? n : 0, 4), flat(a->tokens_after, n, 4),
-                        flat(a->free_pages, a->n_free, 4), flat(a->free_begin, a->free_begin != nullptr ? 1 : 0, 4)};
+                         flat(a->free_end, 1, 4), flat_or(a->slots, a->n_slots, 8)};
+  const Range ins[4] = {flat_or(a->tokens_before, n, 4), flat(a->tokens_after, n, 4),
+                        flat(a->free_pages, a->n_free, 4), flat_or(a->free_begin, 1, 4)};
   for (int i = 0; i < 4; ++i) {
     for (int k = 0; k < 4; ++k)
       if (meet(outs[i], ins[k])) return fail(KAMERA_ERR_ALIAS, "%s: an output overlaps an input", who);
@@ -183,13 +186,17 @@ int build_append(const kamera_append_args* a, kamera::AppendParams& P, bool& lau
     return fail(KAMERA_ERR_RANGE, "%s: k_sum strides span more than the address space", who);
   // how far the rows reach is known only without a row base
   const int64_t ext_in[4] = {a->n_chunks, a->n_layers, a->row_base != nullptr ? 1 : a->n_tokens, a->n_heads};
-  Range in[2];
+  Range in[6];
   if (!span(a->k, a->k_stride, ext_in, 4, a->head_dim, 2, in[0].lo, in[0].hi) ||
       !span(a->v, a->v_stride, ext_in, 4, a->head_dim, 2, in[1].lo, in[1].hi))
     return fail(KAMERA_ERR_RANGE, "%s: row strides span more than the address space", who);
-  for (int i = 0; i < 6; ++i)
-    for (int k = 0; k < 2; ++k)
-      if (meet(out[i], in[k])) return fail(KAMERA_ERR_ALIAS, "%s: an output overlaps the rows", who);
+  in[2] = table_range(a->page_table, a->n_chunks, a->pt_stride, row);
+  in[3] = flat_or(a->chunk_tokens, a->n_chunks, 4);
+  in[4] = flat_or(a->tokens_before, a->n_chunks, 4);
+  in[5] = flat_or(a->row_base, a->n_chunks, 4);
+  for (const Range& o : out)
+    for (const Range& r : in)
+      if (meet(o, r)) return fail(KAMERA_ERR_ALIAS, "%s: an output overlaps an input", who);
   if (a->k_cache == a->v_cache || a->k_scale == a->v_scale)
     return fail(KAMERA_ERR_ALIAS, "%s: keys and values need a cache each", who);
   memset(&P, 0, sizeof(P));
@@ -450,7 +457,7 @@ int build_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& lau
   // how far q, out and lse reach is known only without a row base
   const int64_t n_rows = a->q_base != nullptr ? a->n_queries : (int64_t)a->n_requests * a->n_queries;
   const int64_t ext_q[2] = {n_rows, a->n_q_heads};
-  Range in[6] = {}, out[3] = {};
+  Range in[11] = {}, out[3] = {};
   if (!span(a->q, a->q_stride, ext_q, 2, a->head_dim, 2, in[0].lo, in[0].hi) ||
       !span(a->k_cache, a->k_cache_stride, ext, 3, a->head_dim, el, in[1].lo, in[1].hi) ||
       !span(a->v_cache, a->v_cache_stride, ext, 3, a->head_dim, el, in[2].lo, in[2].hi) ||
@@ -459,14 +466,21 @@ int build_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& lau
       (e4m3 && (!span(a->k_scale, a->k_scale_stride, ext_s, 2, 1, 4, in[3].lo, in[3].hi) ||
                 !span(a->v_scale, a->v_scale_stride, ext_s, 2, 1, 4, in[4].lo, in[4].hi))))
     return fail(KAMERA_ERR_RANGE, "%s: strides span more than the address space", who);
+  const int64_t entries = bounded_product({a->n_requests, a->n_kv_heads, a->sel_stride});
+  if (entries < 0) return fail(KAMERA_ERR_RANGE, "%s: too many selected pages", who);
   in[5] = table_range(a->page_table, a->n_requests, a->pt_stride, row);
+  in[6] = flat(a->kv_tokens, a->n_requests, 4);
+  in[7] = flat_or(a->q_tokens, a->n_requests, 4);
+  in[8] = flat_or(a->q_base, a->n_requests, 4);
+  in[9] = flat_or(a->sel, entries, 4);
+  in[10] = flat_or(a->sel_count, (int64_t)a->n_requests * a->n_kv_heads, 4);
   if (workspace > 0) {
     if ((rc = check_workspace(a->workspace, a->workspace_bytes, workspace, who))) return rc;
     out[2] = flat(a->workspace, workspace, 1);
   }
   for (int i = 0; i < 3; ++i) {
-    for (int k = 0; k < 6; ++k)
-      if (meet(out[i], in[k])) return fail(KAMERA_ERR_ALIAS, "%s: out, lse or workspace overlaps an input", who);
+    for (const Range& r : in)
+      if (meet(out[i], r)) return fail(KAMERA_ERR_ALIAS, "%s: out, lse or workspace overlaps an input", who);
     for (int k = i + 1; k < 3; ++k)
       if (meet(out[i], out[k])) return fail(KAMERA_ERR_ALIAS, "%s: out, lse and workspace overlap", who);
   }

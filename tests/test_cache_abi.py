@@ -329,6 +329,39 @@ def test_rows_of_a_page_table_narrower_than_their_stride(which, change, code):
     assert km.lib().kamera_validate_cache(which, ctypes.byref(a)) == code, km.last_error()
 
 
+@pytest.mark.parametrize("which,change", [
+    # attention: out, lse or the workspace over any of the arrays that a call reads
+    (3, dict(kv_tokens=0x21000000)),
+    (3, dict(q_tokens=0x21000000 + 2 * 2 * 2048 - 4)),
+    (3, dict(q_base=0x21000000 + 4)),
+    (3, dict(lse=P + 4)),
+    (3, dict(workspace=P)),
+    (3, dict(q_tokens=0x60000000)),
+    (3, dict(sel=0x21000000 - 4 * 31, sel_count=P, sel_stride=8)),
+    (3, dict(sel=P, sel_count=0x21000000 - 4 * 3, sel_stride=8)),
+    # append: caches, scales or sums over the table or the lengths
+    (1, dict(page_table=0x30000000 - 4 * 7)),
+    (1, dict(chunk_tokens=0x31000000)),
+    (1, dict(tokens_before=0x32000000 + 4)),
+    (1, dict(row_base=0x34000000 - 4)),
+    (1, dict(page_table=0x35000000)),
+])
+def test_outputs_over_inputs_are_refused(which, change):
+    a = MAKE[which](**change)
+    assert km.lib().kamera_validate_cache(which, ctypes.byref(a)) == km.ERR_ALIAS, km.last_error()
+
+
+@pytest.mark.parametrize("which,change", [
+    (3, dict(q_tokens=0x21000000 - 8)),
+    (3, dict(sel=0x21000000 - 4 * 32, sel_count=0x21000000 + 2 * 2 * 2048, sel_stride=8)),
+    (3, dict(kv_tokens=P, q_tokens=P, q_base=P)),
+    (1, dict(page_table=0x30000000 - 4 * 8, chunk_tokens=0x34000000 - 8, tokens_before=0x34000000 - 8)),
+])
+def test_outputs_beside_inputs_are_taken(which, change):
+    a = MAKE[which](**change)
+    assert km.lib().kamera_validate_cache(which, ctypes.byref(a)) == km.OK, km.last_error()
+
+
 def test_views_of_page_tables_end_where_the_view_does(monkeypatch):
     """A call is told the pages of its view, not those of the tensor behind it."""
     monkeypatch.setattr(cache, "_device", lambda *t: None)
