@@ -325,6 +325,25 @@ def test_select(name):
     assert int(status) == (km.STATUS_BAD_PAGE if c.get("bad") else 0)
 
 
+@pytest.mark.parametrize("G", [3, 20])
+@pytest.mark.parametrize("D", [64, 128])
+def test_select_most_pages_of_many_requests(G, D):
+    """Over 8192 pages a request, scored by the workgroup that selects: more than 128 (request, KV head) pairs."""
+    rng = np.random.default_rng(31)
+    kv, keep, H = [0] * 63 + [16 * km.MAX_SELECT_PAGES, 200000], 40, 2
+    table, pool = table_for(rng, kv, 16)
+    k_sum = rng.integers(-127, 128, size=(pool, H, D)).astype(np.int8)
+    scale = 2.0 ** rng.integers(-3, 3, size=(pool, H))
+    qt, qv = bf16(rng.standard_normal((65, H * G, D)))
+    sel, count = i32(np.full((65, H, keep), -9)), i32(np.full((65, H), -9))
+    km.select_pages(qt, torch.tensor(k_sum, device=DEV), torch.tensor(scale, dtype=torch.float32, device=DEV),
+                    i32(table), i32(kv), sel, count, n_keys=max(kv), page_size=16)
+    torch.cuda.synchronize()
+    want = ref.select(qv[63:], k_sum, scale, table[63:], kv[63:], 16, keep, 1, 1)
+    assert sel[63:].reshape(2 * H, keep).tolist() == want and (count[63:] == keep).all()
+    assert (sel[:63] == -1).all() and (count[:63] == 0).all()
+
+
 @pytest.mark.parametrize("pages", [60, 300, 1100])
 def test_select_scores_that_are_not_numbers(pages):
     """Pages whose sums were never formed: any NaN as their scale (with any bits) ranks them last, and neither
@@ -512,6 +531,18 @@ def test_attend(name):
 
 
 @pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+@pytest.mark.parametrize("nq", [[1, 1, 1], [3, 0, 5], [40, 70, 1]])
+@pytest.mark.parametrize("splits", [8, 9, 65])
+def test_attend_many_parts_of_small_heads(cache, nq, splits):
+    s = attend_case(dict(kv=[700, 33, 1500], nq=nq, H=3, G=2, D=64, cache=cache))
+    out, lse = torch.full_like(s["q"], -7.0), torch.full(s["q"].shape[:2], -7.0, device=DEV)
+    km.attend_paged(s["q"], s["kt"], s["vt"], out, i32(s["table"]), i32(s["kv"]), n_queries=s["n_max"], n_keys=1500,
+                    q_tokens=i32(nq), lse=lse, n_splits=splits, **s["scales"])
+    torch.cuda.synchronize()
+    check_attend(out, lse, s, 64 ** -0.5)
+
+
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
 @pytest.mark.parametrize("kv,nq", [([10, 3, 70], [16, 12, 16]), ([10, 70], [50, 90])])
 def test_attend_longest_window(cache, kv, nq):
     """A window of the type's largest value is no window, also for queries before the first key."""
@@ -624,6 +655,64 @@ def test_attend_clean_keys_poisoned_values():
             assert not np.isfinite(got[hit]).any()
             ok = np.abs(got - want) <= BOUND * size
             assert ok[~hit].all()
+
+
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("nq,window", [(4, 0), (70, 0), (70, 50)])
+@pytest.mark.parametrize("splits", [2, 3, 7])
+def test_attend_poisoned_values_in_split_work(cache, D, nq, window, splits):
+    """As with whole work: a value that is not finite goes to its column of the rows that see it, whichever part
+    of the keys holds it, and to nothing else.  Two in different tiles."""
+    s = attend_case(dict(kv=[300, 150], nq=[nq, nq], H=2, G=4, D=D, cache=cache))
+    cols, when = (5, D - 3), [(0, 300 - nq // 2), (0, 300 - nq), (1, 150 - 2)]
+    for (r, t), col in zip(when, (cols[0], cols[1], cols[0])):
+        pg, at = int(s["table"][r, t // 16]), t % 16
+        s["vt"][pg, at, :, col] = float("inf") if cache == "bf16" else 0x7F
+        s["v"][pg, at, :, col] = 0.0
+    out = torch.full_like(s["q"], -7.0)
+    km.attend_paged(s["q"], s["kt"], s["vt"], out, i32(s["table"]), i32(s["kv"]), n_queries=nq, n_keys=300,
+                    window=window, n_splits=splits, **s["scales"])
+    torch.cuda.synchronize()
+    got = out.double().cpu().numpy()
+    v = np.where(np.isfinite(s["v"]), s["v"], 0.0)            # slots that no request uses hold NaN
+    a = (s["table"], s["kv"], s["nq"], s["base"], 16, D ** -0.5, True, window)
+    want, size = ref.attend(s["qv"], s["k"], v, *a)[0], ref.attend(s["qv"], s["k"], np.abs(v), *a)[0]
+    hit = np.zeros(got.shape, dtype=bool)
+    for (r, t), col in zip(when, (cols[0], cols[1], cols[0])):
+        at = s["kv"][r] - nq + np.arange(nq)
+        sees = (t <= at) & (t > at - window if window else True)
+        hit[r * nq:(r + 1) * nq, :, col] |= sees[:, None]
+    assert not np.isfinite(got[hit]).any()
+    assert (np.abs(got - want) <= BOUND * size)[~hit].all()
+
+
+@pytest.mark.parametrize("cache", ["e4m3", "bf16"])
+@pytest.mark.parametrize("splits", [1, 2])
+def test_attend_poisoned_value_in_a_selected_page(cache, splits):
+    """The last page, seen in part, with a value that is not finite in a token that is seen and one in a token
+    that is not; a page that is not selected is full of them."""
+    s = attend_case(dict(kv=[200, 90], H=2, G=4, cache=cache))
+    sel, count = i32(np.tile([[[1, 3, 12]], [[0, 2, 5]]], (1, 2, 1))), i32(np.full((2, 2), 3))
+    odd = float("inf") if cache == "bf16" else 0x7F
+    for r, n in enumerate(s["kv"]):
+        last = int(s["table"][r, (n - 1) // 16])
+        s["vt"][last, (n - 1) % 16, :, 7] = odd
+        s["vt"][last, n % 16, :, 9] = odd
+        s["vt"][int(s["table"][r, 4])] = odd
+        s["v"][last, (n - 1) % 16, :, 7] = 0.0
+    v = np.where(np.isfinite(s["v"]), s["v"], 0.0)
+    out = torch.full_like(s["q"], -7.0)
+    km.attend_paged(s["q"], s["kt"], s["vt"], out, i32(s["table"]), i32(s["kv"]), n_queries=1, n_keys=200, sel=sel,
+                    sel_count=count, n_splits=splits, **s["scales"])
+    torch.cuda.synchronize()
+    got = out.double().cpu().numpy()
+    a = (s["table"], s["kv"], s["nq"], s["base"], 16, 128 ** -0.5, True, 0, [[1, 3, 12]] * 2 + [[0, 2, 5]] * 2)
+    want, size = ref.attend(s["qv"], s["k"], v, *a)[0], ref.attend(s["qv"], s["k"], np.abs(v), *a)[0]
+    hit = np.zeros(got.shape, dtype=bool)
+    hit[:, :, 7] = True
+    assert not np.isfinite(got[hit]).any()
+    assert (np.abs(got - want) <= BOUND * size)[~hit].all()
 
 
 @pytest.mark.parametrize("cache", ["e4m3", "bf16"])
