@@ -420,7 +420,10 @@ int kamera_gather_paged(const kamera_scatter_args* args, void* stream);
  * finite magnitude is at most 448 * 2^e.  A byte's value, its scaling to bf16
  * and a later change of e by whole steps are therefore exact wherever the
  * byte stays a normal number, and none of it depends on an order of summation:
- * the stored bytes are a function of the rows alone.
+ * the stored bytes are a function of the rows and of how they were divided over
+ * calls.  (A call whose rows raise a page's e rounds the bytes there a second
+ * time, where they leave the normal range; rows that come in one call, or
+ * without a larger magnitude after them, are rounded once.)
  * Element (layer l, page p, token t of the page, head h, column j) is at
  *   base + l*stride[0] + p*stride[1] + t*stride[2] + h*stride[3] + j,
  * any strides that are multiples of 16 bytes (e.g. [layer][page][head][token]
@@ -591,8 +594,9 @@ typedef enum {
  *               scale * <q[i][g], K[t]>,
  * where query i sees the keys t in [0, kv), with causal = 1 those with
  * t <= kv - n + i, and with window > 0 (causal only) of these the last
- * `window`.  A row that sees no key gets 0 (and lse = -infinity).  What a row
- * does not see does not touch it, whatever it holds.  lse (optional, fp32)
+ * `window`.  A row that sees no key gets 0 (and lse = -infinity), and so does
+ * one whose every score is -infinity.  What a row does not see does not touch
+ * it, whatever it holds.  lse (optional, fp32)
  * receives the natural logarithm of sum exp(scale * <q, K[t]>) at
  * lse + row*lse_stride[0] + g*lse_stride[1]; with it, results over parts of a
  * context can be joined.

@@ -265,7 +265,8 @@ def prepare_append_paged8(k, v, k_cache, v_cache, k_scale, v_scale, page_table, 
     k, v: [C, L, n, H, D] (any strides, last dim contiguous), or with row_base (int32 [C]) [L, rows, H, D],
     chunk c's rows from row_base[c] on and at most n_tokens of them.  k_cache, v_cache: float8_e4m3fn (or
     uint8) [L, pages, page_size, H, D]; k_scale, v_scale: fp32 [L, pages, H]; k_sum: int8 [L, pages, H, D]
-    with k_sum_scale fp32 [L, pages, H] (optional).  page_table: int32 [C, pages of a chunk];
+    with k_sum_scale fp32 [L, pages, H] (optional).  page_table: int32 [C, pages of a chunk], also columns of a
+    wider table: a chunk ends (STATUS_BAD_LENGTH) where its row of the view does.
     tokens_before, chunk_tokens: int32 [C] (default 0 and all rows).
     """
     import torch

@@ -7,7 +7,9 @@
 // read off A's bf16 bits: 448 = 1.75 * 2^8, so e = exponent(A) - 8, one more
 // where the fraction of A passes 1.75.  Scaling by 2^-e is exact, so one
 // rounding (v_cvt_pk_fp8_f32, to nearest even) stands between the row and its
-// byte, and any correct implementation stores the same bytes.
+// byte, and a second one only where a later call raises the page's e and the
+// byte leaves the normal range.  Any correct implementation stores the same
+// bytes for the same calls.
 //
 // Bound by HBM: 2 bytes read and 1 written for each element.  Waves keep their
 // rows in registers between the maximum and the conversion, so rows are read

@@ -32,7 +32,7 @@
 // TB/s.  The next step's loads are in flight while a step is computed; the four
 // waves of a workgroup take steps in turn and join in LDS; with few rows the keys
 // are split over workgroups too, and attend_join_kernel joins (65536 keys of one
-// request: 24.4 us of reading, 5.5 TB/s, and 4.5 us of joining).
+// request: 24.0 us of reading, 5.6 TB/s, and 4.4 us of joining).
 
 #include <algorithm>
 

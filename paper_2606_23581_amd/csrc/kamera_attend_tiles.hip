@@ -25,7 +25,7 @@
 // Bound by the softmax's vector instructions beside the matrix pipe: 64 keys cost a
 // wave 1024 cycles of MFMA and about as many of exponentials, maxima and
 // conversions, which two waves a SIMD (two workgroups a CU) overlap in part.  1024
-// queries of 8 x 8 heads over 16384 keys in 8 bits: 507 us, 1050 TFLOP/s, matrix pipe
+// queries of 8 x 8 heads over 16384 keys in 8 bits: 500 us, 1065 TFLOP/s, matrix pipe
 // busy 46%.  64 rows a wave, one wave a SIMD: 522 against 755
 // TFLOP/s in an earlier form, for want of a second wave to overlap with.
 

@@ -379,9 +379,10 @@ int size_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& laun
   memset(&P, 0, sizeof(P));
   P.rows_max = (int32_t)rows;
   // Few rows or many.  The few-rows kernel takes 32 rows of an 8-bit cache at once
-  // (4 queries of 8 heads, 32 requests of 8192 keys: 101 us, with the other kernel
-  // 152), and 16 of a bf16 one, whose loads leave no registers for more (202 us with
-  // the many-rows kernel, 324 with two tiles a wave here).
+  // (4 queries of 8 heads, 32 requests of 8192 keys of 8 KV heads: 100 us, with the
+  // other kernel 151; 5 queries: 158 and 153), and 16 of a bf16 one, whose loads leave
+  // no registers for more (the same 4 queries: 209 us with the many-rows kernel, here 282
+  // with two tiles a wave and 319 with one; 2 queries, 64 requests of 4096 keys: 193, here 201).
   const bool e4m3 = a->cache_type == KAMERA_CACHE_E4M3;
   P.tiles = rows > (e4m3 ? 32 : 16) && a->sel_stride == 0 ? 1 : 0;
   P.row_tiles = !P.tiles && e4m3 && rows > 16 ? 2 : 1;
@@ -393,9 +394,9 @@ int size_attend(const kamera_attend_args* a, kamera::AttendParams& P, bool& laun
   } else {
     // Few rows: one workgroup a CU, parts of at least 128 keys; up to 768 keys in 8
     // bits (384 in bf16) one part is as fast as many, which a second kernel joins (one
-    // request of 8 KV heads, 8 bits, 1 / 8 / 16 / 32 parts: 512 keys 8.1 / 9.8 / 9.8 /
-    // 10.0 us, 1024 keys 10.8 / 10.2 / 10.0 / 10.1, 4096 keys 26.8 / 12.4 / 11.2 / 10.8,
-    // 16384 keys 94.9 / 22.2 / 17.1 / 15.4).  Many rows: two workgroups a CU, parts of
+    // request of 8 KV heads, 8 bits, 1 / 8 / 16 / 32 parts: 512 keys 8.3 / 9.4 / 9.6 /
+    // 9.7 us, 1024 keys 10.8 / 9.9 / 9.9 / 9.9, 4096 keys 27.4 / 12.2 / 11.1 / 10.4,
+    // 16384 keys 96.5 / 21.6 / 16.4 / 13.7).  Many rows: two workgroups a CU, parts of
     // at least 512 keys.
     int64_t span_keys = a->sel_stride > 0 ? (int64_t)a->sel_stride * a->page_size : a->n_keys;
     if (a->window > 0) span_keys = std::min<int64_t>(span_keys, (int64_t)a->window + a->n_queries);
