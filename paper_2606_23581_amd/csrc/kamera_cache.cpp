@@ -335,7 +335,7 @@ int build_select(const kamera_select_args* a, kamera::SelectParams& P, bool& lau
   P.n_keep = a->n_keep;
   P.n_first = a->n_first;
   P.n_last = a->n_last;
-  P.max_pages = (int32_t)std::max<int64_t>(ceil_div(a->n_keys, a->page_size), 1);
+  P.max_pages = (int32_t)ceil_div(a->n_keys, a->page_size);
   P.n_pieces = n_pieces;
   P.keys = static_cast<uint32_t*>(a->workspace);
   launch = true;

@@ -415,6 +415,24 @@ def test_reference_e4m3_agrees_with_torch():
     np.testing.assert_array_equal(ref.encode(x.astype(np.float64)), want)
 
 
+def test_no_more_of_a_table_is_looked_up_than_there_is(tmp_path):
+    _host_program(tmp_path, "cache_params", [], ("launch_stub.cpp", "cache_params.cpp"))
+
+
+def _host_program(tmp_path, name, flags, sources):
+    if shutil.which("g++") is None or not os.path.exists("/opt/rocm/include/hip/hip_runtime_api.h"):
+        pytest.skip("no g++ or HIP headers")
+    exe = str(tmp_path / name)
+    cmd = ["g++", "-std=c++17", "-O1", "-g", "-D__HIP_PLATFORM_AMD__", "-I", "/opt/rocm/include", "-I",
+           os.path.join(ROOT, "include"), "-I", CSRC, "-I", TC, *flags,
+           *[os.path.join(CSRC, f) for f in ("kamera_abi.cpp", "kamera_cache.cpp")],
+           *[os.path.join(TC, f) for f in sources], "-o", exe, "-pthread"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip().endswith("ok"), (r.stdout[-2000:], r.stderr[-4000:])
+
+
 def _sanitized(tmp_path, name, flags):
     if shutil.which("g++") is None or not os.path.exists("/opt/rocm/include/hip/hip_runtime_api.h"):
         pytest.skip("no g++ or HIP headers")

@@ -371,6 +371,16 @@ def test_select_scores_that_are_not_numbers(pages):
         assert (count == keep).all() and (sel[0] == -9).all() and (sel[3] == -9).all()
 
 
+def test_select_without_keys():
+    """No request has a key: nothing is selected, and nothing of the tables is looked at."""
+    q = torch.zeros((3, 8, 128), dtype=torch.bfloat16, device=DEV)
+    sel, count = i32(np.full((3, 2, 4), -9)), i32(np.full((3, 2), -9))
+    km.select_pages(q, torch.zeros((5, 2, 128), dtype=torch.int8, device=DEV), torch.ones((5, 2), device=DEV),
+                    i32(np.full((3, 1), 99)), i32([0, 7, 300]), sel, count, n_keys=0, page_size=16)
+    torch.cuda.synchronize()
+    assert (sel == -1).all() and (count == 0).all()
+
+
 def test_select_zeros_of_either_sign_tie():
     """A negative sum under a scale of zero is a score of -0, which is no less than 0."""
     k_sum = np.full((40, 1, 64), 1, dtype=np.int8)
