@@ -100,6 +100,14 @@ def _typed(t, dtype, name, shape=None, contiguous=True):
     return t
 
 
+def _int(x, name) -> int:
+    """x as the library takes it, in 32 bits (the binding's structs would keep its low ones)."""
+    x = int(x)
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError(f"{name} must fit in 32 bits (got {x})")
+    return x
+
+
 def _table(page_table, n, tokens=None, page_size=1):
     """The row stride of an int32 [n, pages] table whose rows are dense.
 
@@ -230,7 +238,8 @@ def prepare_page_tables(tokens_before, tokens_after, free_pages, page_table, *, 
     L = lib()
     R = tokens_after.shape[0]
     a = CPageTablesArgs()
-    a.n_requests, a.page_size, a.n_pool_pages = R, int(page_size), int(n_pool_pages)
+    a.n_requests, a.page_size = R, _int(page_size, "page_size")
+    a.n_pool_pages = _int(n_pool_pages, "n_pool_pages")
     i32 = torch.int32
     _typed(tokens_before, i32, "tokens_before", (R,)), _typed(tokens_after, i32, "tokens_after", (R,))
     _typed(free_pages, i32, "free_pages"), _typed(free_begin, i32, "free_begin", (1,))
@@ -283,14 +292,14 @@ def prepare_append_paged8(k, v, k_cache, v_cache, k_scale, v_scale, page_table, 
         Ln, _, H, D = k.shape
         a.k_stride[0:4] = (0, *k.stride()[:3])
         a.v_stride[0:4] = (0, *v.stride()[:3])
-        n = int(n_tokens)
+        n = _int(n_tokens, "n_tokens")
     else:
         if k.dim() != 5 or k.shape[0] != C:
             raise ValueError("k and v must be [C, L, n, H, D], C the rows of page_table")
         _, Ln, rows, H, D = k.shape
         a.k_stride[0:4] = k.stride()[:4]
         a.v_stride[0:4] = v.stride()[:4]
-        n = rows if n_tokens is None else int(n_tokens)
+        n = rows if n_tokens is None else _int(n_tokens, "n_tokens")
         if n > rows:
             raise ValueError(f"n_tokens {n} exceeds the {rows} rows of a chunk")
     if k_cache.dim() != 5 or k_cache.shape != v_cache.shape:
@@ -365,15 +374,15 @@ def prepare_select_pages(q, k_sum, k_sum_scale, page_table, kv_tokens, sel, sel_
     _typed(status, torch.int32, "status")
     _device(q, k_sum, k_sum_scale, page_table, kv_tokens, sel, sel_count, workspace, status)
     a = CSelectArgs()
-    a.n_requests, a.n_q_heads, a.n_kv_heads, a.head_dim, a.n_keys = R, HQ, H, D, int(n_keys)
-    a.page_size, a.n_pool_pages = int(page_size), n_pages
-    a.pt_stride = _table(page_table, R, int(n_keys), int(page_size))
+    a.n_requests, a.n_q_heads, a.n_kv_heads, a.head_dim, a.n_keys = R, HQ, H, D, _int(n_keys, "n_keys")
+    a.page_size, a.n_pool_pages = _int(page_size, "page_size"), n_pages
+    a.pt_stride = _table(page_table, R, a.n_keys, a.page_size)
     a.kv_tokens, a.page_table, a.q = _ptr(kv_tokens), _ptr(page_table), _ptr(q)
     a.q_stride[0:2] = q.stride()[:2]
     a.k_sum, a.k_sum_scale = _ptr(k_sum), _ptr(k_sum_scale)
     a.k_sum_stride[0:2] = k_sum.stride()[:2]
     a.k_sum_scale_stride[:] = k_sum_scale.stride()
-    a.n_keep, a.n_first, a.n_last = keep, int(n_first), int(n_last)
+    a.n_keep, a.n_first, a.n_last = keep, _int(n_first, "n_first"), _int(n_last, "n_last")
     a.sel, a.sel_count, a.status = _ptr(sel), _ptr(sel_count), _ptr(status)
     workspace = _workspace(a, L.kamera_select_workspace(ctypes.byref(a)), workspace, q.device)
     call = Prepared(L.kamera_select_pages, a, (q, k_sum, k_sum_scale, page_table, kv_tokens, sel, sel_count,
@@ -427,7 +436,7 @@ def prepare_attend_paged(q, k_cache, v_cache, out, page_table, kv_tokens, *, n_q
         _bf16(k_cache, "k_cache")
     _inner(k_cache, "k_cache"), _inner(v_cache, "v_cache")
     R = kv_tokens.shape[0]
-    n_queries = int(n_queries)
+    n_queries, n_keys = _int(n_queries, "n_queries"), _int(n_keys, "n_keys")
     if q_base is None and R * n_queries > rows:
         raise ValueError(f"{R} requests of {n_queries} queries exceed the {rows} rows of q")
     for t, nm in ((kv_tokens, "kv_tokens"), (q_base, "q_base"), (q_tokens, "q_tokens")):
@@ -437,13 +446,14 @@ def prepare_attend_paged(q, k_cache, v_cache, out, page_table, kv_tokens, *, n_q
     _typed(lse, torch.float32, "lse", (rows, HQ), contiguous=False)
     _typed(status, torch.int32, "status")
     a = CAttendArgs()
-    a.n_requests, a.n_q_heads, a.n_kv_heads, a.head_dim, a.n_queries, a.n_keys = R, HQ, H, D, n_queries, int(n_keys)
+    a.n_requests, a.n_q_heads, a.n_kv_heads, a.head_dim, a.n_queries, a.n_keys = R, HQ, H, D, n_queries, n_keys
     a.page_size, a.n_pool_pages = page_size, n_pages
     # selected pages are whatever sel holds: one past the rows of a view is not seen
-    a.pt_stride = _table(page_table, R, int(n_keys) if sel is None else 0, page_size)
+    a.pt_stride = _table(page_table, R, n_keys if sel is None else 0, page_size)
     a.pt_pages = page_table.shape[1]
     a.cache_type = CACHE_E4M3 if eight else CACHE_BF16
-    a.causal, a.window, a.n_splits = int(causal), int(window), int(n_splits)
+    # a window past 32 bits holds every key there can be
+    a.causal, a.window, a.n_splits = int(causal), _int(min(window, (1 << 31) - 1), "window"), _int(n_splits, "n_splits")
     a.scale = D ** -0.5 if scale is None else float(scale)
     a.q_tokens, a.q_base, a.kv_tokens, a.page_table = _ptr(q_tokens), _ptr(q_base), _ptr(kv_tokens), _ptr(page_table)
     a.q, a.out, a.lse = _ptr(q), _ptr(out), _ptr(lse)

@@ -406,6 +406,47 @@ def test_a_given_workspace_is_as_long_as_it_says(monkeypatch):
                 call(bad)
 
 
+def test_numbers_past_32_bits(monkeypatch):
+    """They would reach the library as their low 32 bits, 2^32 + 5 keys as 5: refused, but for a window, which then
+    holds every key."""
+    monkeypatch.setattr(cache, "_device", lambda *t: None)
+    i4 = torch.int32
+    q, kv, table = torch.zeros((2, 8, 128), dtype=torch.bfloat16), torch.zeros(2, dtype=i4), torch.zeros((2, 3), dtype=i4)
+    planes = [torch.zeros((4, 16, 2, 128), dtype=torch.uint8) for _ in range(2)]
+    scale, rows = torch.ones((4, 2)), torch.zeros((1, 30, 2, 128), dtype=torch.bfloat16)
+
+    def attend(**kw):
+        a = dict(n_queries=1, n_keys=48, q_base=kv, k_scale=scale, v_scale=scale)
+        return km.prepare_attend_paged(q, *planes, torch.zeros_like(q), table, kv, **dict(a, **kw))
+
+    def select(**kw):
+        a = dict(n_keys=48, page_size=16)
+        km.prepare_select_pages(q, torch.zeros((4, 2, 128), dtype=torch.int8), scale, table, kv,
+                                torch.zeros((2, 2, 4), dtype=i4), torch.zeros((2, 2), dtype=i4), **dict(a, **kw))
+
+    def append(**kw):
+        a = dict(n_tokens=20, row_base=kv)
+        km.prepare_append_paged8(rows, rows, *[p[None] for p in planes], *[scale[None].clone() for _ in range(2)], table,
+                                 **dict(a, **kw))
+
+    def tables(**kw):
+        a = dict(page_size=16, n_pool_pages=4, free_end=torch.zeros(1, dtype=i4), token_base=torch.zeros(3, dtype=i4))
+        km.prepare_page_tables(None, kv, torch.zeros(5, dtype=i4), table, **dict(a, **kw))
+
+    far = 1 << 32
+    for call, names in ((attend, ("n_keys", "n_queries", "n_splits")),
+                        (select, ("n_keys", "page_size", "n_first", "n_last")), (append, ("n_tokens",)),
+                        (tables, ("page_size", "n_pool_pages"))):
+        call()
+        for name in names:
+            for x in (far + 1, far + 16, -far + 1, 1 << 31):
+                with pytest.raises(ValueError, match=name):
+                    call(**{name: x})
+    assert attend(window=far + 5).args.window == (1 << 31) - 1
+    with pytest.raises(ValueError, match="window"):
+        attend(window=-far + 5)
+
+
 def test_reference_e4m3_agrees_with_torch():
     """The tests' own e4m3 rounding against torch's cast, at every value, midpoint and many others."""
     pos = ref.e4m3_values()[:127]
