@@ -18,7 +18,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 
-from . import Prepared, _bf16, _check, _i32, _i32_dev, _i64, _ptr, _strides, _vp, lib
+from . import Prepared, _bf16, _check, _i32, _i32_dev, _i64, _ptr, _stream, _vp, lib
 
 STATUS_NO_PAGE = 2
 STATUS_BAD_LENGTH = 4
@@ -167,9 +167,9 @@ def _launch_on(stream, prepare, a, kw) -> None:
         return
     import torch
 
-    s = stream
-    if isinstance(stream, int):
-        s = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    s, handle = stream, _stream(stream)
+    if not isinstance(s, torch.cuda.Stream):         # a raw handle, or an object that has one
+        s = torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
     with torch.cuda.stream(s):
         prepare(*a, **kw).launch(s)
 

@@ -1022,6 +1022,22 @@ def test_own_workspace_is_memory_of_the_given_stream(raw, monkeypatch):
     check_attend(out, None, s, 128 ** -0.5)
 
 
+def test_calls_take_any_object_that_has_a_stream():
+    """As the package's other calls do: what has a cuda_stream."""
+    s = attend_case(dict(kv=[3000, 700], H=2, G=4))
+
+    class Handle:
+        pass
+
+    out, side, handle = torch.zeros_like(s["q"]), torch.cuda.Stream(), Handle()
+    handle.cuda_stream = side.cuda_stream
+    torch.cuda.synchronize()
+    km.attend_paged(s["q"], s["kt"], s["vt"], out, i32(s["table"]), i32(s["kv"]), n_queries=1, n_keys=3000, n_splits=4,
+                    stream=handle, **s["scales"])
+    torch.cuda.synchronize()
+    check_attend(out, None, s, 128 ** -0.5)
+
+
 @pytest.mark.parametrize("cache", ["e4m3", "bf16"])
 @pytest.mark.parametrize("queries", [1, 3, 40])
 def test_a_query_that_is_not_finite_stays_in_its_row(cache, queries):
