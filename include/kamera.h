@@ -29,13 +29,21 @@
  *   kamera_page_tables   pages and token slots for requests that grow;
  *   kamera_append_paged8 bf16 K, V rows into a paged cache held in 8 bits;
  *   kamera_select_pages  the pages a query needs most, by a cheap score;
- *   kamera_attend_paged  attention over the paged cache (8 bits or bf16).
+ *   kamera_attend_paged  attention over the paged cache (8 bits or bf16);
+ *
+ * from rows of a latent and a rope key (MLA), one for all heads of a token:
+ *
+ *   kamera_append_rotated  new rows into the bf16 pool, rotated on the way;
+ *   kamera_project_heads   a product with a matrix of its own for every head;
+ *   kamera_expand_latent   every head's keys and values from the pool's latents;
+ *   kamera_attend_latent   attention over the pool's rows themselves;
+ *   kamera_attend_expanded attention over expanded keys and values.
  *
  * Conventions shared by every entry point
  *   - Every tensor pointer is a DEVICE pointer owned by the caller.  The
  *     library never allocates, frees or synchronises; a call enqueues its
  *     kernel (kamera_form_patch: two or three, one after the other;
- *     kamera_select_pages and kamera_attend_paged: two where split) on
+ *     kamera_select_pages and the attentions: two where split) on
  *     `stream` (a hipStream_t; NULL = the default stream) and returns.  Results are
  *     visible to later work on that stream.
  *   - KV rows are bf16.  Strides are in ELEMENTS (bf16) unless named _bytes;
@@ -674,6 +682,258 @@ int64_t kamera_select_workspace(const kamera_select_args* args);
  * 1 kamera_append_paged8, 2 kamera_select_pages, 3 kamera_attend_paged. */
 int kamera_validate_cache(int32_t which, const void* args);
 
+/* ------------------------------------------------------------------------
+ * Serving from a paged latent cache (MLA).  A pool row holds a token's latent c
+ * (latent_dim columns) and its rotated rope key r (64 columns), shared by all
+ * heads, as kamera_rehydrate writes it.  Head g's keys and values are
+ *   K_g[t] = [c[t] Wk_g | r[t]],   V_g[t] = c[t] Wv_g.
+ * Two forms of the same attention:
+ *   absorbed  q' = q_n Wk_g^T (kamera_project_heads), attention of [q' | q_r]
+ *             over the rows themselves (kamera_attend_latent), and the result
+ *             times Wv_g (kamera_project_heads): a row is read once for all
+ *             heads -- single tokens and a few;
+ *   expanded  every head's c Wk_g and c Wv_g are formed (kamera_expand_latent)
+ *             and attended over (kamera_attend_expanded): less than a third of
+ *             the products -- prompts.
+ * ------------------------------------------------------------------------ */
+
+/* Rotary positions scaled for contexts longer than the rows were trained on.
+ * With f_j = theta^(-2j/rope_dim) a pair turns by position * f'_j,
+ *   LINEAR  f'_j = f_j / factor;
+ *   TURNS, PAIRS  f'_j = f_j (s_j + (1 - s_j) / factor), s_j clamped to [0, 1]:
+ *     TURNS  s_j = (t_j - low_turns) / (high_turns - low_turns), where t_j =
+ *            original_tokens * f_j / (2 pi) is how often pair j turns over the
+ *            original context;
+ *     PAIRS  s_j = 1 - (j - lo) / (hi - lo), with J(t) = (rope_dim / 2) *
+ *            ln(original_tokens / (2 pi t)) / ln(theta), lo =
+ *            max(floor(J(high_turns)), 0), hi = min(ceil(J(low_turns)),
+ *            rope_dim - 1), and hi - lo at least 0.001.
+ * Both rotated columns are multiplied by `amplitude`. */
+typedef enum {
+  KAMERA_SCALING_NONE = 0,
+  KAMERA_SCALING_LINEAR = 1,
+  KAMERA_SCALING_TURNS = 2,
+  KAMERA_SCALING_PAIRS = 3
+} kamera_scaling_kind;
+
+typedef struct {
+  int32_t kind;                  /* kamera_scaling_kind                        */
+  double factor;                 /* > 0 (not looked at with NONE)              */
+  double original_tokens;        /* > 0 (TURNS, PAIRS)                         */
+  double low_turns;              /* 0 < low_turns < high_turns (TURNS, PAIRS)  */
+  double high_turns;
+  double amplitude;              /* finite; 0 counts as 1                      */
+} kamera_rope_scaling;
+
+/* kamera_append_rotated -- n = chunk_tokens[c] (n_tokens if NULL) new bf16 rows
+ * of every chunk c and layer: keys and values into the bf16 paged pool behind
+ * the tokens_before[c] (0 if NULL) tokens that the chunk's pages hold, row i
+ * as token tokens_before[c] + i in page page_table[c][token / page_size], and
+ * the rope bands of their queries, in one pass.
+ *   keys    the columns [rope_offset, rope_offset + rope_dim) of a row of k_dim
+ *           are rotated, the others copied;
+ *   values  copied (v NULL: none, for instance latent rows);
+ *   queries (q NULL: none) rope_dim columns a head, q and q_out being views of
+ *           the band alone; q_out may be q (the same pointer and strides).
+ * Row i of chunk c is at x + c*stride[0] + l*stride[1] + (row_base[c] + i)*
+ * stride[2] + h*stride[3] (row_base NULL = 0).  Its position is
+ * tokens_before[c] + i, or with `positions` the coordinates
+ *   positions[c*position_stride[0] + (row_base[c] + i)*position_stride[1] + x*position_stride[2]],
+ * x = 0, or 0 .. 2 (t, h, w) where the rope has sections.
+ * Angles are taken in fp64, rotations in fp32, results rounded once to bf16.
+ * Tokens past the pages of a row (pt_pages) are left out
+ * (KAMERA_STATUS_BAD_LENGTH), as are those of pages outside the pool
+ * (KAMERA_STATUS_BAD_PAGE); their queries are rotated all the same.
+ * Outputs must not overlap inputs or each other (checked on the extents that
+ * the sizes imply; rows of one tensor that lie beside each other, the same
+ * strides and disjoint columns, are no overlap). */
+typedef struct {
+  int32_t n_chunks;
+  int32_t n_layers;
+  int32_t n_tokens;              /* most new tokens of a chunk                 */
+  int32_t n_k_heads;
+  int32_t k_dim;                 /* multiples of 8, <= KAMERA_MAX_HEAD_DIM     */
+  int32_t n_v_heads;
+  int32_t v_dim;
+  int32_t n_q_heads;
+  int32_t page_size;             /* > 0                                        */
+  int32_t pt_stride;
+  int32_t pt_pages;              /* entries of a page-table row (0: pt_stride) */
+  int32_t n_pool_pages;
+  kamera_rope rope;              /* offset a multiple of 8, dim of 16 (NeoX) or
+                                    8 (interleaved)                            */
+  kamera_rope_scaling scaling;
+  const int32_t* chunk_tokens;   /* device [n_chunks], or NULL                 */
+  const int32_t* tokens_before;  /* device [n_chunks], or NULL                 */
+  const int32_t* row_base;       /* device [n_chunks], or NULL                 */
+  const int32_t* page_table;     /* device [n_chunks][pt_stride], pt_pages of  */
+                                 /*   each row in use                          */
+  const int32_t* positions;      /* optional                                   */
+  int64_t position_stride[3];    /* chunk, row, coordinate                     */
+  const void* k;
+  int64_t k_stride[4];           /* chunk, layer, row, head                    */
+  const void* v;
+  int64_t v_stride[4];
+  const void* q;
+  int64_t q_stride[4];
+  void* q_out;
+  int64_t q_out_stride[4];
+  void* k_cache;
+  int64_t k_cache_stride[4];     /* layer, page, token, head                   */
+  void* v_cache;
+  int64_t v_cache_stride[4];
+  uint32_t* status;
+} kamera_append_rotated_args;
+
+/* kamera_project_heads -- out[i][g] = x[i][g] W[g]: n_rows rows of n_heads
+ * heads, each times its own n_in x n_out matrix; sums in fp32, rounded once to
+ * bf16.  Element (a, b) of W[g] is at w + g*w_stride[0] + a*w_stride[1] +
+ * b*w_stride[2]; one of the last two strides is 1.  A head stride of 0 shares
+ * x or W among the heads.  out must not overlap x or w. */
+typedef struct {
+  int32_t n_rows;
+  int32_t n_heads;
+  int32_t n_in;                  /* multiples of 64, <= KAMERA_MAX_HEAD_DIM    */
+  int32_t n_out;
+  const void* x;
+  int64_t x_stride[2];           /* row, head                                  */
+  const void* w;
+  int64_t w_stride[3];           /* head, in, out                              */
+  void* out;
+  int64_t out_stride[2];
+} kamera_project_args;
+
+/* kamera_expand_latent -- the same product with the rows of a paged pool: for
+ * token t < kv_tokens[r] of request r and head g
+ *   out[row_base[r] + t][g] = c W[g],   c the first n_in columns of its pool row
+ * (row_base NULL: r * n_keys).  Rows of tokens in pages outside the pool are
+ * left as they were (KAMERA_STATUS_BAD_PAGE), as is every other row. */
+typedef struct {
+  int32_t n_requests;
+  int32_t n_heads;
+  int32_t n_in;                  /* multiples of 64, <= KAMERA_MAX_HEAD_DIM    */
+  int32_t n_out;
+  int32_t n_keys;                /* most cached tokens of a request            */
+  int32_t page_size;             /* > 0                                        */
+  int32_t pt_stride;
+  int32_t n_pool_pages;
+  const int32_t* kv_tokens;      /* device [n_requests], at most n_keys        */
+  const int32_t* row_base;       /* device [n_requests], or NULL               */
+  const int32_t* page_table;     /* device [n_requests][pt_stride]             */
+  const void* cache;
+  int64_t cache_stride[2];       /* page, token                                */
+  const void* w;
+  int64_t w_stride[3];           /* head, in, out                              */
+  void* out;
+  int64_t out_stride[2];         /* row, head                                  */
+  uint32_t* status;
+} kamera_expand_args;
+
+/* kamera_attend_latent -- softmax attention of a batch of requests over the
+ * rows of a paged latent pool (the absorbed form).  Request r has n =
+ * q_tokens[r] (n_queries if NULL) query tokens, rows q_base[r] + i
+ * (r*n_queries + i if NULL) of q and out, and kv = kv_tokens[r] tokens in the
+ * pool, its queries' own included.  With x[t] = [c[t] | r[t]] the pool row of
+ * token t,
+ *   out[i][g] = sum_t p[t] c[t],  p = softmax over the seen t of
+ *               scale * <q[i][g], x[t]>.
+ * Which keys a query sees, rows that see none, values in what a row does not
+ * see, lse, pages outside the pool and the precision of sums and weights are as
+ * in kamera_attend_paged.
+ *
+ * The work is spread evenly over n_parts workgroups (0: chosen from the
+ * sizes); where that divides a row's keys a second kernel on the same stream
+ * joins the parts, and workspace holds them (as in kamera_attend_paged;
+ * kamera_attend_latent_workspace bytes). */
+typedef struct {
+  int32_t n_requests;
+  int32_t n_heads;
+  int32_t latent_dim;            /* 256 or 512                                 */
+  int32_t rope_dim;              /* 64                                         */
+  int32_t n_queries;             /* most query tokens of a request             */
+  int32_t n_keys;                /* most cached tokens of a request            */
+  int32_t page_size;             /* a multiple of 16                           */
+  int32_t pt_stride;
+  int32_t n_pool_pages;
+  int32_t causal;                /* 1 or 0                                     */
+  int32_t window;                /* > 0: keys seen at most; 0: all             */
+  float scale;                   /* finite                                     */
+  int32_t n_parts;               /* 0: automatic; else 1 .. 1024               */
+  const int32_t* q_tokens;       /* device [n_requests], or NULL               */
+  const int32_t* q_base;         /* device [n_requests], or NULL               */
+  const int32_t* kv_tokens;      /* device [n_requests], at most n_keys        */
+  const int32_t* page_table;     /* device [n_requests][pt_stride]             */
+  const void* q;                 /* bf16, rows of latent_dim + rope_dim        */
+  int64_t q_stride[2];           /* row, head                                  */
+  void* out;                     /* bf16, rows of latent_dim                   */
+  int64_t out_stride[2];
+  float* lse;                    /* optional                                   */
+  int64_t lse_stride[2];
+  const void* cache;             /* rows of latent_dim + rope_dim              */
+  int64_t cache_stride[2];       /* page, token                                */
+  void* workspace;
+  int64_t workspace_bytes;
+  uint32_t* status;
+} kamera_attend_latent_args;
+
+/* kamera_attend_expanded -- the same over expanded keys and values: key t of
+ * request r and head g is [k[kv_base[r] + t][g] | r[t]] with r[t] the rope key
+ * in the pool, its value v[kv_base[r] + t][g] (kv_base NULL: r * n_keys),
+ *   out[i][g] = sum_t p[t] v[t][g],  p = softmax over the seen t of
+ *               scale * (<q[i][g][:head_dim], k[t][g]> + <q[i][g][head_dim:], r[t]>).
+ * Everything else is as in kamera_attend_latent; a key whose page is outside
+ * the pool is not seen. */
+typedef struct {
+  int32_t n_requests;
+  int32_t n_heads;
+  int32_t head_dim;              /* 64 or 128                                  */
+  int32_t rope_dim;              /* 64                                         */
+  int32_t n_queries;
+  int32_t n_keys;
+  int32_t page_size;             /* a multiple of 16                           */
+  int32_t pt_stride;
+  int32_t n_pool_pages;
+  int32_t causal;
+  int32_t window;
+  float scale;
+  int32_t n_parts;
+  const int32_t* q_tokens;
+  const int32_t* q_base;
+  const int32_t* kv_tokens;
+  const int32_t* kv_base;        /* device [n_requests], or NULL               */
+  const int32_t* page_table;
+  const void* q;                 /* bf16, rows of head_dim + rope_dim          */
+  int64_t q_stride[2];           /* row, head                                  */
+  void* out;                     /* bf16, rows of head_dim                     */
+  int64_t out_stride[2];
+  float* lse;
+  int64_t lse_stride[2];
+  const void* k;                 /* rows of head_dim                           */
+  int64_t k_stride[2];           /* row, head                                  */
+  const void* v;
+  int64_t v_stride[2];
+  const void* rope_cache;        /* the pool's rope columns                    */
+  int64_t rope_cache_stride[2];  /* page, token                                */
+  void* workspace;
+  int64_t workspace_bytes;
+  uint32_t* status;
+} kamera_attend_expanded_args;
+
+int kamera_append_rotated(const kamera_append_rotated_args* args, void* stream);
+int kamera_project_heads(const kamera_project_args* args, void* stream);
+int kamera_expand_latent(const kamera_expand_args* args, void* stream);
+int kamera_attend_latent(const kamera_attend_latent_args* args, void* stream);
+int kamera_attend_expanded(const kamera_attend_expanded_args* args, void* stream);
+
+/* As kamera_attend_workspace. */
+int64_t kamera_attend_latent_workspace(const kamera_attend_latent_args* args);
+int64_t kamera_attend_expanded_workspace(const kamera_attend_expanded_args* args);
+
+/* As kamera_validate, for the entry points above: 0 kamera_append_rotated,
+ * 1 kamera_project_heads, 2 kamera_expand_latent, 3 kamera_attend_latent,
+ * 4 kamera_attend_expanded. */
+int kamera_validate_latent(int32_t which, const void* args);
+
 /* Host-side check of a page table copy (host memory, n_chunks x pt_stride,
  * the first ceil(tokens/page_size) entries of each row are used): every used
  * entry in [0, n_pool_pages) and no page used twice.  Returns KAMERA_OK or
@@ -714,8 +974,9 @@ int kamera_rehydrate_schedule(const kamera_rehydrate_args* args);
 const char* kamera_last_error(void);
 int kamera_abi_version(void);
 /* sizeof of the argument structs: 0 rehydrate, 1 shift, 2 scatter, 3 plane,
- * 4 rope, 5 form, 6 page tables, 7 append, 8 select, 9 attend; -1 otherwise.  Lets a foreign-function binding check its
- * layout. */
+ * 4 rope, 5 form, 6 page tables, 7 append, 8 select, 9 attend, 10 append
+ * rotated, 11 project, 12 expand, 13 attend latent, 14 attend expanded; -1
+ * otherwise.  Lets a foreign-function binding check its layout. */
 int64_t kamera_struct_size(int32_t which);
 
 #ifdef __cplusplus

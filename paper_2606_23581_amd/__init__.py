@@ -18,6 +18,8 @@ Entry points (same names as the C ABI):
                     (App. A): U = U_svd S [:, :m], W = Vt[:m]
 * ``page_tables``, ``append_paged8``, ``select_pages``, ``attend_paged``
                     serving from the paged cache (module ``cache``)
+* ``append_rotated``, ``project_heads``, ``expand_latent``, ``attend_latent``, ``attend_expanded``
+                    serving from a paged latent cache (module ``latent``)
 """
 
 from __future__ import annotations
@@ -148,7 +150,7 @@ def lib() -> ctypes.CDLL:
     global _LIB
     if _LIB is not None:
         return _LIB
-    from . import cache as _cache
+    from . import cache as _cache, latent as _latent
 
     # torch ships its own HIP runtime: load it first so that the library binds
     # to the same runtime instance torch's tensors and streams live in
@@ -192,8 +194,9 @@ def lib() -> ctypes.CDLL:
     L.kamera_struct_size.argtypes = [_i32]
     L.kamera_struct_size.restype = _i64
     _cache.declare(L)
+    _latent.declare(L)
     sizes = {0: CRehydrateArgs, 1: CShiftArgs, 2: CScatterArgs, 3: CPlane, 4: CRope, 5: CFormArgs,
-             **_cache.STRUCTS}
+             **_cache.STRUCTS, **_latent.STRUCTS}
     for k, cls in sizes.items():
         if L.kamera_struct_size(k) != ctypes.sizeof(cls):
             raise KameraUnavailable(f"struct layout mismatch for {cls.__name__}: "
@@ -601,5 +604,7 @@ def check_page_table(page_table_host, n_tokens: int, page_size: int, n_pool_page
 
 from .cache import *  # noqa: E402,F401,F403
 from .cache import EXPORTS as _CACHE_EXPORTS  # noqa: E402
+from .latent import *  # noqa: E402,F401,F403
+from .latent import EXPORTS as _LATENT_EXPORTS  # noqa: E402
 
-EXPORTS = EXPORTS + _CACHE_EXPORTS
+EXPORTS = EXPORTS + _CACHE_EXPORTS + _LATENT_EXPORTS

@@ -38,8 +38,9 @@ def _run(cmd, verbose):
 
 DEVICE_SOURCES = ("kamera_kernels.hip", "kamera_rows.hip", "kamera_patch.hip", "kamera_tridiag.hip",
                   "kamera_tables.hip", "kamera_append.hip", "kamera_select.hip", "kamera_attend.hip",
-                  "kamera_attend_tiles.hip")
-HOST_SOURCES = ("kamera_abi.cpp", "kamera_cache.cpp")
+                  "kamera_attend_tiles.hip", "kamera_rotate.hip", "kamera_project.hip", "kamera_attend_latent.hip",
+                  "kamera_attend_expanded.hip")
+HOST_SOURCES = ("kamera_abi.cpp", "kamera_cache.cpp", "kamera_latent.cpp")
 
 
 def build(verbose: bool = False, save_temps: bool = False) -> str:

@@ -1,0 +1,457 @@
+// kamera_attend_latent: attention over the rows of a paged latent pool.
+//
+// A row is key and value at once: x = [c | r], scores <q, x>, results sum p c.  The
+// rows of a request -- every query token's heads -- are one matrix, taken in blocks of
+// 16 RW rows: RW waves of 16 rows each share the keys of a group, and the KW groups
+// of a workgroup take 32 keys in turn.  Keys go from the pool straight into LDS and
+// are read from there twice, as rows for the scores and, transposed, as columns for
+// the results:
+//   S^T = X Q^T and O^T = C^T P^T with 16x16x32 bf16 MFMAs.  In S^T lane l holds row
+//   l % 16 and keys 4 (l / 16) + i of each 16; these registers are P^T's B operand as
+//   they are when the inner index of the second product runs over the keys in that
+//   order, which transposed reads give at no cost.
+// 16 rows a wave and not 32, which would halve the reads of LDS for each product: the
+// results of 32 rows (256 registers) and their queries (144) leave the compiler no room
+// and it spills.
+//
+// LDS: a slot holds 32 keys.  16-byte chunks are exchanged by an exclusive-or of their
+// number with bits 1 .. 3 of the key, highest last, so that 16 keys' reads of a chunk
+// and eight keys' of 32 bytes both spread over all banks.
+//
+// Softmax in powers of two (scale * log2 e folded in), fp32.  A row's running maximum
+// moves only when a score passes it by more than 8.
+
+#include "kamera_mla_device.h"
+
+namespace kamera {
+
+namespace {
+
+constexpr int kStepKeys = 32;
+constexpr int kJoinThreads = 256;
+
+__device__ __forceinline__ uint32_t twist(uint32_t key) {
+  return ((key >> 1) & 1) << 2 | ((key >> 2) & 1) << 1 | ((key >> 3) & 1);
+}
+
+__device__ __forceinline__ float max_x16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_x16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+}  // namespace
+
+template <int LAT, int RW>
+__global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void attend_latent_kernel(MlaParams) {
+  const MlaParams& p = kernel_params<MlaParams>();
+  constexpr int NW = latent_waves(RW), kThr = NW * 64, KW = latent_groups(RW), NB = 4 / KW;
+  constexpr int kRowB = (LAT + kRopeCols) * 2, CH = kRowB / 16, kSlot = kStepKeys * kRowB;
+  constexpr int kUnit = kStepKeys * KW, KS = (LAT + kRopeCols) / 32, DT = LAT / 16;
+  constexpr int LPG = CH / 8;                      // loads of a wave for 8 keys
+  constexpr int LW = RW < 4 ? RW : 4;              // waves that load a step's keys (of 8, those take turns)
+  constexpr int NA = 4 / LW;                       // groups of 8 keys that a wave loads
+  constexpr int kPad = 132;                        // floats of a row of the epilogue's tile
+  static_assert(kUnit == 32 * KW && NB >= 1, "");
+  extern __shared__ u32x4 s_buf[];
+  __shared__ float s_ml[NW][16][3];
+  __shared__ int s_odd;                            // a value that is not finite was left out of a product
+  const uint32_t lds = lds_offset(s_buf);
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c16 = lane & 15, g = lane >> 4, wr = wave % RW, kg = wave / RW;
+
+  Share share;
+  if (p.n_parts > 0) {
+    share = divide<kUnit, kThr>(p, blockIdx.x, reinterpret_cast<int*>(s_buf));
+  } else {
+    share.task = p.n_tasks - 1 - blockIdx.x;       // late row blocks, which see the most keys, first
+    share.skip = 0;
+    share.units = units_of<kUnit>(block_of(p, share.task));
+  }
+
+  // this lane's pieces of 8 keys that the wave loads: offset from the first one's row
+  const uint32_t t_stride = (uint32_t)p.pool_s[1];
+  uint32_t off[LPG], flip = 0;
+#pragma unroll
+  for (int b = 0; b < LPG; ++b) {
+    const uint32_t i = b * 64 + lane, key = i / CH, c = (i % CH) ^ twist(key);
+    off[b] = key * t_stride + c * 16;
+    flip |= (c & 1) << b;
+  }
+  // places of the operands in a slot: chunk 4 s + g of key c16, and of keys 4 g ..
+  uint32_t k_at[2], v_at[4];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) k_at[s] = c16 * kRowB + (((4 * s + g) ^ twist(c16)) << 4);
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    const uint32_t key = 4 * g + (c16 >> 2), c = 2 * b + ((c16 & 3) >> 1);
+    v_at[b] = key * kRowB + ((c ^ twist(key)) << 4) + (c16 & 1) * 8;
+  }
+
+  uint32_t task = share.task;
+  int skip = share.skip, units = share.units, segment = 0;
+  for (; units > 0; ++task, skip = 0) {
+    const Block blk = block_of(p, task);
+    const int total = units_of<kUnit>(blk), take = min(total - skip, units);
+    if (take <= 0) continue;
+    units -= take;
+    const int key0 = (blk.lo / kUnit + skip) * kUnit + kg * kStepKeys;   // the group's keys of the first unit
+    const int part_begin = blk.lo >> 4, part_end = (blk.hi >> 4) + 1;
+
+    // this wave's rows; lane l has row l % 16
+    const int wave_row = blk.row_first + wr * 16, row = wave_row + c16;
+    const int64_t row0 = p.q_base != nullptr ? (int64_t)p.q_base[blk.r] : (int64_t)blk.r * p.n_queries;
+    const int query = (int)fast_div((uint32_t)row, p.fd_group);
+    bf16x8 qf[KS];
+    int row_lo = INT32_MAX;                        // sees the keys row_lo .. row_lo + row_span; none past the end
+    uint32_t row_span = 0;
+    {
+      const bool there = row < blk.row_end;
+      const int last = mla_last_key(p, blk.n, blk.kv, query);
+      if (there && last >= 0 && blk.kv > 0) {
+        row_lo = mla_first_key(p, last);
+        row_span = (uint32_t)(min(last, blk.kv - 1) - row_lo);
+      }
+      const uint16_t* src = p.q + (row0 + query) * p.q_s[0] + (int64_t)(row - query * p.group) * p.q_s[1] + g * 8;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        u32x4 x = {0u, 0u, 0u, 0u};
+        if (there) x = *reinterpret_cast<const u32x4*>(src + ks * 32) ^ p.q_sign;
+        qf[ks] = __builtin_bit_cast(bf16x8, x);
+      }
+    }
+    f32x4 o[DT];
+    float m = kLow, l = 0.f, lx = 0.f;
+#pragma unroll
+    for (int b = 0; b < DT; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    // pages looked up 32 steps at a time: lane i has part i % 2 of step i / 2 of the batch
+    auto batch = [&](int it) {
+      const int at = it + (lane >> 1);
+      return fetch_pool_parts(p, blk.r, at < take ? ((key0 + at * kUnit) >> 4) + (lane & 1) : -1, part_begin, part_end);
+    };
+    PoolParts parts = batch(0);
+    if (tid == 0) s_odd = 0;
+    lds_barrier();
+    auto slot_of = [&](int it) { return lds + (kg * NB + (NB > 1 ? it % NB : 0)) * kSlot; };
+
+    // Step it's keys into its slot: the wave's share of them.  The result: which of its
+    // two parts are in the pool.
+    auto issue = [&](int it) {
+      if (it > 0 && (it & 31) == 0) parts = batch(it);
+      const uint32_t ok = (uint32_t)(parts.ok >> (2 * (it & 31))) & 3u;
+      if (RW == 8 && ((wave >> 2) ^ it) & 1) return ok;
+      const int pos = key0 + it * kUnit;
+      const bool whole = ok == 3u && pos >= blk.lo && pos + kStepKeys - 1 <= blk.hi;
+#pragma unroll
+      for (int a = 0; a < NA; ++a) {
+        const int first = ((wr % LW) * NA + a) * 8;                // its first key in the step
+        const uint32_t odd = (first >> 3) & 1, to = slot_of(it) + first * kRowB;
+        const uint64_t base = lane_u64(parts.at, 2 * (it & 31) + (first >> 4)) + odd * (8 * (uint64_t)t_stride);
+#pragma unroll
+        for (int b = 0; b < LPG; ++b) {
+          const uint32_t at = off[b] + odd * (16 - ((flip >> b) & 1) * 32);
+          if (whole) {
+            load_lds((const uint8_t*)base, at, to + b * 1024);
+          } else {
+            const uint32_t i = b * 64 + opaque(lane);
+            const int key = pos + first + (int)(i / CH);
+            const bool seen = ((ok >> (first >> 4)) & 1) && key >= blk.lo && key <= blk.hi;
+            load_lds(seen ? base + at : (uint64_t)g_zero_row + (i % CH) * 16, to + b * 1024);
+          }
+        }
+      }
+      return ok;
+    };
+
+    // Scores and softmax of a step; the weights as the second product takes them.
+    auto weigh = [&](int pos, uint32_t slot, uint32_t ok) {
+      f32x4 sc[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) sc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(read_chunk(slot + k_at[ks & 1] + (ks >> 1) * 128 + u * 16 * kRowB),
+                                                          qf[ks], sc[u], 0, 0, 0);
+
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = sc[i >> 2][i & 3];
+      if (ok != 3u || pos + kStepKeys - 1 > blk.all_hi || pos < blk.all_lo) {      // some row does not see it whole
+        const int at = pos + 4 * g - row_lo;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const bool there = (ok >> (i >> 2)) & 1;
+          x[i] = there && (uint32_t)(at + (16 * (i >> 2) + (i & 3))) <= row_span ? x[i] : -INFINITY;
+        }
+      }
+      float top = max2(max2(max2(x[0], x[1]), max2(x[2], x[3])), max2(max2(x[4], x[5]), max2(x[6], x[7]))) * p.scale2;
+      if (__ballot(top > m + kSlack) != 0) {
+        const float m_new = fmaxf(m, max_x32(max_x16(top)));
+        const float down = exp2_fast(m - m_new);
+        m = m_new;
+        l *= down;
+        lx *= down;
+#pragma unroll
+        for (int b = 0; b < DT; ++b) o[b] *= down;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = exp2_fast(__builtin_fmaf(x[i], p.scale2, -m));
+      if (p.lse != nullptr) lx += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+      const u32x4 w = {pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+      l = add_pair(w.w, add_pair(w.z, add_pair(w.y, add_pair(w.x, l))));
+      return __builtin_bit_cast(bf16x8, w);
+    };
+    auto gather = [&](uint32_t slot, bf16x8 pf) {
+#pragma unroll
+      for (int b = 0; b < DT; ++b) {
+        const uint32_t at = slot + v_at[b & 3] + (b >> 2) * 128;
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join(read_columns(at), read_columns(at + 16 * kRowB)), pf, o[b], 0, 0, 0);
+      }
+    };
+    // The values of a group's slot without what is not finite, by its RW waves.
+    auto clean = [&](uint32_t slot) {
+      bool met = false;
+      for (int i = wr * 64 + lane; i < kStepKeys * (LAT / 8); i += RW * 64)
+        met |= clean_chunk(slot + (i / (LAT / 8)) * kRowB + (i % (LAT / 8)) * 16);
+      if (met) s_odd = 1;
+    };
+    // a step in which the wave has work
+    auto busy = [&](int pos) { return pos <= blk.hi && pos + kStepKeys > blk.lo && wave_row < blk.row_end; };
+
+    if constexpr (NB == 1) {
+      // a wave's keys are its own: no one else waits for them
+      uint32_t ok = issue(0);
+      for (int it = 0; it < take; ++it) {
+        const int pos = key0 + it * kUnit;
+        vm_wait<0>();
+        if (busy(pos)) {
+          const bf16x8 pf = weigh(pos, slot_of(it), ok);
+          if (mixed(blk, pos, kStepKeys)) clean(slot_of(it));
+          gather(slot_of(it), pf);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (it + 1 < take) ok = issue(it + 1);
+      }
+    } else {
+      uint32_t oks = 0;                            // two bits a slot
+#pragma unroll
+      for (int i = 0; i < NB - 1; ++i)
+        if (i < take) oks |= issue(i) << (2 * i);
+      for (int it = 0; it < take; ++it) {
+        // the wave's loads of the NB - 2 steps behind this one may be under way (half of
+        // them where waves load in turn)
+        if (it + NB - 2 < take) vm_wait<(RW == 8 ? (NB - 2) / 2 : NB - 2) * NA * LPG>();
+        else vm_wait<0>();
+        lds_barrier();                             // the step's keys are there, and the slot before is free
+        const int next = it + NB - 1, s = next % NB;
+        if (next < take) oks = (oks & ~(3u << (2 * s))) | (issue(next) << (2 * s));
+        const int pos = key0 + it * kUnit;
+        bf16x8 pf = {};
+        if (busy(pos)) pf = weigh(pos, slot_of(it), (oks >> (2 * (it % NB))) & 3u);
+        if (mixed(blk, pos - kg * kStepKeys, kUnit)) {             // the same for all waves
+          lds_barrier();
+          clean(slot_of(it));
+          lds_barrier();
+        }
+        if (busy(pos)) gather(slot_of(it), pf);
+      }
+    }
+
+    // the groups' results are joined 128 columns at a time
+    l = sum_x32(sum_x16(l));
+    lx = sum_x32(sum_x16(lx));
+    lds_barrier();
+    if (g == 0) {
+      s_ml[wave][c16][0] = m;
+      s_ml[wave][c16][1] = l;
+      s_ml[wave][c16][2] = lx;
+    }
+    lds_barrier();
+    const bool odd = __builtin_amdgcn_readfirstlane(s_odd) != 0;   // cleared for the next task behind the barriers below
+    float top = kLow;
+#pragma unroll
+    for (int k = 0; k < KW; ++k) top = fmaxf(top, s_ml[k * RW + wr][c16][0]);
+    const float down = exp2_fast(m - top);
+    float* tile = reinterpret_cast<float*>(s_buf);
+    const bool direct = skip == 0 && take == total;
+    const int64_t part = ((int64_t)blockIdx.x * 2 + (segment > 0 ? 1 : 0)) * p.rows_block;
+    ++segment;
+#pragma unroll
+    for (int cq = 0; cq < DT / 8; ++cq) {
+#pragma unroll
+      for (int b = 0; b < 8; ++b) *reinterpret_cast<f32x4*>(tile + (wave * 16 + c16) * kPad + b * 16 + 4 * g) = o[cq * 8 + b] * down;
+      lds_barrier();
+      for (int j = tid >> 5; j < RW * 16; j += kThr / 32) {
+        const int col = (tid & 31) * 4, w0 = j >> 4, at = j & 15;
+        const int out_row = blk.row_first + j;
+        if (out_row >= blk.row_end) break;
+        f32x4 a = {0.f, 0.f, 0.f, 0.f};
+        float mm = kLow, ll = 0.f, lxx = 0.f;
+#pragma unroll
+        for (int k = 0; k < KW; ++k) {
+          a += *reinterpret_cast<const f32x4*>(tile + ((k * RW + w0) * 16 + at) * kPad + col);
+          mm = fmaxf(mm, s_ml[k * RW + w0][at][0]);
+        }
+#pragma unroll
+        for (int k = 0; k < KW; ++k) {
+          const float f = exp2_fast(s_ml[k * RW + w0][at][0] - mm);
+          ll += s_ml[k * RW + w0][at][1] * f;
+          lxx += s_ml[k * RW + w0][at][2] * f;
+        }
+        if (direct) {
+          const int i = (int)fast_div((uint32_t)out_row, p.fd_group);
+          const int64_t hq = out_row - i * p.group;
+          const float inv = ll == 0.f ? 0.f : 1.0f / ll;
+          *reinterpret_cast<u32x2*>(p.out + (row0 + i) * p.out_s[0] + hq * p.out_s[1] + cq * 128 + col) =
+              u32x2{pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv)};
+          if (p.lse != nullptr && cq == 0 && col == 0) p.lse[(row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] = row_lse(mm, lxx);
+        } else {
+          *reinterpret_cast<f32x4*>(p.part_o + (part + j) * LAT + cq * 128 + col) = a;
+          if (cq == 0 && col == 0) *reinterpret_cast<f32x4*>(p.part_ml + (part + j) * 4) = f32x4{mm, ll, lxx, 0.f};
+        }
+      }
+      lds_barrier();
+    }
+    if (odd) {
+      const int from = (blk.lo / kUnit + skip) * kUnit;
+      add_nonfinite(p, blk, from, from + take * kUnit, NB == 1 ? kStepKeys : kUnit, LAT, direct, part, row0, [&](int key) {
+        const int k = (int)fast_div((uint32_t)key >> 4, p.fd_page16);
+        const int page = p.page_table[(int64_t)blk.r * p.pt_stride + k];
+        if (page < 0 || page >= p.n_pool_pages) return (const uint16_t*)nullptr;
+        return (const uint16_t*)(p.pool + page * p.pool_s[0] + (key - k * p.page_size) * p.pool_s[1]);
+      });
+    }
+  }
+}
+
+// Joins the parts of each row: with M the largest of the parts' maxima m_s,
+// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.  A workgroup takes 128 columns
+// of a row; eight ways of 32 threads take every eighth part and meet in LDS.
+__global__ __launch_bounds__(kJoinThreads) void mla_join_kernel(MlaParams) {
+  const MlaParams& p = kernel_params<MlaParams>();
+  constexpr int kWays = 8, kChunk = 4;
+  __shared__ f32x4 s_o[kWays][32];
+  __shared__ float s_ml[kWays][3];
+  const int tid = threadIdx.x, col = tid & 31, way = tid >> 5;
+  const int quarters = p.dim >> 7 > 0 ? p.dim >> 7 : 1;
+  const int cq = blockIdx.y % quarters, rr = blockIdx.y / quarters;
+  const uint32_t task = blockIdx.x;
+  const int u0 = p.prefix[task], u1 = p.prefix[task + 1], per = p.prefix[p.n_tasks + 1];
+  if (u1 <= u0) return;
+  const int w0 = u0 / per, w1 = (u1 - 1) / per;
+  if (w0 == w1) return;                            // one workgroup had it all
+  const Block blk = block_of(p, task);
+  const int row = blk.row_first + rr;
+  if (row >= blk.row_end) return;
+  const int c0 = cq * 128 + col * 4;
+  const bool there = c0 < p.dim;
+  // the first part lies in its workgroup's first segment only where that begins with it
+  const int first_slot = u0 == w0 * per ? 0 : 1;
+
+  float top = kLow, l = 0.f, lx = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = w0 + way; s0 <= w1; s0 += kChunk * kWays) {
+    f32x4 ml[kChunk], o[kChunk];
+#pragma unroll
+    for (int k = 0; k < kChunk; ++k) {
+      const int s = min(s0 + k * kWays, w1);       // one past the end is read again and left out
+      const int64_t at = ((int64_t)s * 2 + (s == w0 ? first_slot : 0)) * p.rows_block + rr;
+      ml[k] = *reinterpret_cast<const f32x4*>(p.part_ml + at * 4);
+      o[k] = there ? *reinterpret_cast<const f32x4*>(p.part_o + at * p.dim + c0) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    float m = top;
+#pragma unroll
+    for (int k = 0; k < kChunk; ++k) m = fmaxf(m, ml[k].x);
+    const float down = exp2_fast(top - m);
+    top = m;
+    l *= down;
+    lx *= down;
+    acc *= down;
+#pragma unroll
+    for (int k = 0; k < kChunk; ++k)
+      if (s0 + k * kWays <= w1) {
+        const float f = exp2_fast(ml[k].x - top);
+        l += ml[k].y * f;
+        lx += ml[k].z * f;
+        acc += o[k] * f;
+      }
+  }
+  s_o[way][col] = acc;
+  if (col == 0) {
+    s_ml[way][0] = top;
+    s_ml[way][1] = l;
+    s_ml[way][2] = lx;
+  }
+  __syncthreads();
+  if (way != 0) return;
+  const float own = top;
+#pragma unroll
+  for (int k = 1; k < kWays; ++k) top = fmaxf(top, s_ml[k][0]);
+  const float down = exp2_fast(own - top);
+  l *= down;
+  lx *= down;
+  acc *= down;
+#pragma unroll
+  for (int k = 1; k < kWays; ++k) {
+    const float f = exp2_fast(s_ml[k][0] - top);
+    l += s_ml[k][1] * f;
+    lx += s_ml[k][2] * f;
+    acc += s_o[k][col] * f;
+  }
+  const int64_t row0 = p.q_base != nullptr ? (int64_t)p.q_base[blk.r] : (int64_t)blk.r * p.n_queries;
+  const int i = (int)fast_div((uint32_t)row, p.fd_group);
+  const int64_t hq = blk.h * p.group + row - i * p.group;
+  acc *= l == 0.f ? 0.f : 1.0f / l;
+  if (there)
+    *reinterpret_cast<u32x2*>(p.out + (row0 + i) * p.out_s[0] + hq * p.out_s[1] + c0) =
+        u32x2{pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w)};
+  if (cq == 0 && col == 0 && p.lse != nullptr) p.lse[(row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] = row_lse(top, lx);
+}
+
+hipError_t launch_mla_join(const MlaParams& p, hipStream_t s) {
+  const int quarters = p.dim >> 7 > 0 ? p.dim >> 7 : 1;
+  const int rows = (int)((int64_t)p.n_queries * p.group < p.rows_block ? (int64_t)p.n_queries * p.group : p.rows_block);
+  hipLaunchKernelGGL(mla_join_kernel, dim3((uint32_t)p.n_tasks, (uint32_t)(rows * quarters)), dim3(kJoinThreads), 0, s, p);
+  return hipGetLastError();
+}
+
+namespace {
+
+template <int LAT, int RW>
+hipError_t launch_rows(const MlaParams& p, hipStream_t s) {
+  static std::atomic<bool> done[kMaxDevices];
+  const int slots = 4 * kStepKeys * (LAT + kRopeCols) * 2, tile = latent_waves(RW) * 16 * 132 * 4;
+  const int lds = slots > tile ? slots : tile;
+  const hipError_t e = ensure_lds_limit((const void*)attend_latent_kernel<LAT, RW>, lds, done);
+  if (e != hipSuccess) return e;
+  const uint32_t grid = (uint32_t)(p.n_parts > 0 ? p.n_parts : p.n_tasks);
+  hipLaunchKernelGGL((attend_latent_kernel<LAT, RW>), dim3(grid), dim3(latent_waves(RW) * 64), lds, s, p);
+  return hipGetLastError();
+}
+
+template <int LAT>
+hipError_t launch_lat(const MlaParams& p, hipStream_t s) {
+  switch (p.row_waves) {
+    case 1: return launch_rows<LAT, 1>(p, s);
+    case 2: return launch_rows<LAT, 2>(p, s);
+    case 4: return launch_rows<LAT, 4>(p, s);
+    default: return launch_rows<LAT, 8>(p, s);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_attend_latent(const MlaParams& p, hipStream_t s) {
+  const hipError_t e = p.dim == 512 ? launch_lat<512>(p, s) : launch_lat<256>(p, s);
+  if (e != hipSuccess || p.n_parts == 0) return e;
+  return launch_mla_join(p, s);
+}
+
+}  // namespace kamera

@@ -14,27 +14,6 @@ using namespace kamera::host;
 
 namespace {
 
-struct Range {
-  uintptr_t lo, hi;
-};
-
-// Byte range of n elements from p.
-Range flat(const void* p, int64_t n, int bytes) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(p);
-  return {a, a + (uintptr_t)n * bytes};
-}
-
-// The same of an optional array.
-Range flat_or(const void* p, int64_t n, int bytes) { return flat(p, p != nullptr ? n : 0, bytes); }
-
-bool meet(const Range& a, const Range& b) { return a.lo < a.hi && b.lo < b.hi && overlap(a.lo, a.hi, b.lo, b.hi); }
-
-bool multiples(const int64_t* s, int n, int64_t of) {
-  for (int k = 0; k < n; ++k)
-    if (s[k] % of != 0) return false;
-  return true;
-}
-
 // Page selection: from so many pages a request on they are scored by workgroups of
 // their own (see kamera_select.hip).
 constexpr int64_t kSelectSplit = 1024;
@@ -51,33 +30,6 @@ int check_heads(int32_t q_heads, int32_t kv_heads, const char* who) {
   if (q_heads / kv_heads > KAMERA_MAX_GROUP)
     return fail(KAMERA_ERR_RANGE, "%s: %d query heads share a KV head, at most %d can", who, q_heads / kv_heads,
                 KAMERA_MAX_GROUP);
-  return KAMERA_OK;
-}
-
-// `pages`: the entries of a row.
-int check_table(const int32_t* table, int32_t pt_stride, int32_t pages, int32_t page_size, int32_t n_pool_pages,
-                int64_t tokens, const char* who) {
-  if (table == nullptr) return fail(KAMERA_ERR_NULL, "%s: page_table is NULL", who);
-  if (n_pool_pages <= 0) return fail(KAMERA_ERR_SHAPE, "%s: n_pool_pages must be positive", who);
-  if (pt_stride < 0 || pages < ceil_div(tokens, page_size))
-    return fail(KAMERA_ERR_SHAPE, "%s: %d pages a row (stride %d) < %lld pages needed for %lld tokens", who, pages,
-                pt_stride, (long long)ceil_div(tokens, page_size), (long long)tokens);
-  return KAMERA_OK;
-}
-
-// Entries that a row of a page table has.
-int32_t row_pages(int32_t pt_stride, int32_t pt_pages) { return pt_pages != 0 ? pt_pages : pt_stride; }
-
-// Bytes of a table of n rows.
-Range table_range(const int32_t* table, int64_t n, int32_t pt_stride, int32_t pages) {
-  return flat(table, n > 0 && pages > 0 ? (n - 1) * pt_stride + pages : 0, 4);
-}
-
-int check_workspace(const void* workspace, int64_t bytes, int64_t needed, const char* who) {
-  if (workspace == nullptr) return fail(KAMERA_ERR_NULL, "%s: workspace is NULL", who);
-  if (bytes < needed)
-    return fail(KAMERA_ERR_SHAPE, "%s: workspace of %lld bytes, %lld needed", who, (long long)bytes, (long long)needed);
-  if (!aligned16(workspace)) return fail(KAMERA_ERR_ALIGN, "%s: workspace must be 16-byte aligned", who);
   return KAMERA_OK;
 }
 

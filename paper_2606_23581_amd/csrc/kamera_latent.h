@@ -1,0 +1,124 @@
+// Launch parameters of the kernels that serve from a paged latent cache (kernel
+// arguments), built and validated by the host layer in kamera_latent.cpp.
+#pragma once
+
+#include <stdint.h>
+
+#include <hip/hip_runtime_api.h>
+
+#include "kamera_launch.h"
+
+namespace kamera {
+
+constexpr int kRopeCols = 64;        // columns of the rope key behind a latent
+
+// ---- rotated append ----
+
+constexpr int kRotateTokens = 32;    // most tokens of a workgroup
+
+struct RotatePlane {
+  const uint16_t* in;
+  uint16_t* out;
+  int64_t in_s[4];                   // chunk, layer, row, head
+  int64_t out_s[4];                  // the same (queries); layer, page, token, head (pool)
+  int32_t n_heads;                   // 0: the plane is not there
+  int32_t n_items;                   // threads' pieces of a head's row: the band's first, then 16-byte copies
+  int32_t band_items;
+  int32_t band_vec;                  // first 16-byte vector of the band
+  FastDiv fd_heads, fd_items;
+};
+
+struct RotateParams {
+  RopeParams rope;
+  RotatePlane plane[3];              // keys, values, queries
+  const int32_t* chunk_tokens;
+  const int32_t* tokens_before;
+  const int32_t* row_base;
+  const int32_t* page_table;
+  const int32_t* positions;
+  int64_t position_s[3];
+  uint32_t* status;
+  float amplitude;
+  int32_t n_tokens, page_size, pt_stride, pt_pages, n_pool_pages;
+  int32_t n_layers, n_blocks;
+  int32_t block_tokens;              // tokens of a workgroup
+  int32_t n_tasks;
+  FastDiv fd_blocks, fd_layers, fd_page;
+};
+
+// ---- products ----
+
+struct ProjectParams {
+  const uint16_t* x;
+  const uint16_t* w;
+  uint16_t* out;
+  int64_t x_s[2];                    // row, head (dense); page, token (paged)
+  int64_t w_s[3];
+  int64_t out_s[2];
+  // paged
+  const int32_t* kv_tokens;
+  const int32_t* row_base;
+  const int32_t* page_table;
+  uint32_t* status;
+  int32_t n_requests, n_keys, page_size, pt_stride, n_pool_pages;
+  int32_t n_rows, n_heads, n_in, n_out;
+  int32_t paged;
+  int32_t w_k;                       // 1: W's columns of one output lie together (stride `in` is 1)
+  int32_t small;                     // 1: tiles of 32 rows
+  int32_t n_row_blocks, n_col_blocks;
+  int32_t n_tasks, per_xcd;
+  FastDiv fd_rows, fd_cols, fd_heads, fd_page;
+};
+
+// ---- attention ----
+
+constexpr int kMlaDivideTasks = 2048;   // from so many (request, head, row block) tasks on a workgroup takes one whole
+
+// Latent form: waves of a workgroup whose row blocks are `row_waves` waves (of 16 rows) high,
+// and its groups, which take 32 keys in turn.
+constexpr int latent_waves(int row_waves) { return row_waves >= 4 ? 8 : 4; }
+constexpr int latent_groups(int row_waves) { return latent_waves(row_waves) / row_waves; }
+
+struct MlaParams {
+  const int32_t* q_tokens;
+  const int32_t* q_base;
+  const int32_t* kv_tokens;
+  const int32_t* kv_base;            // expanded
+  const int32_t* page_table;
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;
+  const uint8_t* pool;               // latent rows, or the rope columns (expanded)
+  const uint8_t* k;                  // expanded
+  const uint8_t* v;
+  float* part_o;                     // [workgroup][2][rows of a block][columns] unnormalised sums
+  float* part_ml;                    // [workgroup][2][rows of a block][4] running maximum (in powers of 2), sum of
+                                     // the rounded weights, sum of the weights
+  int32_t* prefix;                   // [n_tasks + 1] units before each task, then the units of a workgroup
+  uint32_t* status;
+  int64_t q_s[2], out_s[2], lse_s[2];
+  int64_t pool_s[2];                 // bytes: page, token
+  int64_t k_s[2], v_s[2];            // bytes: row, head
+  float scale2;                      // |scale| * log2(e), at least 1e-30
+  uint32_t q_sign;                   // 0x80008000 where the scale is negative: q's signs are turned
+  int32_t n_requests, n_heads, dim;  // dim: latent_dim or head_dim
+  int32_t n_queries, n_keys, page_size, pt_stride, n_pool_pages;
+  int32_t causal, window;
+  int32_t group;                     // heads of a token that are rows of one task (latent: all, expanded: 1)
+  int32_t task_heads;                // heads that are tasks of their own (latent: 1, expanded: all)
+  int32_t rows_block;                // rows of a task
+  int32_t row_waves;                 // latent: waves of a row block, 1, 2, 4 or 8
+  int32_t n_row_blocks;
+  int32_t n_tasks;
+  int32_t n_parts;                   // > 0: workgroups among which all tasks' units are divided; 0: one a task
+  int32_t min_units;                 // least units of a workgroup
+  FastDiv fd_group, fd_blocks, fd_heads, fd_page16;
+};
+
+hipError_t launch_rotate(const RotateParams& p, hipStream_t s);
+hipError_t launch_project(const ProjectParams& p, hipStream_t s);
+hipError_t launch_attend_latent(const MlaParams& p, hipStream_t s);
+hipError_t launch_attend_expanded(const MlaParams& p, hipStream_t s);
+hipError_t launch_mla_join(const MlaParams& p, hipStream_t s);      // by the two above
+
+}  // namespace kamera
