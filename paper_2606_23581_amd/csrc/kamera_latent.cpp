@@ -57,6 +57,9 @@ int check_rows(const void* p, const int64_t* s, int n, const char* what, const c
   return KAMERA_OK;
 }
 
+// A stride in bytes (one that does not fit belongs to a dimension of one element).
+int64_t in_bytes(int64_t s) { return (int64_t)((uint64_t)s * 2); }
+
 // ---------------------------------------------------------------------------
 
 int check_scaling(const kamera_rope_scaling& s, const char* who) {
@@ -136,7 +139,6 @@ int build_rotate(const kamera_append_rotated_args* a, kamera::RotateParams& P, b
   if (a->n_chunks == 0 || a->n_layers == 0 || a->n_tokens == 0) return KAMERA_OK;
   const int32_t row = row_pages(a->pt_stride, a->pt_pages);
   if ((rc = check_table(a->page_table, a->pt_stride, row, a->page_size, a->n_pool_pages, 0, who))) return rc;
-  if (row < 0) return fail(KAMERA_ERR_SHAPE, "%s: negative pt_pages", who);
   if (a->k == nullptr || a->k_cache == nullptr) return fail(KAMERA_ERR_NULL, "%s: k and k_cache are needed", who);
   if (has_v != (a->v_cache != nullptr)) return fail(KAMERA_ERR_NULL, "%s: v and v_cache go together", who);
   if (has_q != (a->q_out != nullptr)) return fail(KAMERA_ERR_NULL, "%s: q and q_out go together", who);
@@ -156,7 +158,7 @@ int build_rotate(const kamera_append_rotated_args* a, kamera::RotateParams& P, b
   fill_rope(a->rope, P.rope);
   scale_rope(a->rope, a->scaling, P.rope);
   P.amplitude = a->scaling.amplitude == 0.0 ? 1.0f : (float)a->scaling.amplitude;
-  fill_plane(P.plane[0], a->k, a->k_stride, a->k_cache, a->k_cache_stride, (int32_t)kh, a->k_dim, a->rope, a->rope.rope_offset);
+  if (kh > 0) fill_plane(P.plane[0], a->k, a->k_stride, a->k_cache, a->k_cache_stride, (int32_t)kh, a->k_dim, a->rope, a->rope.rope_offset);
   if (vh > 0) fill_plane(P.plane[1], a->v, a->v_stride, a->v_cache, a->v_cache_stride, (int32_t)vh, a->v_dim, a->rope, -1);
   if (qh > 0) fill_plane(P.plane[2], a->q, a->q_stride, a->q_out, a->q_out_stride, (int32_t)qh, a->rope.rope_dim, a->rope, 0);
   // what overlaps; how far rows reach is known only without a row base
@@ -481,7 +483,7 @@ int build_mla(const A* a, int32_t dim, const void* pool, const int64_t* pool_s, 
     P.q_s[k] = a->q_stride[k];
     P.out_s[k] = a->out_stride[k];
     P.lse_s[k] = a->lse_stride[k];
-    P.pool_s[k] = pool_s[k] * 2;
+    P.pool_s[k] = in_bytes(pool_s[k]);
   }
   // the kernels take a largest score by its product with a positive factor; a
   // zero scale becomes one that leaves every score a difference of zero
@@ -546,8 +548,8 @@ int build_expanded(const kamera_attend_expanded_args* a, kamera::MlaParams& P, b
   P.v = static_cast<const uint8_t*>(a->v);
   P.kv_base = a->kv_base;
   for (int k = 0; k < 2; ++k) {
-    P.k_s[k] = a->k_stride[k] * 2;
-    P.v_s[k] = a->v_stride[k] * 2;
+    P.k_s[k] = in_bytes(a->k_stride[k]);
+    P.v_s[k] = in_bytes(a->v_stride[k]);
   }
   launch = true;
   return KAMERA_OK;

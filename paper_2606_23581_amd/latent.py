@@ -153,6 +153,9 @@ def prepare_append_rotated(k, v, k_cache, v_cache, page_table, *, rope: RopeSpec
     if packed and n_tokens is None:
         raise ValueError("with row_base, n_tokens is given")
     a = CAppendRotatedArgs()
+    a.rope = rope.to_c()
+    if scaling is not None:
+        a.scaling = scaling.to_c()
 
     def rows(t, name, field):
         _inner(_bf16(t, name), name)
@@ -204,9 +207,6 @@ def prepare_append_rotated(k, v, k_cache, v_cache, page_table, *, rope: RopeSpec
     a.n_chunks, a.n_layers, a.n_tokens, a.n_k_heads, a.k_dim = C, Ln, n, H, D
     # chunks may outgrow the rows of a view: they end where the view does
     a.page_size, a.pt_stride, a.pt_pages, a.n_pool_pages = page_size, _table(page_table, C, 0), page_table.shape[1], n_pages
-    a.rope = rope.to_c()
-    if scaling is not None:
-        a.scaling = scaling.to_c()
     a.chunk_tokens, a.tokens_before, a.row_base = _ptr(chunk_tokens), _ptr(tokens_before), _ptr(row_base)
     a.page_table, a.positions = _ptr(page_table), _ptr(positions)
     a.k, a.v, a.q, a.q_out = _ptr(k), _ptr(v), _ptr(q), _ptr(q_out)
