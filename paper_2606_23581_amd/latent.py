@@ -203,10 +203,10 @@ def prepare_append_rotated(k, v, k_cache, v_cache, page_table, *, rope: RopeSpec
     for t, nm in ((tokens_before, "tokens_before"), (chunk_tokens, "chunk_tokens"), (row_base, "row_base")):
         _typed(t, torch.int32, nm, (C,))
     _typed(status, torch.int32, "status")
-    _device(k, v, q, q_out, k_cache, v_cache, page_table, positions, tokens_before, chunk_tokens, row_base, status)
     a.n_chunks, a.n_layers, a.n_tokens, a.n_k_heads, a.k_dim = C, Ln, n, H, D
     # chunks may outgrow the rows of a view: they end where the view does
     a.page_size, a.pt_stride, a.pt_pages, a.n_pool_pages = page_size, _table(page_table, C, 0), page_table.shape[1], n_pages
+    _device(k, v, q, q_out, k_cache, v_cache, page_table, positions, tokens_before, chunk_tokens, row_base, status)
     a.chunk_tokens, a.tokens_before, a.row_base = _ptr(chunk_tokens), _ptr(tokens_before), _ptr(row_base)
     a.page_table, a.positions = _ptr(page_table), _ptr(positions)
     a.k, a.v, a.q, a.q_out = _ptr(k), _ptr(v), _ptr(q), _ptr(q_out)
@@ -288,9 +288,9 @@ def prepare_expand_latent(cache, w, out, page_table, kv_tokens, *, n_keys: int, 
         raise ValueError(f"{R} requests of {a.n_keys} tokens exceed the {out.shape[0]} rows of out")
     _typed(kv_tokens, torch.int32, "kv_tokens", (R,)), _typed(row_base, torch.int32, "row_base", (R,))
     _typed(status, torch.int32, "status")
-    _device(cache, w, out, page_table, kv_tokens, row_base, status)
     a.n_requests, a.n_heads, a.page_size, a.n_pool_pages = R, out.shape[1], page_size, n_pages
     a.pt_stride = _table(page_table, R, a.n_keys, page_size)
+    _device(cache, w, out, page_table, kv_tokens, row_base, status)
     a.kv_tokens, a.row_base, a.page_table = _ptr(kv_tokens), _ptr(row_base), _ptr(page_table)
     a.cache, a.out, a.status = _ptr(cache), _ptr(out), _ptr(status)
     a.cache_stride[0:2], a.out_stride[0:2] = cache.stride()[:2], out.stride()[:2]
