@@ -39,7 +39,7 @@ def _run(cmd, verbose):
 DEVICE_SOURCES = ("kamera_kernels.hip", "kamera_rows.hip", "kamera_patch.hip", "kamera_tridiag.hip",
                   "kamera_tables.hip", "kamera_append.hip", "kamera_select.hip", "kamera_attend.hip",
                   "kamera_attend_tiles.hip", "kamera_rotate.hip", "kamera_project.hip", "kamera_attend_latent.hip",
-                  "kamera_attend_expanded.hip")
+                  "kamera_attend_expanded.hip", "kamera_mla_join.hip")
 HOST_SOURCES = ("kamera_abi.cpp", "kamera_cache.cpp", "kamera_latent.cpp")
 
 

@@ -43,7 +43,7 @@ __global__ __launch_bounds__(kExpThreads, 2) void attend_expanded_kernel(MlaPara
   if (wg >= n_wgs) return;
   Share share;
   if (p.n_parts > 0) {
-    share = divide<kTileKeys, kExpThreads>(p, wg, reinterpret_cast<int*>(s_buf));
+    share = divide<kTileKeys>(p, wg);
   } else {
     share.task = p.n_tasks - 1 - wg;               // late row blocks, which see the most keys, first
     share.skip = 0;

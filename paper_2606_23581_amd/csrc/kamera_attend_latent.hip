@@ -28,7 +28,6 @@ namespace kamera {
 namespace {
 
 constexpr int kStepKeys = 32;
-constexpr int kJoinThreads = 256;
 
 __device__ __forceinline__ uint32_t twist(uint32_t key) {
   return ((key >> 1) & 1) << 2 | ((key >> 2) & 1) << 1 | ((key >> 3) & 1);
@@ -66,7 +65,7 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
 
   Share share;
   if (p.n_parts > 0) {
-    share = divide<kUnit, kThr>(p, blockIdx.x, reinterpret_cast<int*>(s_buf));
+    share = divide<kUnit>(p, blockIdx.x);
   } else {
     share.task = p.n_tasks - 1 - blockIdx.x;       // late row blocks, which see the most keys, first
     share.skip = 0;
@@ -329,97 +328,6 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
       });
     }
   }
-}
-
-// Joins the parts of each row: with M the largest of the parts' maxima m_s,
-// out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.  A workgroup takes 128 columns
-// of a row; eight ways of 32 threads take every eighth part and meet in LDS.
-__global__ __launch_bounds__(kJoinThreads) void mla_join_kernel(MlaParams) {
-  const MlaParams& p = kernel_params<MlaParams>();
-  constexpr int kWays = 8, kChunk = 4;
-  __shared__ f32x4 s_o[kWays][32];
-  __shared__ float s_ml[kWays][3];
-  const int tid = threadIdx.x, col = tid & 31, way = tid >> 5;
-  const int quarters = p.dim >> 7 > 0 ? p.dim >> 7 : 1;
-  const int cq = blockIdx.y % quarters, rr = blockIdx.y / quarters;
-  const uint32_t task = blockIdx.x;
-  const int u0 = p.prefix[task], u1 = p.prefix[task + 1], per = p.prefix[p.n_tasks + 1];
-  if (u1 <= u0) return;
-  const int w0 = u0 / per, w1 = (u1 - 1) / per;
-  if (w0 == w1) return;                            // one workgroup had it all
-  const Block blk = block_of(p, task);
-  const int row = blk.row_first + rr;
-  if (row >= blk.row_end) return;
-  const int c0 = cq * 128 + col * 4;
-  const bool there = c0 < p.dim;
-  // the first part lies in its workgroup's first segment only where that begins with it
-  const int first_slot = u0 == w0 * per ? 0 : 1;
-
-  float top = kLow, l = 0.f, lx = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = w0 + way; s0 <= w1; s0 += kChunk * kWays) {
-    f32x4 ml[kChunk], o[kChunk];
-#pragma unroll
-    for (int k = 0; k < kChunk; ++k) {
-      const int s = min(s0 + k * kWays, w1);       // one past the end is read again and left out
-      const int64_t at = ((int64_t)s * 2 + (s == w0 ? first_slot : 0)) * p.rows_block + rr;
-      ml[k] = *reinterpret_cast<const f32x4*>(p.part_ml + at * 4);
-      o[k] = there ? *reinterpret_cast<const f32x4*>(p.part_o + at * p.dim + c0) : f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    float m = top;
-#pragma unroll
-    for (int k = 0; k < kChunk; ++k) m = fmaxf(m, ml[k].x);
-    const float down = exp2_fast(top - m);
-    top = m;
-    l *= down;
-    lx *= down;
-    acc *= down;
-#pragma unroll
-    for (int k = 0; k < kChunk; ++k)
-      if (s0 + k * kWays <= w1) {
-        const float f = exp2_fast(ml[k].x - top);
-        l += ml[k].y * f;
-        lx += ml[k].z * f;
-        acc += o[k] * f;
-      }
-  }
-  s_o[way][col] = acc;
-  if (col == 0) {
-    s_ml[way][0] = top;
-    s_ml[way][1] = l;
-    s_ml[way][2] = lx;
-  }
-  __syncthreads();
-  if (way != 0) return;
-  const float own = top;
-#pragma unroll
-  for (int k = 1; k < kWays; ++k) top = fmaxf(top, s_ml[k][0]);
-  const float down = exp2_fast(own - top);
-  l *= down;
-  lx *= down;
-  acc *= down;
-#pragma unroll
-  for (int k = 1; k < kWays; ++k) {
-    const float f = exp2_fast(s_ml[k][0] - top);
-    l += s_ml[k][1] * f;
-    lx += s_ml[k][2] * f;
-    acc += s_o[k][col] * f;
-  }
-  const int64_t row0 = p.q_base != nullptr ? (int64_t)p.q_base[blk.r] : (int64_t)blk.r * p.n_queries;
-  const int i = (int)fast_div((uint32_t)row, p.fd_group);
-  const int64_t hq = blk.h * p.group + row - i * p.group;
-  acc *= l == 0.f ? 0.f : 1.0f / l;
-  if (there)
-    *reinterpret_cast<u32x2*>(p.out + (row0 + i) * p.out_s[0] + hq * p.out_s[1] + c0) =
-        u32x2{pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w)};
-  if (cq == 0 && col == 0 && p.lse != nullptr) p.lse[(row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] = row_lse(top, lx);
-}
-
-hipError_t launch_mla_join(const MlaParams& p, hipStream_t s) {
-  const int quarters = p.dim >> 7 > 0 ? p.dim >> 7 : 1;
-  const int rows = (int)((int64_t)p.n_queries * p.group < p.rows_block ? (int64_t)p.n_queries * p.group : p.rows_block);
-  hipLaunchKernelGGL(mla_join_kernel, dim3((uint32_t)p.n_tasks, (uint32_t)(rows * quarters)), dim3(kJoinThreads), 0, s, p);
-  return hipGetLastError();
 }
 
 namespace {

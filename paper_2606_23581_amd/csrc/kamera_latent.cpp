@@ -400,7 +400,7 @@ int size_mla(const AttendSizes& a, kamera::MlaParams& P, bool& launch, int64_t& 
   if (P.n_parts > 0) {
     workspace = bounded_product({P.n_parts, 2, P.rows_block, a.dim + 4, 4});
     if (workspace < 0) return fail(KAMERA_ERR_RANGE, "%s: workspace too large", who);
-    workspace += ceil_div((tasks + 2) * 4, 16) * 16;
+    workspace += ceil_div((tasks + 2 + P.n_parts) * 4, 16) * 16;
   }
   launch = true;
   return KAMERA_OK;

@@ -94,7 +94,7 @@ struct MlaParams {
   float* part_o;                     // [workgroup][2][rows of a block][columns] unnormalised sums
   float* part_ml;                    // [workgroup][2][rows of a block][4] running maximum (in powers of 2), sum of
                                      // the rounded weights, sum of the weights
-  int32_t* prefix;                   // [n_tasks + 1] units before each task, then the units of a workgroup
+  int32_t* prefix;                   // [n_tasks + 1] units before each task, units of a workgroup, [n_parts] first tasks
   uint32_t* status;
   int64_t q_s[2], out_s[2], lse_s[2];
   int64_t pool_s[2];                 // bytes: page, token

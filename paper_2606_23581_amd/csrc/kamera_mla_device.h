@@ -97,54 +97,48 @@ struct Share {
 };
 
 // The tasks' units, divided evenly: workgroup w takes the w-th range of `per` units.
-// Every workgroup adds up all tasks' units (a few loads a thread); the first one
-// leaves the sums for the kernel that joins the parts.  scratch: [blockDim + 4] of LDS.
-template <int UNIT, int THREADS>
-__device__ __forceinline__ Share divide(const MlaParams& p, uint32_t w, int* scratch) {
-  const int tid = threadIdx.x, each = (p.n_tasks + THREADS - 1) / THREADS;
-  const int t0 = min(tid * each, p.n_tasks), t1 = min(t0 + each, p.n_tasks);
+// Every wave adds up all tasks' units, some a lane (a few loads and shuffles, no
+// barrier); the first workgroup leaves the sums, and each its first task, for the kernel
+// that joins the parts.
+template <int UNIT>
+__device__ __forceinline__ Share divide(const MlaParams& p, uint32_t w) {
+  const int lane = threadIdx.x & 63, each = (p.n_tasks + 63) / 64;
+  const int t0 = min(lane * each, p.n_tasks), t1 = min(t0 + each, p.n_tasks);
   int sum = 0;
   for (int t = t0; t < t1; ++t) sum += units_of<UNIT>(block_of(p, t));
-  scratch[tid] = sum;
-  __syncthreads();
-  // inclusive sums: doubling distances
-  int x = sum;
+  int x = sum;                                     // inclusive sums over the lanes
 #pragma unroll
-  for (int d = 1; d < THREADS; d *= 2) {
-    const int y = tid >= d ? scratch[tid - d] : 0;
-    __syncthreads();
-    x += y;
-    scratch[tid] = x;
-    __syncthreads();
+  for (int d = 1; d < 64; d *= 2) {
+    const int y = __shfl_up(x, d);
+    x += lane >= d ? y : 0;
   }
-  const int total = scratch[THREADS - 1];
+  const int total = __builtin_amdgcn_readlane(x, 63);
   const int per = max((total + p.n_parts - 1) / p.n_parts, p.min_units);
   const int64_t begin = (int64_t)w * per;
-  int at = x - sum;                                // units before this thread's tasks
-  if (tid == 0) scratch[THREADS] = p.n_tasks;
-  __syncthreads();
-  if (w == 0 || (begin >= at && begin < x)) {
+  int at = x - sum, task = p.n_tasks, skip = 0;    // units before this lane's tasks
+  const bool mine = begin >= at && begin < x, first = w == 0 && threadIdx.x < 64;
+  if (mine || first) {
     for (int t = t0; t < t1; ++t) {
-      const int u = units_of<UNIT>(block_of(p, t));
-      if (w == 0) p.prefix[t] = at;
+      const int u = each == 1 ? sum : units_of<UNIT>(block_of(p, t));
+      if (first) p.prefix[t] = at;
       if (begin >= at && begin < at + u) {
-        scratch[THREADS] = t;
-        scratch[THREADS + 1] = (int)(begin - at);
+        task = t;
+        skip = (int)(begin - at);
       }
       at += u;
     }
   }
-  if (w == 0 && tid == 0) {
+  const uint64_t found = __ballot(mine);
+  const int from = found != 0 ? __builtin_ctzll(found) : 0;
+  Share s;
+  s.task = (uint32_t)__builtin_amdgcn_readlane(task, from);
+  s.skip = __builtin_amdgcn_readlane(skip, from);
+  s.units = begin >= total ? 0 : (int)min((int64_t)per, total - begin);
+  if (first && lane == 0) {
     p.prefix[p.n_tasks] = total;
     p.prefix[p.n_tasks + 1] = per;
   }
-  __syncthreads();
-  Share s;
-  s.task = (uint32_t)__builtin_amdgcn_readfirstlane(scratch[THREADS]);
-  s.skip = __builtin_amdgcn_readfirstlane(scratch[THREADS + 1]);
-  s.units = begin >= total ? 0 : (int)min((int64_t)per, total - begin);
-  s.units = __builtin_amdgcn_readfirstlane(s.units);
-  __syncthreads();
+  if (threadIdx.x == 0) p.prefix[p.n_tasks + 2 + w] = (int)s.task;
   return s;
 }
 
