@@ -18,6 +18,9 @@ ARCH = "gfx950"
 # hipcc -O3 forms packed-fp32 instructions from plain float code by itself;
 # keep them out of every device compile.
 NO_PACKED_FP32 = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+# Matrix results stay in ordinary registers where a kernel may use the accumulators' as
+# well: results that are also scaled would be copied to and fro at every step.
+MORE_FLAGS = {"kamera_attend_latent.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _hipcc() -> str:
@@ -54,7 +57,7 @@ def build(verbose: bool = False, save_temps: bool = False) -> str:
     cmds, objs = [], []
     for src in DEVICE_SOURCES:
         obj = os.path.join(BUILD, os.path.splitext(src)[0] + ".o")
-        cmd = [hipcc, "-c", "-O3", f"--offload-arch={ARCH}", *NO_PACKED_FP32, *common,
+        cmd = [hipcc, "-c", "-O3", f"--offload-arch={ARCH}", *NO_PACKED_FP32, *common, *MORE_FLAGS.get(src, ()),
                "-Wno-unused-command-line-argument", os.path.join(CSRC, src), "-o", obj]
         if save_temps:
             cmd.insert(2, "-save-temps=obj")

@@ -85,37 +85,9 @@ __global__ __launch_bounds__(kExpThreads, 2) void attend_expanded_kernel(MlaPara
     units -= take;
     const int tile0 = blk.lo / kTileKeys + skip;
     const int part_begin = blk.lo >> 4, part_end = (blk.hi >> 4) + 1;
-    const int64_t key_row = p.kv_base != nullptr ? (int64_t)p.kv_base[blk.r] : (int64_t)blk.r * p.n_keys;
+    const int64_t key_row = first_row(p.kv_base, blk.r, p.n_keys);
     const uint64_t k_head = (uint64_t)p.k + key_row * p.k_s[0] + blk.h * p.k_s[1];
     const uint64_t v_head = (uint64_t)p.v + key_row * p.v_s[0] + blk.h * p.v_s[1];
-
-    const int wave_row = blk.row_first + wave * 32, row = wave_row + c32;
-    const int64_t row0 = p.q_base != nullptr ? (int64_t)p.q_base[blk.r] : (int64_t)blk.r * p.n_queries;
-    bf16x8 qf[KS + RS];
-    int row_lo = INT32_MAX;                        // sees the keys row_lo .. row_lo + row_span; none past the end
-    uint32_t row_span = 0;
-    {
-      const bool there = row < blk.row_end;
-      const int last = mla_last_key(p, blk.n, blk.kv, row);
-      if (there && last >= 0 && blk.kv > 0) {
-        row_lo = mla_first_key(p, last);
-        row_span = (uint32_t)(min(last, blk.kv - 1) - row_lo);
-      }
-      const uint16_t* src = p.q + (row0 + row) * p.q_s[0] + blk.h * p.q_s[1] + hf * 8;
-#pragma unroll
-      for (int ks = 0; ks < KS + RS; ++ks) {
-        u32x4 x = {0u, 0u, 0u, 0u};
-        if (there) x = *reinterpret_cast<const u32x4*>(src + ks * 16) ^ p.q_sign;
-        qf[ks] = __builtin_bit_cast(bf16x8, x);
-      }
-    }
-    f32x16 o[DT];
-    float m = kLow, l = 0.f, l1 = 0.f, lx = 0.f;
-    bool odd = false;                              // a value that is not finite was left out of a product
-#pragma unroll
-    for (int b = 0; b < DT; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
 
     // parts looked up 16 tiles at a time: lane i has part i % 4 of tile i / 4 of the batch
     auto batch = [&](int it) {
@@ -142,22 +114,52 @@ __global__ __launch_bounds__(kExpThreads, 2) void attend_expanded_kernel(MlaPara
       } else {
         const bool there = (ok >> wave) & 1;
         const uint64_t zero = (uint64_t)g_zero_row;
-#pragma unroll
+        auto place = [&](int key, uint64_t at) { return there && key >= blk.lo && key <= blk.hi ? at : zero; };
+#pragma unroll 1
         for (int j = 0; j < NL; ++j) {
-          const int key = first + RPL * j + opaque(lane) / (kRowB / 16);
-          const bool seen = there && key >= blk.lo && key <= blk.hi;
-          load_lds(seen ? kb + k_off[j] : zero, to + (wave * NL + j) * 1024);
-          load_lds(seen ? vb + v_off[j] : zero, to + kVAt + (wave * NL + j) * 1024);
+          const uint32_t in_part = RPL * j + lane / (kRowB / 16), c = lane % (kRowB / 16);
+          const uint32_t kc = c ^ (D == 128 ? in_part & 15 : (in_part >> 1) & 7);
+          const uint32_t vc = c ^ (D == 128 ? (in_part & 3) << 2 : (in_part & 2) << 1);
+          load_lds(place(first + in_part, kb + in_part * k_stride) + kc * 16, to + (wave * NL + j) * 1024);
+          load_lds(place(first + in_part, vb + in_part * v_stride) + vc * 16, to + kVAt + (wave * NL + j) * 1024);
         }
-#pragma unroll
+#pragma unroll 1
         for (int j = 0; j < 2; ++j) {
-          const int key = first + 8 * j + (opaque(lane) >> 3);
-          const bool seen = there && key >= blk.lo && key <= blk.hi;
-          load_lds(seen ? rope + r_off[j] : zero, to + kRAt + (wave * 2 + j) * 1024);
+          const uint32_t in_part = 8 * j + (lane >> 3);
+          load_lds(place(first + in_part, rope + in_part * t_stride) + (((lane & 7) ^ ((in_part >> 1) & 7)) << 4),
+                   to + kRAt + (wave * 2 + j) * 1024);
         }
       }
       return ok;
     };
+
+    uint32_t ok = issue(0);
+
+    // this wave's rows; lane l has row l % 32 (past the end the last one, whose results
+    // are not stored)
+    const int wave_row = blk.row_first + wave * 32, row = min(wave_row + c32, blk.row_end - 1);
+    const int64_t row0 = first_row(p.q_base, blk.r, p.n_queries);
+    bf16x8 qf[KS + RS];
+    int row_lo = INT32_MAX;                        // sees the keys row_lo .. row_lo + row_span, or none
+    uint32_t row_span = 0;
+    {
+      const int last = mla_last_key(p, blk.n, blk.kv, row);
+      if (last >= 0 && blk.kv > 0) {
+        row_lo = mla_first_key(p, last);
+        row_span = (uint32_t)(min(last, blk.kv - 1) - row_lo);
+      }
+      const uint16_t* src = p.q + (row0 + row) * p.q_s[0] + blk.h * p.q_s[1] + hf * 8;
+#pragma unroll
+      for (int ks = 0; ks < KS + RS; ++ks)
+        qf[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(src + ks * 16) ^ p.q_sign);
+    }
+    f32x16 o[DT];
+    float m = kLow, l = 0.f, l1 = 0.f, lx = 0.f;
+    bool odd = false;                              // a value that is not finite was left out of a product
+#pragma unroll
+    for (int b = 0; b < DT; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
 
     // Scores and softmax of a tile; the weights as the second product takes them.
     auto weigh = [&](int pos, uint32_t buf, uint32_t ok, bf16x8 (&pf)[4]) {
@@ -230,7 +232,6 @@ __global__ __launch_bounds__(kExpThreads, 2) void attend_expanded_kernel(MlaPara
         }
     };
 
-    uint32_t ok = issue(0);
     for (int it = 0; it < take; ++it) {
       vm_wait<0>();
       lds_barrier();                               // the tile is there, and the other buffer is free
@@ -261,7 +262,7 @@ __global__ __launch_bounds__(kExpThreads, 2) void attend_expanded_kernel(MlaPara
     const bool direct = skip == 0 && take == total;
     const int64_t part = ((int64_t)wg * 2 + (segment > 0 ? 1 : 0)) * p.rows_block, at = part + wave * 32 + c32;
     ++segment;
-    if (row < blk.row_end) {
+    if (wave_row + c32 < blk.row_end) {
       if (direct) {
         const float inv = l == 0.f ? 0.f : 1.0f / l;
         uint16_t* dst = p.out + (row0 + row) * p.out_s[0] + blk.h * p.out_s[1] + 4 * hf;

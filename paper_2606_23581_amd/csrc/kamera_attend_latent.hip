@@ -28,6 +28,7 @@ namespace kamera {
 namespace {
 
 constexpr int kStepKeys = 32;
+constexpr int kMfma = 0x8, kDsRead = 0x100;        // instruction groups of the scheduler
 
 __device__ __forceinline__ uint32_t twist(uint32_t key) {
   return ((key >> 1) & 1) << 2 | ((key >> 2) & 1) << 1 | ((key >> 3) & 1);
@@ -42,6 +43,22 @@ __device__ __forceinline__ float sum_x16(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// The order of N products, each of READS operand reads: kAhead products' reads before
+// the first one.
+template <int N, int READS, int kAhead>
+__device__ __forceinline__ void pipeline() {
+  __builtin_amdgcn_sched_group_barrier(kDsRead, kAhead * READS, 0);
+#pragma unroll
+  for (int i = 0; i < N - kAhead; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kDsRead, READS, 0);
+    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(kMfma, kAhead, 0);
+}
+
+// Columns of the groups' results that fit the slots at a time.
+constexpr int latent_join_cols(int lat, int rw) { return lat * latent_waves(rw) > 2048 ? lat / 2 : lat; }
+
 }  // namespace
 
 template <int LAT, int RW>
@@ -53,9 +70,10 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
   constexpr int LPG = CH / 8;                      // loads of a wave for 8 keys
   constexpr int LW = RW < 4 ? RW : 4;              // waves that load a step's keys (of 8, those take turns)
   constexpr int NA = 4 / LW;                       // groups of 8 keys that a wave loads
-  constexpr int kPad = 132;                        // floats of a row of the epilogue's tile
+  constexpr int kAhead = NW == 4 ? 6 : 4;          // products whose operands are read ahead
+  constexpr int kCols = latent_join_cols(LAT, RW), kPad = kCols + 4;   // the epilogue's tile: columns, floats of a row
   static_assert(kUnit == 32 * KW && NB >= 1, "");
-  extern __shared__ u32x4 s_buf[];
+  extern __shared__ __attribute__((aligned(128))) u32x4 s_buf[];
   __shared__ float s_ml[NW][16][3];
   __shared__ int s_odd;                            // a value that is not finite was left out of a product
   const uint32_t lds = lds_offset(s_buf);
@@ -82,14 +100,9 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
     flip |= (c & 1) << b;
   }
   // places of the operands in a slot: chunk 4 s + g of key c16, and of keys 4 g ..
-  uint32_t k_at[2], v_at[4];
-#pragma unroll
-  for (int s = 0; s < 2; ++s) k_at[s] = c16 * kRowB + (((4 * s + g) ^ twist(c16)) << 4);
-#pragma unroll
-  for (int b = 0; b < 4; ++b) {
-    const uint32_t key = 4 * g + (c16 >> 2), c = 2 * b + ((c16 & 3) >> 1);
-    v_at[b] = key * kRowB + ((c ^ twist(key)) << 4) + (c16 & 1) * 8;
-  }
+  // (rows and slots are multiples of 128 bytes, so that chunks are exchanged in the address)
+  const uint32_t k_at = c16 * kRowB + ((g ^ twist(c16)) << 4), v_key = 4 * g + (c16 >> 2);
+  const uint32_t v_at = v_key * kRowB + ((((c16 & 3) >> 1) ^ twist(v_key)) << 4) + (c16 & 1) * 8;
 
   uint32_t task = share.task;
   int skip = share.skip, units = share.units, segment = 0;
@@ -101,41 +114,12 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
     const int key0 = (blk.lo / kUnit + skip) * kUnit + kg * kStepKeys;   // the group's keys of the first unit
     const int part_begin = blk.lo >> 4, part_end = (blk.hi >> 4) + 1;
 
-    // this wave's rows; lane l has row l % 16
-    const int wave_row = blk.row_first + wr * 16, row = wave_row + c16;
-    const int64_t row0 = p.q_base != nullptr ? (int64_t)p.q_base[blk.r] : (int64_t)blk.r * p.n_queries;
-    const int query = (int)fast_div((uint32_t)row, p.fd_group);
-    bf16x8 qf[KS];
-    int row_lo = INT32_MAX;                        // sees the keys row_lo .. row_lo + row_span; none past the end
-    uint32_t row_span = 0;
-    {
-      const bool there = row < blk.row_end;
-      const int last = mla_last_key(p, blk.n, blk.kv, query);
-      if (there && last >= 0 && blk.kv > 0) {
-        row_lo = mla_first_key(p, last);
-        row_span = (uint32_t)(min(last, blk.kv - 1) - row_lo);
-      }
-      const uint16_t* src = p.q + (row0 + query) * p.q_s[0] + (int64_t)(row - query * p.group) * p.q_s[1] + g * 8;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        u32x4 x = {0u, 0u, 0u, 0u};
-        if (there) x = *reinterpret_cast<const u32x4*>(src + ks * 32) ^ p.q_sign;
-        qf[ks] = __builtin_bit_cast(bf16x8, x);
-      }
-    }
-    f32x4 o[DT];
-    float m = kLow, l = 0.f, lx = 0.f;
-#pragma unroll
-    for (int b = 0; b < DT; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
-
     // pages looked up 32 steps at a time: lane i has part i % 2 of step i / 2 of the batch
     auto batch = [&](int it) {
       const int at = it + (lane >> 1);
       return fetch_pool_parts(p, blk.r, at < take ? ((key0 + at * kUnit) >> 4) + (lane & 1) : -1, part_begin, part_end);
     };
     PoolParts parts = batch(0);
-    if (tid == 0) s_odd = 0;
-    lds_barrier();
     auto slot_of = [&](int it) { return lds + (kg * NB + (NB > 1 ? it % NB : 0)) * kSlot; };
 
     // Step it's keys into its slot: the wave's share of them.  The result: which of its
@@ -144,40 +128,84 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
       if (it > 0 && (it & 31) == 0) parts = batch(it);
       const uint32_t ok = (uint32_t)(parts.ok >> (2 * (it & 31))) & 3u;
       if (RW == 8 && ((wave >> 2) ^ it) & 1) return ok;
-      const int pos = key0 + it * kUnit;
-      const bool whole = ok == 3u && pos >= blk.lo && pos + kStepKeys - 1 <= blk.hi;
+      const int pos = key0 + it * kUnit, first = (wr % LW) * NA * 8;       // first key that the wave loads
+      const uint32_t to = slot_of(it) + first * kRowB;
+      if (ok == 3u && pos >= blk.lo && pos + kStepKeys - 1 <= blk.hi) {
 #pragma unroll
-      for (int a = 0; a < NA; ++a) {
-        const int first = ((wr % LW) * NA + a) * 8;                // its first key in the step
-        const uint32_t odd = (first >> 3) & 1, to = slot_of(it) + first * kRowB;
-        const uint64_t base = lane_u64(parts.at, 2 * (it & 31) + (first >> 4)) + odd * (8 * (uint64_t)t_stride);
+        for (int a = 0; a < NA; ++a) {
+          const uint32_t odd = (first >> 3) + a & 1;
+          const uint64_t base = lane_u64(parts.at, 2 * (it & 31) + ((first + 8 * a) >> 4)) + odd * (8 * (uint64_t)t_stride);
 #pragma unroll
-        for (int b = 0; b < LPG; ++b) {
-          const uint32_t at = off[b] + odd * (16 - ((flip >> b) & 1) * 32);
-          if (whole) {
-            load_lds((const uint8_t*)base, at, to + b * 1024);
-          } else {
-            const uint32_t i = b * 64 + opaque(lane);
-            const int key = pos + first + (int)(i / CH);
-            const bool seen = ((ok >> (first >> 4)) & 1) && key >= blk.lo && key <= blk.hi;
-            load_lds(seen ? base + at : (uint64_t)g_zero_row + (i % CH) * 16, to + b * 1024);
-          }
+          for (int b = 0; b < LPG; ++b)
+            load_lds((const uint8_t*)base, off[b] + odd * (16 - ((flip >> b) & 1) * 32), to + (a * LPG + b) * 1024);
+        }
+      } else {
+        const uint64_t part0 = lane_u64(parts.at, 2 * (it & 31)), part1 = lane_u64(parts.at, 2 * (it & 31) + 1);
+#pragma unroll 1
+        for (int j = 0; j < NA * LPG; ++j) {
+          const uint32_t i = j * 64 + lane, in_step = first + i / CH, c = (i % CH) ^ twist(in_step);
+          const int key = pos + (int)in_step;
+          const bool seen = ((ok >> (in_step >> 4)) & 1) && key >= blk.lo && key <= blk.hi;
+          const uint64_t row = (in_step >> 4 ? part1 : part0) + (in_step & 15) * t_stride;
+          load_lds((seen ? row : (uint64_t)g_zero_row) + c * 16, to + j * 1024);
         }
       }
       return ok;
     };
+    uint32_t oks = 0;                              // two bits a slot
+#pragma unroll
+    for (int i = 0; i < (NB > 1 ? NB - 1 : 1); ++i)
+      if (i < take) oks |= issue(i) << (2 * i);
+
+    // this wave's rows; lane l has row l % 16 (past the end the last one, whose results
+    // are not stored)
+    const int wave_row = blk.row_first + wr * 16, row = min(wave_row + c16, blk.row_end - 1);
+    const int64_t row0 = first_row(p.q_base, blk.r, p.n_queries);
+    const int query = (int)fast_div((uint32_t)row, p.fd_group);
+    bf16x8 qf[KS];
+    int row_lo = INT32_MAX;                        // sees the keys row_lo .. row_lo + row_span, or none
+    uint32_t row_span = 0;
+    {
+      const int last = mla_last_key(p, blk.n, blk.kv, query);
+      if (last >= 0 && blk.kv > 0) {
+        row_lo = mla_first_key(p, last);
+        row_span = (uint32_t)(min(last, blk.kv - 1) - row_lo);
+      }
+      const uint16_t* src = p.q + (row0 + query) * p.q_s[0] + (int64_t)(row - query * p.group) * p.q_s[1] + g * 8;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) qf[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(src + ks * 32) ^ p.q_sign);
+    }
+    f32x4 o[DT];
+    float m = kLow, l = 0.f, lx = 0.f;
+#pragma unroll
+    for (int b = 0; b < DT; ++b) o[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (tid == 0) s_odd = 0;
+    lds_barrier();
 
     // Scores and softmax of a step; the weights as the second product takes them.
     auto weigh = [&](int pos, uint32_t slot, uint32_t ok) {
+      if constexpr (NW == 4) {                     // the queries in the accumulators' registers, of which there are enough
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+a"(qf[ks]));
+#pragma unroll
+        for (int b = 0; b < DT; ++b) asm volatile("" : "+v"(o[b]));
+      }
       f32x4 sc[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) sc[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+      // operand i of 2 KS: inner step i / 2, keys 16 (i % 2) on; read kAhead products ahead
+      auto rows = [&](int i) {
+        return read_chunk(((slot + k_at) ^ ((i >> 1 & 1) << 6)) + (i >> 2) * 128 + (i & 1) * 16 * kRowB);
+      };
+      bf16x8 kf[2 * KS];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
+      for (int i = 0; i < kAhead; ++i) kf[i] = rows(i);
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-          sc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(read_chunk(slot + k_at[ks & 1] + (ks >> 1) * 128 + u * 16 * kRowB),
-                                                          qf[ks], sc[u], 0, 0, 0);
+      for (int i = 0; i < 2 * KS; ++i) {
+        if (i + kAhead < 2 * KS) kf[i + kAhead] = rows(i + kAhead);
+        sc[i & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[i], qf[i >> 1], sc[i & 1], 0, 0, 0);
+      }
+      pipeline<2 * KS, 1, kAhead>();
 
       float x[8];
 #pragma unroll
@@ -208,11 +236,19 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
       return __builtin_bit_cast(bf16x8, w);
     };
     auto gather = [&](uint32_t slot, bf16x8 pf) {
+      auto columns = [&](int b) {
+        const uint32_t at = ((slot + v_at) ^ ((b & 3) << 5)) + (b >> 2) * 128;
+        return join(read_columns(at), read_columns(at + 16 * kRowB));
+      };
+      bf16x8 vf[DT];
+#pragma unroll
+      for (int b = 0; b < kAhead; ++b) vf[b] = columns(b);
 #pragma unroll
       for (int b = 0; b < DT; ++b) {
-        const uint32_t at = slot + v_at[b & 3] + (b >> 2) * 128;
-        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join(read_columns(at), read_columns(at + 16 * kRowB)), pf, o[b], 0, 0, 0);
+        if (b + kAhead < DT) vf[b + kAhead] = columns(b + kAhead);
+        o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[b], pf, o[b], 0, 0, 0);
       }
+      pipeline<DT, 2, kAhead>();
     };
     // The values of a group's slot without what is not finite, by its RW waves.
     auto clean = [&](uint32_t slot) {
@@ -226,23 +262,18 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
 
     if constexpr (NB == 1) {
       // a wave's keys are its own: no one else waits for them
-      uint32_t ok = issue(0);
       for (int it = 0; it < take; ++it) {
         const int pos = key0 + it * kUnit;
         vm_wait<0>();
         if (busy(pos)) {
-          const bf16x8 pf = weigh(pos, slot_of(it), ok);
+          const bf16x8 pf = weigh(pos, slot_of(it), oks);
           if (mixed(blk, pos, kStepKeys)) clean(slot_of(it));
           gather(slot_of(it), pf);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (it + 1 < take) ok = issue(it + 1);
+        if (it + 1 < take) oks = issue(it + 1);
       }
     } else {
-      uint32_t oks = 0;                            // two bits a slot
-#pragma unroll
-      for (int i = 0; i < NB - 1; ++i)
-        if (i < take) oks |= issue(i) << (2 * i);
       for (int it = 0; it < take; ++it) {
         // the wave's loads of the NB - 2 steps behind this one may be under way (half of
         // them where waves load in turn)
@@ -263,60 +294,74 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
       }
     }
 
-    // the groups' results are joined 128 columns at a time
     l = sum_x32(sum_x16(l));
     lx = sum_x32(sum_x16(lx));
-    lds_barrier();
-    if (g == 0) {
-      s_ml[wave][c16][0] = m;
-      s_ml[wave][c16][1] = l;
-      s_ml[wave][c16][2] = lx;
-    }
-    lds_barrier();
-    const bool odd = __builtin_amdgcn_readfirstlane(s_odd) != 0;   // cleared for the next task behind the barriers below
-    float top = kLow;
-#pragma unroll
-    for (int k = 0; k < KW; ++k) top = fmaxf(top, s_ml[k * RW + wr][c16][0]);
-    const float down = exp2_fast(m - top);
-    float* tile = reinterpret_cast<float*>(s_buf);
     const bool direct = skip == 0 && take == total;
     const int64_t part = ((int64_t)blockIdx.x * 2 + (segment > 0 ? 1 : 0)) * p.rows_block;
     ++segment;
+    // Four columns of a row, and its maximum and sums, to where they belong.
+    auto store = [&](int out_row, int col, f32x4 a, float mm, float ll, float lxx) {
+      if (direct) {
+        const int i = (int)fast_div((uint32_t)out_row, p.fd_group);
+        const int64_t hq = out_row - i * p.group;
+        const float inv = ll == 0.f ? 0.f : 1.0f / ll;
+        *reinterpret_cast<u32x2*>(p.out + (row0 + i) * p.out_s[0] + hq * p.out_s[1] + col) =
+            u32x2{pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv)};
+        if (p.lse != nullptr && col == 0) p.lse[(row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] = row_lse(mm, lxx);
+      } else {
+        const int64_t at = part + out_row - blk.row_first;
+        *reinterpret_cast<f32x4*>(p.part_o + at * LAT + col) = a;
+        if (col == 0) *reinterpret_cast<f32x4*>(p.part_ml + at * 4) = f32x4{mm, ll, lxx, 0.f};
+      }
+    };
+    lds_barrier();                                 // the slots are free
+    const bool odd = __builtin_amdgcn_readfirstlane(s_odd) != 0;   // cleared for the next task behind a barrier below
+    if constexpr (KW == 1) {
+      if (wave_row + c16 < blk.row_end) {
 #pragma unroll
-    for (int cq = 0; cq < DT / 8; ++cq) {
-#pragma unroll
-      for (int b = 0; b < 8; ++b) *reinterpret_cast<f32x4*>(tile + (wave * 16 + c16) * kPad + b * 16 + 4 * g) = o[cq * 8 + b] * down;
-      lds_barrier();
-      for (int j = tid >> 5; j < RW * 16; j += kThr / 32) {
-        const int col = (tid & 31) * 4, w0 = j >> 4, at = j & 15;
-        const int out_row = blk.row_first + j;
-        if (out_row >= blk.row_end) break;
-        f32x4 a = {0.f, 0.f, 0.f, 0.f};
-        float mm = kLow, ll = 0.f, lxx = 0.f;
-#pragma unroll
-        for (int k = 0; k < KW; ++k) {
-          a += *reinterpret_cast<const f32x4*>(tile + ((k * RW + w0) * 16 + at) * kPad + col);
-          mm = fmaxf(mm, s_ml[k * RW + w0][at][0]);
-        }
-#pragma unroll
-        for (int k = 0; k < KW; ++k) {
-          const float f = exp2_fast(s_ml[k * RW + w0][at][0] - mm);
-          ll += s_ml[k * RW + w0][at][1] * f;
-          lxx += s_ml[k * RW + w0][at][2] * f;
-        }
-        if (direct) {
-          const int i = (int)fast_div((uint32_t)out_row, p.fd_group);
-          const int64_t hq = out_row - i * p.group;
-          const float inv = ll == 0.f ? 0.f : 1.0f / ll;
-          *reinterpret_cast<u32x2*>(p.out + (row0 + i) * p.out_s[0] + hq * p.out_s[1] + cq * 128 + col) =
-              u32x2{pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv)};
-          if (p.lse != nullptr && cq == 0 && col == 0) p.lse[(row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] = row_lse(mm, lxx);
-        } else {
-          *reinterpret_cast<f32x4*>(p.part_o + (part + j) * LAT + cq * 128 + col) = a;
-          if (cq == 0 && col == 0) *reinterpret_cast<f32x4*>(p.part_ml + (part + j) * 4) = f32x4{mm, ll, lxx, 0.f};
-        }
+        for (int b = 0; b < DT; ++b) store(wave_row + c16, b * 16 + 4 * g, o[b], m, l, lx);
       }
       lds_barrier();
+    } else {
+      // the groups' results are joined in LDS, kCols columns at a time
+      if (g == 0) {
+        s_ml[wave][c16][0] = m;
+        s_ml[wave][c16][1] = l;
+        s_ml[wave][c16][2] = lx;
+      }
+      lds_barrier();
+      float top = kLow;
+#pragma unroll
+      for (int k = 0; k < KW; ++k) top = fmaxf(top, s_ml[k * RW + wr][c16][0]);
+      const float down = exp2_fast(m - top);
+      float* tile = reinterpret_cast<float*>(s_buf);
+#pragma unroll
+      for (int cq = 0; cq < LAT / kCols; ++cq) {
+#pragma unroll
+        for (int b = 0; b < kCols / 16; ++b)
+          *reinterpret_cast<f32x4*>(tile + (wave * 16 + c16) * kPad + b * 16 + 4 * g) = o[cq * (kCols / 16) + b] * down;
+        lds_barrier();
+        constexpr int kSpan = kThr / (kCols / 4);
+        for (int j = tid / (kCols / 4); j < RW * 16; j += kSpan) {
+          const int col = tid % (kCols / 4) * 4, w0 = j >> 4, at = j & 15;
+          if (blk.row_first + j >= blk.row_end) break;
+          f32x4 a = {0.f, 0.f, 0.f, 0.f};
+          float mm = kLow, ll = 0.f, lxx = 0.f;
+#pragma unroll
+          for (int k = 0; k < KW; ++k) {
+            a += *reinterpret_cast<const f32x4*>(tile + ((k * RW + w0) * 16 + at) * kPad + col);
+            mm = fmaxf(mm, s_ml[k * RW + w0][at][0]);
+          }
+#pragma unroll
+          for (int k = 0; k < KW; ++k) {
+            const float f = exp2_fast(s_ml[k * RW + w0][at][0] - mm);
+            ll += s_ml[k * RW + w0][at][1] * f;
+            lxx += s_ml[k * RW + w0][at][2] * f;
+          }
+          store(blk.row_first + j, cq * kCols + col, a, mm, ll, lxx);
+        }
+        lds_barrier();
+      }
     }
     if (odd) {
       const int from = (blk.lo / kUnit + skip) * kUnit;
@@ -335,7 +380,8 @@ namespace {
 template <int LAT, int RW>
 hipError_t launch_rows(const MlaParams& p, hipStream_t s) {
   static std::atomic<bool> done[kMaxDevices];
-  const int slots = 4 * kStepKeys * (LAT + kRopeCols) * 2, tile = latent_waves(RW) * 16 * 132 * 4;
+  const int slots = 4 * kStepKeys * (LAT + kRopeCols) * 2;
+  const int tile = latent_waves(RW) * 16 * (latent_join_cols(LAT, RW) + 4) * 4;
   const int lds = slots > tile ? slots : tile;
   const hipError_t e = ensure_lds_limit((const void*)attend_latent_kernel<LAT, RW>, lds, done);
   if (e != hipSuccess) return e;

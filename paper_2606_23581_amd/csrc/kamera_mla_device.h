@@ -13,6 +13,18 @@ constexpr float kSlack = 8.0f;                     // by how much (in powers of 
 // v_exp_f32: 2^x, about 1 ulp
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Memory that no kernel writes while this one runs, at a wave-uniform address: a scalar
+// load.
+template <typename T>
+__device__ __forceinline__ T uniform_load(const T* p) {
+  return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
+}
+
+// First row of a request's in q and out, or of its expanded keys.
+__device__ __forceinline__ int64_t first_row(const int32_t* base, int r, int most) {
+  return base != nullptr ? (int64_t)uniform_load(base + r) : (int64_t)r * most;
+}
+
 // The larger of two, NaN if one is.
 __device__ __forceinline__ float max2(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
@@ -56,6 +68,8 @@ __device__ __forceinline__ int mla_first_key(const MlaParams& p, int last) {
   return p.window > 0 ? max(0, last - p.window + 1) : 0;
 }
 
+// UNIFORM: the task is the same for the whole wave, and its lengths are scalar loads.
+template <bool UNIFORM = true>
 __device__ __forceinline__ Block block_of(const MlaParams& p, uint32_t task) {
   Block b;
   uint32_t d = fast_div(task, p.fd_blocks);
@@ -63,8 +77,12 @@ __device__ __forceinline__ Block block_of(const MlaParams& p, uint32_t task) {
   const uint32_t r = fast_div(d, p.fd_heads);
   b.h = (int)(d - r * p.task_heads);
   b.r = (int)r;
-  b.n = p.q_tokens != nullptr ? min(max(p.q_tokens[r], 0), p.n_queries) : p.n_queries;
-  b.kv = min(max(p.kv_tokens[r], 0), p.n_keys);
+  // both at once, without a branch between them
+  const int32_t* q_tokens = p.q_tokens != nullptr ? p.q_tokens : p.kv_tokens;
+  const int n = UNIFORM ? uniform_load(q_tokens + r) : q_tokens[r];
+  const int kv = UNIFORM ? uniform_load(p.kv_tokens + r) : p.kv_tokens[r];
+  b.n = p.q_tokens != nullptr ? min(max(n, 0), p.n_queries) : p.n_queries;
+  b.kv = min(max(kv, 0), p.n_keys);
   const int rows = b.n * p.group;
   b.row_first = b.rb * p.rows_block;
   b.row_end = min(rows, b.row_first + p.rows_block);
@@ -105,7 +123,7 @@ __device__ __forceinline__ Share divide(const MlaParams& p, uint32_t w) {
   const int lane = threadIdx.x & 63, each = (p.n_tasks + 63) / 64;
   const int t0 = min(lane * each, p.n_tasks), t1 = min(t0 + each, p.n_tasks);
   int sum = 0;
-  for (int t = t0; t < t1; ++t) sum += units_of<UNIT>(block_of(p, t));
+  for (int t = t0; t < t1; ++t) sum += units_of<UNIT>(block_of<false>(p, t));
   int x = sum;                                     // inclusive sums over the lanes
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
@@ -119,7 +137,7 @@ __device__ __forceinline__ Share divide(const MlaParams& p, uint32_t w) {
   const bool mine = begin >= at && begin < x, first = w == 0 && threadIdx.x < 64;
   if (mine || first) {
     for (int t = t0; t < t1; ++t) {
-      const int u = each == 1 ? sum : units_of<UNIT>(block_of(p, t));
+      const int u = each == 1 ? sum : units_of<UNIT>(block_of<false>(p, t));
       if (first) p.prefix[t] = at;
       if (begin >= at && begin < at + u) {
         task = t;
@@ -172,13 +190,6 @@ __device__ __forceinline__ uint64_t lane_u64(uint64_t x, int lane) {
 
 // A row of zeros: where a key that no row of a block may see would be loaded.
 static __device__ __attribute__((aligned(16))) uint32_t g_zero_row[(512 + kRopeCols) / 2];
-
-// A lane's value that the compiler does not see through: what is worked out from it
-// stays where it is written, and takes no registers before.
-__device__ __forceinline__ int opaque(int x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
 
 // The keys [pos, pos + n) hold some that a row of the block sees and another does not.
 __device__ __forceinline__ bool mixed(const Block& b, int pos, int n) {

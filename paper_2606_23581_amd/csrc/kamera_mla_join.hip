@@ -96,7 +96,7 @@ __global__ __launch_bounds__(kJoinThreads) void mla_join_kernel(MlaParams) {
       acc += s_o[k][col] * f;
     }
   }
-  const int64_t row0 = p.q_base != nullptr ? (int64_t)p.q_base[blk.r] : (int64_t)blk.r * p.n_queries;
+  const int64_t row0 = first_row(p.q_base, blk.r, p.n_queries);
   const int i = (int)fast_div((uint32_t)row, p.fd_group);
   const int64_t hq = (int64_t)blk.h * p.group + row - i * p.group;
   acc *= l == 0.f ? 0.f : 1.0f / l;
