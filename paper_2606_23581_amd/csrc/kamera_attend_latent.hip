@@ -75,6 +75,7 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
   static_assert(kUnit == 32 * KW && NB >= 1, "");
   extern __shared__ __attribute__((aligned(128))) u32x4 s_buf[];
   __shared__ float s_ml[NW][16][3];
+  __shared__ uint32_t s_off[NW == 8 ? LPG : 1][64];
   __shared__ int s_odd;                            // a value that is not finite was left out of a product
   const uint32_t lds = lds_offset(s_buf);
 
@@ -90,15 +91,21 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
     share.units = units_of<kUnit>(block_of(p, share.task));
   }
 
-  // this lane's pieces of 8 keys that the wave loads: offset from the first one's row
+  // this lane's pieces of 8 keys that the wave loads: offset from the first one's row, and
+  // in bit 0 whether the chunk's number is odd (in LDS where registers are short)
   const uint32_t t_stride = (uint32_t)p.pool_s[1];
-  uint32_t off[LPG], flip = 0;
+  uint32_t off[NW == 8 ? 1 : LPG];
 #pragma unroll
   for (int b = 0; b < LPG; ++b) {
     const uint32_t i = b * 64 + lane, key = i / CH, c = (i % CH) ^ twist(key);
-    off[b] = key * t_stride + c * 16;
-    flip |= (c & 1) << b;
+    const uint32_t x = key * t_stride + c * 16 + (c & 1);
+    if (NW == 8) s_off[NW == 8 ? b : 0][lane] = x;             // every wave writes the same
+    else off[NW == 8 ? 0 : b] = x;
   }
+  auto piece = [&](int b, uint32_t odd) {
+    const uint32_t x = NW == 8 ? s_off[NW == 8 ? b : 0][lane] : off[NW == 8 ? 0 : b];
+    return (x & ~15u) + odd * (16 - (x & 1) * 32);
+  };
   // places of the operands in a slot: chunk 4 s + g of key c16, and of keys 4 g ..
   // (rows and slots are multiples of 128 bytes, so that chunks are exchanged in the address)
   const uint32_t k_at = c16 * kRowB + ((g ^ twist(c16)) << 4), v_key = 4 * g + (c16 >> 2);
@@ -129,6 +136,7 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
       const uint32_t ok = (uint32_t)(parts.ok >> (2 * (it & 31))) & 3u;
       if (RW == 8 && ((wave >> 2) ^ it) & 1) return ok;
       const int pos = key0 + it * kUnit, first = (wr % LW) * NA * 8;       // first key that the wave loads
+      if (pos > blk.hi || pos + kStepKeys <= blk.lo) return ok;            // no row sees any: not looked at
       const uint32_t to = slot_of(it) + first * kRowB;
       if (ok == 3u && pos >= blk.lo && pos + kStepKeys - 1 <= blk.hi) {
 #pragma unroll
@@ -137,7 +145,7 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
           const uint64_t base = lane_u64(parts.at, 2 * (it & 31) + ((first + 8 * a) >> 4)) + odd * (8 * (uint64_t)t_stride);
 #pragma unroll
           for (int b = 0; b < LPG; ++b)
-            load_lds((const uint8_t*)base, off[b] + odd * (16 - ((flip >> b) & 1) * 32), to + (a * LPG + b) * 1024);
+            load_lds((const uint8_t*)base, piece(b, odd), to + (a * LPG + b) * 1024);
         }
       } else {
         const uint64_t part0 = lane_u64(parts.at, 2 * (it & 31)), part1 = lane_u64(parts.at, 2 * (it & 31) + 1);
@@ -299,28 +307,43 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
     const bool direct = skip == 0 && take == total;
     const int64_t part = ((int64_t)blockIdx.x * 2 + (segment > 0 ? 1 : 0)) * p.rows_block;
     ++segment;
-    // Four columns of a row, and its maximum and sums, to where they belong.
-    auto store = [&](int out_row, int col, f32x4 a, float mm, float ll, float lxx) {
+    // Where a row's results belong: looked up before the waits below.
+    struct Place {
+      uint16_t* out;
+      float* part_o;
+      float* lse;
+      float* part_ml;
+    };
+    auto place_of = [&](int out_row, int col) {
+      const int i = (int)fast_div((uint32_t)out_row, p.fd_group);
+      const int64_t hq = out_row - i * p.group, at = part + out_row - blk.row_first;
+      Place d;
+      d.out = p.out + (row0 + i) * p.out_s[0] + hq * p.out_s[1] + col;
+      d.lse = p.lse != nullptr ? p.lse + (row0 + i) * p.lse_s[0] + hq * p.lse_s[1] : nullptr;
+      d.part_o = p.part_o + at * LAT + col;
+      d.part_ml = p.part_ml + at * 4;
+      return d;
+    };
+    // A row's columns, [N] of four `step` apart.
+    auto store = [&](const Place& d, int step, const auto& a, float mm, float ll, float lxx, bool lead) {
+      constexpr int N = sizeof(a) / sizeof(f32x4);
       if (direct) {
-        const int i = (int)fast_div((uint32_t)out_row, p.fd_group);
-        const int64_t hq = out_row - i * p.group;
         const float inv = ll == 0.f ? 0.f : 1.0f / ll;
-        *reinterpret_cast<u32x2*>(p.out + (row0 + i) * p.out_s[0] + hq * p.out_s[1] + col) =
-            u32x2{pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv)};
-        if (p.lse != nullptr && col == 0) p.lse[(row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] = row_lse(mm, lxx);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          *reinterpret_cast<u32x2*>(d.out + n * step) =
+              u32x2{pack_bf16x2(a[n].x * inv, a[n].y * inv), pack_bf16x2(a[n].z * inv, a[n].w * inv)};
+        if (lead && d.lse != nullptr) *d.lse = row_lse(mm, lxx);
       } else {
-        const int64_t at = part + out_row - blk.row_first;
-        *reinterpret_cast<f32x4*>(p.part_o + at * LAT + col) = a;
-        if (col == 0) *reinterpret_cast<f32x4*>(p.part_ml + at * 4) = f32x4{mm, ll, lxx, 0.f};
+#pragma unroll
+        for (int n = 0; n < N; ++n) *reinterpret_cast<f32x4*>(d.part_o + n * step) = a[n];
+        if (lead) *reinterpret_cast<f32x4*>(d.part_ml) = f32x4{mm, ll, lxx, 0.f};
       }
     };
     lds_barrier();                                 // the slots are free
     const bool odd = __builtin_amdgcn_readfirstlane(s_odd) != 0;   // cleared for the next task behind a barrier below
     if constexpr (KW == 1) {
-      if (wave_row + c16 < blk.row_end) {
-#pragma unroll
-        for (int b = 0; b < DT; ++b) store(wave_row + c16, b * 16 + 4 * g, o[b], m, l, lx);
-      }
+      if (wave_row + c16 < blk.row_end) store(place_of(wave_row + c16, 4 * g), 16, o, m, l, lx, g == 0);
       lds_barrier();
     } else {
       // the groups' results are joined in LDS, kCols columns at a time
@@ -329,36 +352,38 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
         s_ml[wave][c16][1] = l;
         s_ml[wave][c16][2] = lx;
       }
-      lds_barrier();
-      float top = kLow;
-#pragma unroll
-      for (int k = 0; k < KW; ++k) top = fmaxf(top, s_ml[k * RW + wr][c16][0]);
-      const float down = exp2_fast(m - top);
+      // kPer threads a row
+      constexpr int kPer = kThr / (RW * 16);
+      const int mine = tid / kPer, first = tid % kPer * 4;
+      const Place place = place_of(blk.row_first + mine, first);
       float* tile = reinterpret_cast<float*>(s_buf);
 #pragma unroll
       for (int cq = 0; cq < LAT / kCols; ++cq) {
 #pragma unroll
         for (int b = 0; b < kCols / 16; ++b)
-          *reinterpret_cast<f32x4*>(tile + (wave * 16 + c16) * kPad + b * 16 + 4 * g) = o[cq * (kCols / 16) + b] * down;
+          *reinterpret_cast<f32x4*>(tile + (wave * 16 + c16) * kPad + b * 16 + 4 * g) = o[cq * (kCols / 16) + b];
         lds_barrier();
-        constexpr int kSpan = kThr / (kCols / 4);
-        for (int j = tid / (kCols / 4); j < RW * 16; j += kSpan) {
-          const int col = tid % (kCols / 4) * 4, w0 = j >> 4, at = j & 15;
-          if (blk.row_first + j >= blk.row_end) break;
-          f32x4 a = {0.f, 0.f, 0.f, 0.f};
-          float mm = kLow, ll = 0.f, lxx = 0.f;
+        float f[KW], mm = kLow, ll = 0.f, lxx = 0.f;
 #pragma unroll
-          for (int k = 0; k < KW; ++k) {
-            a += *reinterpret_cast<const f32x4*>(tile + ((k * RW + w0) * 16 + at) * kPad + col);
-            mm = fmaxf(mm, s_ml[k * RW + w0][at][0]);
-          }
+        for (int k = 0; k < KW; ++k) mm = fmaxf(mm, s_ml[k * RW + (mine >> 4)][mine & 15][0]);
 #pragma unroll
-          for (int k = 0; k < KW; ++k) {
-            const float f = exp2_fast(s_ml[k * RW + w0][at][0] - mm);
-            ll += s_ml[k * RW + w0][at][1] * f;
-            lxx += s_ml[k * RW + w0][at][2] * f;
-          }
-          store(blk.row_first + j, cq * kCols + col, a, mm, ll, lxx);
+        for (int k = 0; k < KW; ++k) {
+          f[k] = exp2_fast(s_ml[k * RW + (mine >> 4)][mine & 15][0] - mm);
+          ll += s_ml[k * RW + (mine >> 4)][mine & 15][1] * f[k];
+          lxx += s_ml[k * RW + (mine >> 4)][mine & 15][2] * f[k];
+        }
+        constexpr int N = kCols / (4 * kPer);
+        f32x4 a[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) a[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KW; ++k)
+#pragma unroll
+          for (int n = 0; n < N; ++n)
+            a[n] += *reinterpret_cast<const f32x4*>(tile + (k * RW * 16 + mine) * kPad + first + n * kPer * 4) * f[k];
+        if (blk.row_first + mine < blk.row_end) {
+          const Place d = {place.out + cq * kCols, place.part_o + cq * kCols, place.lse, place.part_ml};
+          store(d, kPer * 4, a, mm, ll, lxx, cq == 0 && first == 0);
         }
         lds_barrier();
       }
