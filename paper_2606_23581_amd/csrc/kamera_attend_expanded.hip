@@ -21,6 +21,7 @@ namespace {
 
 constexpr int kExpThreads = 256;
 constexpr int kTileKeys = 64;
+constexpr int kAhead = 4;                          // products whose operands are read ahead
 
 }  // namespace
 
@@ -47,7 +48,7 @@ __global__ __launch_bounds__(kExpThreads, 2) void attend_expanded_kernel(MlaPara
   } else {
     share.task = p.n_tasks - 1 - wg;               // late row blocks, which see the most keys, first
     share.skip = 0;
-    share.units = units_of<kTileKeys>(block_of(p, share.task));
+    share.units = INT32_MAX;
   }
 
   // this lane's pieces of the wave's 16 keys of a tile: key and chunk of load j
@@ -78,12 +79,12 @@ __global__ __launch_bounds__(kExpThreads, 2) void attend_expanded_kernel(MlaPara
 
   uint32_t task = share.task;
   int skip = share.skip, units = share.units, segment = 0;
-  for (; units > 0; ++task, skip = 0) {
+  const uint32_t end = p.n_parts > 0 ? p.n_tasks : task + 1;
+  for (; units > 0 && task < end; ++task, skip = 0) {
     const Block blk = block_of(p, task);
-    const int total = units_of<kTileKeys>(blk), take = min(total - skip, units);
-    if (take <= 0) continue;
-    units -= take;
-    const int tile0 = blk.lo / kTileKeys + skip;
+    Segment seg;
+    if (!take_segment(p, blk, kTileKeys, task, share, units, skip, seg)) continue;
+    const int take = seg.to - seg.from, tile0 = blk.lo / kTileKeys + seg.from;
     const int part_begin = blk.lo >> 4, part_end = (blk.hi >> 4) + 1;
     const int64_t key_row = first_row(p.kv_base, blk.r, p.n_keys);
     const uint64_t k_head = (uint64_t)p.k + key_row * p.k_s[0] + blk.h * p.k_s[1];
@@ -161,21 +162,31 @@ __global__ __launch_bounds__(kExpThreads, 2) void attend_expanded_kernel(MlaPara
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
 
-    // Scores and softmax of a tile; the weights as the second product takes them.
-    auto weigh = [&](int pos, uint32_t buf, uint32_t ok, bf16x8 (&pf)[4]) {
+    // A tile: scores, softmax and the product with the values.
+    auto compute = [&](int pos, uint32_t buf, uint32_t ok) {
       f32x16 sc[2];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sc[u][i] = 0.f;
+      // operand i: keys 32 (i / N) on, inner step i % N
+      constexpr int N = KS + RS;
+      auto rows = [&](int i) {
+        const int u = i / N, ks = i % N;
+        return ks < KS ? read_chunk(buf + k_at[ks < KS ? ks : 0] + u * 32 * kRowB)
+                       : read_chunk(buf + r_at[ks < KS ? 0 : ks - KS] + u * 32 * kRopeCols * 2);
+      };
+      __builtin_amdgcn_s_setprio(1);
+      bf16x8 kf[2 * N];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_chunk(buf + k_at[ks] + u * 32 * kRowB), qf[ks], sc[u], 0, 0, 0);
+      for (int i = 0; i < kAhead; ++i) kf[i] = rows(i);
 #pragma unroll
-        for (int ks = 0; ks < RS; ++ks)
-          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_chunk(buf + r_at[ks] + u * 32 * kRopeCols * 2), qf[KS + ks],
-                                                          sc[u], 0, 0, 0);
+      for (int i = 0; i < 2 * N; ++i) {
+        if (i + kAhead < 2 * N) kf[i + kAhead] = rows(i + kAhead);
+        sc[i / N] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[i % N], sc[i / N], 0, 0, 0);
       }
+      pipeline<2 * N, 1, kAhead>();
+      __builtin_amdgcn_s_setprio(0);
       if (ok != 15u || pos + kTileKeys - 1 > blk.all_hi || pos < blk.all_lo) {     // some row does not see it whole
         const int at = pos + 4 * hf - row_lo;
 #pragma unroll
@@ -202,8 +213,18 @@ __global__ __launch_bounds__(kExpThreads, 2) void attend_expanded_kernel(MlaPara
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[b][i] *= down;
       }
+      // the products with the first half's weights run beside the second half's exponentials
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
+        bf16x8 vf[2][DT];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int b = 0; b < DT; ++b) {
+            const uint32_t at = buf + v_at[b] + (2 * u + s) * 16 * kRowB;
+            vf[s][b] = join(read_columns(at), read_columns(at + 8 * kRowB));
+          }
         float x[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = exp2_fast(__builtin_fmaf(sc[u][i], p.scale2, -m));
@@ -217,19 +238,12 @@ __global__ __launch_bounds__(kExpThreads, 2) void attend_expanded_kernel(MlaPara
                            pack_bf16x2(x[8 * s + 4], x[8 * s + 5]), pack_bf16x2(x[8 * s + 6], x[8 * s + 7])};
           l = add_pair(w.y, add_pair(w.x, l));
           l1 = add_pair(w.w, add_pair(w.z, l1));
-          pf[2 * u + s] = __builtin_bit_cast(bf16x8, w);
+          const bf16x8 pf = __builtin_bit_cast(bf16x8, w);
+#pragma unroll
+          for (int b = 0; b < DT; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s][b], pf, o[b], 0, 0, 0);
         }
       }
-
-    };
-    auto gather = [&](uint32_t buf, const bf16x8 (&pf)[4]) {
-#pragma unroll
-      for (int s = 0; s < 4; ++s)
-#pragma unroll
-        for (int b = 0; b < DT; ++b) {
-          const uint32_t at = buf + v_at[b] + s * 16 * kRowB;
-          o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(join(read_columns(at), read_columns(at + 8 * kRowB)), pf[s], o[b], 0, 0, 0);
-        }
+      __builtin_amdgcn_s_setprio(0);
     };
 
     for (int it = 0; it < take; ++it) {
@@ -239,14 +253,12 @@ __global__ __launch_bounds__(kExpThreads, 2) void attend_expanded_kernel(MlaPara
       if (it + 1 < take) ok_next = issue(it + 1);
       const int pos = (tile0 + it) * kTileKeys;
       const uint32_t buf = lds + (it & 1) * kBuf;
-      bf16x8 pf[4] = {};
-      if (wave_row < blk.row_end) weigh(pos, buf, ok, pf);
       if (mixed(blk, pos, kTileKeys)) {
-        lds_barrier();
+        // what is not finite is left out of the product and added to the stored results
         for (int i = tid; i < kTile / 16; i += kExpThreads) odd |= clean_chunk(buf + kVAt + i * 16);
         lds_barrier();
       }
-      if (wave_row < blk.row_end) gather(buf, pf);
+      if (wave_row < blk.row_end) compute(pos, buf, ok);
       ok = ok_next;
     }
     lds_barrier();                                 // the buffers are free
@@ -259,7 +271,7 @@ __global__ __launch_bounds__(kExpThreads, 2) void attend_expanded_kernel(MlaPara
 
     l = sum_x32(l + l1);
     lx = sum_x32(lx);
-    const bool direct = skip == 0 && take == total;
+    const bool direct = seg.whole();
     const int64_t part = ((int64_t)wg * 2 + (segment > 0 ? 1 : 0)) * p.rows_block, at = part + wave * 32 + c32;
     ++segment;
     if (wave_row + c32 < blk.row_end) {

@@ -28,7 +28,6 @@ namespace kamera {
 namespace {
 
 constexpr int kStepKeys = 32;
-constexpr int kMfma = 0x8, kDsRead = 0x100;        // instruction groups of the scheduler
 
 __device__ __forceinline__ uint32_t twist(uint32_t key) {
   return ((key >> 1) & 1) << 2 | ((key >> 2) & 1) << 1 | ((key >> 3) & 1);
@@ -41,19 +40,6 @@ __device__ __forceinline__ float max_x16(float x) {
 __device__ __forceinline__ float sum_x16(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// The order of N products, each of READS operand reads: kAhead products' reads before
-// the first one.
-template <int N, int READS, int kAhead>
-__device__ __forceinline__ void pipeline() {
-  __builtin_amdgcn_sched_group_barrier(kDsRead, kAhead * READS, 0);
-#pragma unroll
-  for (int i = 0; i < N - kAhead; ++i) {
-    __builtin_amdgcn_sched_group_barrier(kDsRead, READS, 0);
-    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-  }
-  __builtin_amdgcn_sched_group_barrier(kMfma, kAhead, 0);
 }
 
 // Columns of the groups' results that fit the slots at a time.
@@ -88,7 +74,7 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
   } else {
     share.task = p.n_tasks - 1 - blockIdx.x;       // late row blocks, which see the most keys, first
     share.skip = 0;
-    share.units = units_of<kUnit>(block_of(p, share.task));
+    share.units = INT32_MAX;
   }
 
   // this lane's pieces of 8 keys that the wave loads: offset from the first one's row, and
@@ -113,12 +99,13 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
 
   uint32_t task = share.task;
   int skip = share.skip, units = share.units, segment = 0;
-  for (; units > 0; ++task, skip = 0) {
+  const uint32_t end = p.n_parts > 0 ? p.n_tasks : task + 1;
+  for (; units > 0 && task < end; ++task, skip = 0) {
     const Block blk = block_of(p, task);
-    const int total = units_of<kUnit>(blk), take = min(total - skip, units);
-    if (take <= 0) continue;
-    units -= take;
-    const int key0 = (blk.lo / kUnit + skip) * kUnit + kg * kStepKeys;   // the group's keys of the first unit
+    Segment seg;
+    if (!take_segment(p, blk, kUnit, task, share, units, skip, seg)) continue;
+    const int take = seg.to - seg.from;
+    const int key0 = (blk.lo / kUnit + seg.from) * kUnit + kg * kStepKeys;   // the group's keys of the first unit
     const int part_begin = blk.lo >> 4, part_end = (blk.hi >> 4) + 1;
 
     // pages looked up 32 steps at a time: lane i has part i % 2 of step i / 2 of the batch
@@ -304,7 +291,7 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
 
     l = sum_x32(sum_x16(l));
     lx = sum_x32(sum_x16(lx));
-    const bool direct = skip == 0 && take == total;
+    const bool direct = seg.whole();
     const int64_t part = ((int64_t)blockIdx.x * 2 + (segment > 0 ? 1 : 0)) * p.rows_block;
     ++segment;
     // Where a row's results belong: looked up before the waits below.
@@ -389,7 +376,7 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
       }
     }
     if (odd) {
-      const int from = (blk.lo / kUnit + skip) * kUnit;
+      const int from = (blk.lo / kUnit + seg.from) * kUnit;
       add_nonfinite(p, blk, from, from + take * kUnit, NB == 1 ? kStepKeys : kUnit, LAT, direct, part, row0, [&](int key) {
         const int k = (int)fast_div((uint32_t)key >> 4, p.fd_page16);
         const int page = p.page_table[(int64_t)blk.r * p.pt_stride + k];

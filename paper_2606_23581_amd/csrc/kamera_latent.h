@@ -64,7 +64,7 @@ struct ProjectParams {
   int32_t n_rows, n_heads, n_in, n_out;
   int32_t paged;
   int32_t w_k;                       // 1: W's columns of one output lie together (stride `in` is 1)
-  int32_t small;                     // 1: tiles of 32 rows
+  int32_t tile_rows;                 // 32, 128 (tiles of 128 columns) or 256 (of 256)
   int32_t n_row_blocks, n_col_blocks;
   int32_t n_tasks, per_xcd;
   FastDiv fd_rows, fd_cols, fd_heads, fd_page;
@@ -94,7 +94,7 @@ struct MlaParams {
   float* part_o;                     // [workgroup][2][rows of a block][columns] unnormalised sums
   float* part_ml;                    // [workgroup][2][rows of a block][4] running maximum (in powers of 2), sum of
                                      // the rounded weights, sum of the weights
-  int32_t* prefix;                   // [n_tasks + 1] units before each task, units of a workgroup, [n_parts] first tasks
+  int32_t* prefix;                   // [n_tasks] units before each task, units of a workgroup, [n_parts] first tasks
   uint32_t* status;
   int64_t q_s[2], out_s[2], lse_s[2];
   int64_t pool_s[2];                 // bytes: page, token
@@ -112,6 +112,9 @@ struct MlaParams {
   int32_t n_tasks;
   int32_t n_parts;                   // > 0: workgroups among which all tasks' units are divided; 0: one a task
   int32_t min_units;                 // least units of a workgroup
+  int32_t unit;                      // keys of a unit
+  int32_t fixed;                     // units that a task costs beside its own
+  int32_t lanes;                     // of a wave that add up a request's units: a power of two up to 64
   FastDiv fd_group, fd_blocks, fd_heads, fd_page16;
 };
 

@@ -12,6 +12,13 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) uint8_t* LdsBytes;
 typedef const __attribute__((address_space(1))) uint8_t* GlobalBytes;
 
+// Memory that no kernel writes while this one runs, at a wave-uniform address: a scalar
+// load.
+template <typename T>
+__device__ __forceinline__ T uniform_load(const T* p) {
+  return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
+}
+
 // Offset of a __shared__ object in the workgroup's LDS.
 __device__ __forceinline__ uint32_t lds_offset(const void* p) { return (uint32_t)(uintptr_t)(LdsBytes)p; }
 
@@ -51,5 +58,20 @@ __device__ __forceinline__ bf16x8 read_chunk(uint32_t at) {
   return *(const __attribute__((address_space(3))) bf16x8*)(uintptr_t)at;
 }
 __device__ __forceinline__ bf16x8 join(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+constexpr int kMfma = 0x8, kDsRead = 0x100;        // instruction groups of the scheduler
+
+// The order of N products, each of READS operand reads: kAhead products' reads before
+// the first one.
+template <int N, int READS, int kAhead>
+__device__ __forceinline__ void pipeline() {
+  __builtin_amdgcn_sched_group_barrier(kDsRead, kAhead * READS, 0);
+#pragma unroll
+  for (int i = 0; i < N - kAhead; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kDsRead, READS, 0);
+    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(kMfma, kAhead, 0);
+}
 
 }  // namespace kamera

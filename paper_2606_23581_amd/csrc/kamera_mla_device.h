@@ -13,13 +13,6 @@ constexpr float kSlack = 8.0f;                     // by how much (in powers of 
 // v_exp_f32: 2^x, about 1 ulp
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Memory that no kernel writes while this one runs, at a wave-uniform address: a scalar
-// load.
-template <typename T>
-__device__ __forceinline__ T uniform_load(const T* p) {
-  return *(const __attribute__((address_space(4))) T*)(uintptr_t)p;
-}
-
 // First row of a request's in q and out, or of its expanded keys.
 __device__ __forceinline__ int64_t first_row(const int32_t* base, int r, int most) {
   return base != nullptr ? (int64_t)uniform_load(base + r) : (int64_t)r * most;
@@ -68,19 +61,11 @@ __device__ __forceinline__ int mla_first_key(const MlaParams& p, int last) {
   return p.window > 0 ? max(0, last - p.window + 1) : 0;
 }
 
-// UNIFORM: the task is the same for the whole wave, and its lengths are scalar loads.
-template <bool UNIFORM = true>
-__device__ __forceinline__ Block block_of(const MlaParams& p, uint32_t task) {
+__device__ __forceinline__ Block block_from(const MlaParams& p, int r, int h, int rb, int n, int kv) {
   Block b;
-  uint32_t d = fast_div(task, p.fd_blocks);
-  b.rb = (int)(task - d * p.n_row_blocks);
-  const uint32_t r = fast_div(d, p.fd_heads);
-  b.h = (int)(d - r * p.task_heads);
-  b.r = (int)r;
-  // both at once, without a branch between them
-  const int32_t* q_tokens = p.q_tokens != nullptr ? p.q_tokens : p.kv_tokens;
-  const int n = UNIFORM ? uniform_load(q_tokens + r) : q_tokens[r];
-  const int kv = UNIFORM ? uniform_load(p.kv_tokens + r) : p.kv_tokens[r];
+  b.r = r;
+  b.h = h;
+  b.rb = rb;
   b.n = p.q_tokens != nullptr ? min(max(n, 0), p.n_queries) : p.n_queries;
   b.kv = min(max(kv, 0), p.n_keys);
   const int rows = b.n * p.group;
@@ -98,65 +83,140 @@ __device__ __forceinline__ Block block_of(const MlaParams& p, uint32_t task) {
   return b;
 }
 
-// Units of UNIT keys that a block walks: those from lo / UNIT on.  A block that sees
-// no key has one all the same, so that its rows are written.
-template <int UNIT>
-__device__ __forceinline__ int units_of(const Block& b) {
-  if (b.row_first >= b.row_end) return 0;
-  return b.hi < b.lo ? 1 : b.hi / UNIT - b.lo / UNIT + 1;
+// The block of a task that is the same for the whole wave.
+__device__ __forceinline__ Block block_of(const MlaParams& p, uint32_t task) {
+  const uint32_t d = fast_div(task, p.fd_blocks), r = fast_div(d, p.fd_heads);
+  // both lengths at once, without a branch between them
+  const int n = uniform_load((p.q_tokens != nullptr ? p.q_tokens : p.kv_tokens) + r), kv = uniform_load(p.kv_tokens + r);
+  return block_from(p, (int)r, (int)(d - r * p.task_heads), (int)(task - d * p.n_row_blocks), n, kv);
 }
 
-// What a workgroup does: units [u0, u1) of consecutive tasks, from task `task` on, of
-// which `skip` units belong to workgroups before it.
+// Units of `unit` keys that a block walks: those from lo / unit on.  A block that sees
+// no key has one all the same, so that its rows are written.
+__device__ __forceinline__ int units_of(const Block& b, int unit) {
+  if (b.row_first >= b.row_end) return 0;
+  return b.hi < b.lo ? 1 : b.hi / unit - b.lo / unit + 1;
+}
+
+// What a block costs, in units: p.fixed of them, in which nothing is walked, for taking it
+// up and storing its results, and its own.  Without the first, workgroups with many short
+// blocks end last (ragged prompts of eight requests: 122 us, now XX).
+__device__ __forceinline__ int cost_of(const MlaParams& p, const Block& b, int unit) {
+  const int u = units_of(b, unit);
+  return u > 0 ? u + p.fixed : 0;
+}
+
+// What a workgroup does: costs `units` of consecutive tasks, from task `task` on, of which
+// `skip` belong to workgroups before it.
 struct Share {
   uint32_t task;
   int skip;
   int units;
+  int begin;                         // cost before its range
 };
 
-// The tasks' units, divided evenly: workgroup w takes the w-th range of `per` units.
-// Every wave adds up all tasks' units, some a lane (a few loads and shuffles, no
-// barrier); the first workgroup leaves the sums, and each its first task, for the kernel
-// that joins the parts.
-template <int UNIT>
-__device__ __forceinline__ Share divide(const MlaParams& p, uint32_t w) {
-  const int lane = threadIdx.x & 63, each = (p.n_tasks + 63) / 64;
-  const int t0 = min(lane * each, p.n_tasks), t1 = min(t0 + each, p.n_tasks);
-  int sum = 0;
-  for (int t = t0; t < t1; ++t) sum += units_of<UNIT>(block_of<false>(p, t));
-  int x = sum;                                     // inclusive sums over the lanes
+// The units [from, to) of a task that a workgroup walks, of its `total`.
+struct Segment {
+  int from, to, total;
+  __device__ __forceinline__ bool whole() const { return from == 0 && to == total; }
+};
+
+// The next task's part of a share; false where there is nothing to walk in it.
+__device__ __forceinline__ bool take_segment(const MlaParams& p, const Block& b, int unit, uint32_t task, const Share& share,
+                                             int& units, int skip, Segment& s) {
+  s.total = units_of(b, unit);
+  if (s.total == 0) return false;
+  if (p.n_parts > 0 && skip == 0 && threadIdx.x == 0) p.prefix[task] = share.begin + share.units - units;
+  const int take = min(s.total + p.fixed - skip, units);
+  units -= take;
+  s.from = max(skip - p.fixed, 0);
+  s.to = max(skip + take - p.fixed, 0);
+  return s.from < s.to;
+}
+
+// Inclusive sums over the lanes.
+__device__ __forceinline__ int lane_sums(int x) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
     const int y = __shfl_up(x, d);
     x += lane >= d ? y : 0;
   }
-  const int total = __builtin_amdgcn_readlane(x, 63);
+  return x;
+}
+
+// The tasks' costs, divided evenly: workgroup w takes the w-th range of `per` units.
+// Every wave adds up all requests' costs: so many lanes a request as it has row blocks,
+// a request's heads alike.
+template <int UNIT>
+__device__ __forceinline__ Share divide(const MlaParams& p, uint32_t w) {
+  const int lane = threadIdx.x & 63, width = p.lanes, slot = lane & (width - 1), each = 64 / width;
+  // cost of one head of the lane's request in this pass, the same in all its lanes
+  auto units_in = [&](int pass) {
+    const int r = pass * each + lane / width;
+    int s = 0;
+    if (r < p.n_requests) {
+      const int n = (p.q_tokens != nullptr ? p.q_tokens : p.kv_tokens)[r], kv = p.kv_tokens[r];
+      for (int rb = slot; rb < p.n_row_blocks; rb += width) s += cost_of(p, block_from(p, r, 0, rb, n, kv), UNIT);
+    }
+    for (int d = 1; d < width; d *= 2) s += __shfl_xor(s, d);
+    return s;
+  };
+  const int passes = (p.n_requests + each - 1) / each;
+  int total = 0, one = 0, sums = 0;
+  for (int i = 0; i < passes; ++i) {
+    one = units_in(i);
+    sums = lane_sums(slot == 0 ? one * p.task_heads : 0);
+    total += __builtin_amdgcn_readlane(sums, 63);
+  }
   const int per = max((total + p.n_parts - 1) / p.n_parts, p.min_units);
   const int64_t begin = (int64_t)w * per;
-  int at = x - sum, task = p.n_tasks, skip = 0;    // units before this lane's tasks
-  const bool mine = begin >= at && begin < x, first = w == 0 && threadIdx.x < 64;
-  if (mine || first) {
-    for (int t = t0; t < t1; ++t) {
-      const int u = each == 1 ? sum : units_of<UNIT>(block_of<false>(p, t));
-      if (first) p.prefix[t] = at;
-      if (begin >= at && begin < at + u) {
-        task = t;
-        skip = (int)(begin - at);
-      }
-      at += u;
-    }
-  }
-  const uint64_t found = __ballot(mine);
-  const int from = found != 0 ? __builtin_ctzll(found) : 0;
   Share s;
-  s.task = (uint32_t)__builtin_amdgcn_readlane(task, from);
-  s.skip = __builtin_amdgcn_readlane(skip, from);
+  s.task = p.n_tasks;
+  s.skip = 0;
   s.units = begin >= total ? 0 : (int)min((int64_t)per, total - begin);
-  if (first && lane == 0) {
-    p.prefix[p.n_tasks] = total;
-    p.prefix[p.n_tasks + 1] = per;
+  if (w == 0 && threadIdx.x == 0) p.prefix[p.n_tasks] = per;
+  if (s.units > 0) {
+    // the request, its head, its row block
+    int at = 0, r = 0, rest = 0, head_units = 1;
+    for (int i = 0; i < passes; ++i) {
+      if (passes > 1) {
+        one = units_in(i);
+        sums = lane_sums(slot == 0 ? one * p.task_heads : 0);
+      }
+      const int mine = slot == 0 ? one * p.task_heads : 0;
+      const uint64_t found = __ballot(begin >= at + sums - mine && begin < at + sums);
+      if (found != 0) {
+        const int from = __builtin_ctzll(found);
+        r = i * each + from / width;
+        rest = (int)(begin - at) - __builtin_amdgcn_readlane(sums - mine, from);
+        head_units = __builtin_amdgcn_readlane(one, from);
+        break;
+      }
+      at += __builtin_amdgcn_readlane(sums, 63);
+    }
+    const int h = rest / head_units;
+    rest -= h * head_units;
+    const int n = uniform_load((p.q_tokens != nullptr ? p.q_tokens : p.kv_tokens) + r), kv = uniform_load(p.kv_tokens + r);
+    for (int rb0 = 0; rb0 < p.n_row_blocks; rb0 += 64) {
+      const int u = rb0 + lane < p.n_row_blocks ? cost_of(p, block_from(p, r, h, rb0 + lane, n, kv), UNIT) : 0;
+      const int x = lane_sums(u);
+      const uint64_t found = __ballot(rest >= x - u && rest < x);
+      if (found != 0) {
+        const int from = __builtin_ctzll(found);
+        s.task = ((uint32_t)r * p.task_heads + h) * p.n_row_blocks + rb0 + from;
+        s.skip = rest - __builtin_amdgcn_readlane(x - u, from);
+        break;
+      }
+      rest -= __builtin_amdgcn_readlane(x, 63);
+    }
+    s.task = __builtin_amdgcn_readfirstlane(s.task);
+    s.skip = __builtin_amdgcn_readfirstlane(s.skip);
   }
-  if (threadIdx.x == 0) p.prefix[p.n_tasks + 2 + w] = (int)s.task;
+  // for the kernel that joins the parts: the task that each range begins in, and (left by
+  // the workgroup that begins a task) the cost before each task
+  if (threadIdx.x == 0) p.prefix[p.n_tasks + 1 + w] = (int)s.task;
+  s.begin = (int)begin;
   return s;
 }
 

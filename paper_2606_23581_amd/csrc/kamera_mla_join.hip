@@ -25,24 +25,25 @@ __global__ __launch_bounds__(kJoinThreads) void mla_join_kernel(MlaParams) {
   __shared__ f32x4 s_o[WAYS > 1 ? WAYS : 1][32];
   __shared__ float s_ml[WAYS > 1 ? WAYS : 1][3];
   const int tid = threadIdx.x, col = tid & 31, way = WAYS > 1 ? tid >> 5 : 0;
-  const int per = p.prefix[p.n_tasks + 1];
+  const int per = uniform_load(p.prefix + p.n_tasks);
   // the task, and the workgroups w0 .. w1 that share it
   const bool by_task = p.n_tasks < p.n_parts;
-  const int task = by_task ? (int)blockIdx.x : p.prefix[p.n_tasks + 3 + blockIdx.x];
+  const int task = by_task ? (int)blockIdx.x : uniform_load(p.prefix + p.n_tasks + 2 + blockIdx.x);
   if (task >= p.n_tasks) return;
-  const int u0 = p.prefix[task], u1 = p.prefix[task + 1];
-  if (u1 <= u0) return;
-  const int w0 = u0 / per, w1 = (u1 - 1) / per;
+  const Block blk = block_of(p, task);
+  const int n_units = units_of(blk, p.unit);
+  if (n_units == 0) return;
+  // (the cost before it, and then p.fixed in which nothing is walked)
+  const int u0 = uniform_load(p.prefix + task), w0 = (u0 + p.fixed) / per, w1 = (u0 + p.fixed + n_units - 1) / per;
   if (w0 == w1 || (!by_task && (int)blockIdx.x != w0)) return;     // one workgroup had it all, or not its first range
   const int quarters = (p.dim + 127) >> 7, cq = blockIdx.y % quarters;
   const int rr = blockIdx.y / quarters * kRows + (WAYS > 1 ? 0 : tid >> 5);
-  const Block blk = block_of(p, task);
   const int row = blk.row_first + rr;
   if (row >= blk.row_end) return;                  // of all 256 threads where they meet in LDS
   const int c0 = cq * 128 + col * 4;
   const bool there = c0 < p.dim;
-  // the first part is its workgroup's first segment only where that begins with it
-  const int first_slot = u0 == w0 * per ? 0 : 1;
+  // the first part is its workgroup's first segment only where that's range begins with it
+  const int first_slot = w0 * per >= u0 ? 0 : 1;
 
   float top = kLow, l = 0.f, lx = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};

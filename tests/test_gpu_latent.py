@@ -238,7 +238,8 @@ def product_bound(x, w):
 @pytest.mark.parametrize("w_rows", [True, False])
 @pytest.mark.parametrize("rows,heads,n_in,n_out", [(1, 1, 64, 64), (1, 16, 128, 512), (3, 5, 512, 128), (33, 2, 192, 320),
                                                    (64, 3, 128, 128), (65, 3, 64, 192), (127, 1, 256, 64),
-                                                   (129, 4, 128, 512), (300, 2, 576, 448), (1000, 3, 512, 128)])
+                                                   (129, 4, 128, 512), (300, 2, 576, 448), (1000, 3, 512, 128),
+                                                   (300, 256, 64, 256), (515, 90, 192, 512)])
 def test_project_heads(rows, heads, n_in, n_out, w_rows):
     rng = np.random.default_rng(rows)
     x, x64 = bf16(rng.standard_normal((rows, heads, n_in)))
@@ -289,7 +290,8 @@ def test_project_heads_not_finite_stays_in_its_row():
 @pytest.mark.parametrize("w_rows", [True, False])
 @pytest.mark.parametrize("lengths,page,heads,n_in,n_out", [([1], 16, 1, 256, 64), ([5, 0, 17, 64], 16, 3, 512, 128),
                                                            ([200, 33], 7, 2, 512, 192), ([300, 129, 128], 64, 4, 256, 256),
-                                                           ([20] * 40, 16, 2, 64, 128)])
+                                                           ([20] * 40, 16, 2, 64, 128),
+                                                           ([257, 31, 300] * 16, 16, 6, 64, 256)])
 def test_expand_latent(lengths, page, heads, n_in, n_out, w_rows):
     rng = np.random.default_rng(2)
     table, pool = table_for(rng, lengths, page)

@@ -258,9 +258,9 @@ def test_workspace():
     a = latent_args(n_parts=5)
     # two segments of a workgroup, a block's rows (16 of each wave): sums, and four words; then the
     # tasks' and the workgroups' places
-    assert L.kamera_attend_latent_workspace(ctypes.byref(a)) == 5 * 2 * 16 * (512 + 4) * 4 + 48
+    assert L.kamera_attend_latent_workspace(ctypes.byref(a)) == 5 * 2 * 16 * (512 + 4) * 4 + 32
     a = latent_args(n_parts=3, n_queries=9)                      # 144 rows: two blocks of 128 for each request
-    assert L.kamera_attend_latent_workspace(ctypes.byref(a)) == 3 * 2 * 128 * (512 + 4) * 4 + 48
+    assert L.kamera_attend_latent_workspace(ctypes.byref(a)) == 3 * 2 * 128 * (512 + 4) * 4 + 32
     a = expanded_args(n_parts=4)
     assert L.kamera_attend_expanded_workspace(ctypes.byref(a)) == 4 * 2 * 128 * (128 + 4) * 4 + 160
     # short contexts, and enough work for all: a workgroup takes a block's keys whole
