@@ -3,8 +3,8 @@
 //
 // With M the largest of the parts' maxima m_s,
 //   out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.
-// 32 threads take 128 columns of a row's parts; with WAYS = 8 every eighth part, the
-// ways meeting in LDS, else eight rows a workgroup.  Tasks that were divided are found
+// 32 threads take 128 columns of a row's parts: with WAYS > 1 every WAYS-th part, the
+// ways meeting in LDS, else all of them, for one row or for four.  Tasks that were divided are found
 // from where the workgroups' ranges begin: a grid over the ranges where there are
 // fewer of them than tasks, else over the tasks.
 
@@ -12,16 +12,25 @@
 
 namespace kamera {
 
-namespace {
+// A row's running maximum, sums and four columns.
+struct Sum {
+  float top, l, lx;
+  f32x4 acc;
+  // Two such sums become one.
+  __device__ __forceinline__ void add(const Sum& b) {
+    const float m = fmaxf(top, b.top), f = exp2_fast(top - m), g = exp2_fast(b.top - m);
+    top = m;
+    l = l * f + b.l * g;
+    lx = lx * f + b.lx * g;
+    acc = acc * f + b.acc * g;
+  }
+};
 
-constexpr int kJoinThreads = 256;
-
-}  // namespace
-
-template <int WAYS>
-__global__ __launch_bounds__(kJoinThreads) void mla_join_kernel(MlaParams) {
+// OWN: rows of a thread, 8 apart.
+template <int WAYS, int OWN>
+__global__ __launch_bounds__(WAYS > 1 ? WAYS * 32 : 256) void mla_join_kernel(MlaParams) {
   const MlaParams& p = kernel_params<MlaParams>();
-  constexpr int kChunk = 4, kRows = 8 / WAYS;
+  constexpr int kChunk = OWN > 1 ? 2 : 8;          // parts of a row that a thread has in flight
   __shared__ f32x4 s_o[WAYS > 1 ? WAYS : 1][32];
   __shared__ float s_ml[WAYS > 1 ? WAYS : 1][3];
   const int tid = threadIdx.x, col = tid & 31, way = WAYS > 1 ? tid >> 5 : 0;
@@ -37,74 +46,75 @@ __global__ __launch_bounds__(kJoinThreads) void mla_join_kernel(MlaParams) {
   const int u0 = uniform_load(p.prefix + task), w0 = (u0 + p.fixed) / per, w1 = (u0 + p.fixed + n_units - 1) / per;
   if (w0 == w1 || (!by_task && (int)blockIdx.x != w0)) return;     // one workgroup had it all, or not its first range
   const int quarters = (p.dim + 127) >> 7, cq = blockIdx.y % quarters;
-  const int rr = blockIdx.y / quarters * kRows + (WAYS > 1 ? 0 : tid >> 5);
-  const int row = blk.row_first + rr;
-  if (row >= blk.row_end) return;                  // of all 256 threads where they meet in LDS
+  const int rr = blockIdx.y / quarters * (WAYS > 1 ? 1 : 8 * OWN) + (WAYS > 1 ? 0 : tid >> 5);
+  if (blk.row_first + rr >= blk.row_end) return;   // of all 256 threads where they meet in LDS
   const int c0 = cq * 128 + col * 4;
   const bool there = c0 < p.dim;
   // the first part is its workgroup's first segment only where that's range begins with it
   const int first_slot = w0 * per >= u0 ? 0 : 1;
 
-  float top = kLow, l = 0.f, lx = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  Sum sum[OWN];
+#pragma unroll
+  for (int n = 0; n < OWN; ++n) sum[n] = {kLow, 0.f, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
   for (int s0 = w0 + way; s0 <= w1; s0 += kChunk * WAYS) {
-    f32x4 ml[kChunk], o[kChunk];
+    f32x4 ml[OWN][kChunk], o[OWN][kChunk];
 #pragma unroll
-    for (int k = 0; k < kChunk; ++k) {
-      const int s = min(s0 + k * WAYS, w1);        // one past the end is read again and left out
-      const int64_t at = ((int64_t)s * 2 + (s == w0 ? first_slot : 0)) * p.rows_block + rr;
-      ml[k] = *reinterpret_cast<const f32x4*>(p.part_ml + at * 4);
-      o[k] = *reinterpret_cast<const f32x4*>(p.part_o + at * p.dim + (there ? c0 : 0));
-    }
-    float m = top;
+    for (int n = 0; n < OWN; ++n)
 #pragma unroll
-    for (int k = 0; k < kChunk; ++k) m = fmaxf(m, ml[k].x);
-    const float down = exp2_fast(top - m);
-    top = m;
-    l *= down;
-    lx *= down;
-    acc *= down;
-#pragma unroll
-    for (int k = 0; k < kChunk; ++k)
-      if (s0 + k * WAYS <= w1) {
-        const float f = exp2_fast(ml[k].x - top);
-        l += ml[k].y * f;
-        lx += ml[k].z * f;
-        acc += o[k] * f;
+      for (int k = 0; k < kChunk; ++k) {
+        // a part or row past the end is read again and left out
+        const int s = min(s0 + k * WAYS, w1), row = min(rr + 8 * n, blk.row_end - blk.row_first - 1);
+        const int64_t at = ((int64_t)s * 2 + (s == w0 ? first_slot : 0)) * p.rows_block + row;
+        ml[n][k] = *reinterpret_cast<const f32x4*>(p.part_ml + at * 4);
+        o[n][k] = *reinterpret_cast<const f32x4*>(p.part_o + at * p.dim + (there ? c0 : 0));
       }
+#pragma unroll
+    for (int n = 0; n < OWN; ++n) {
+      float m = sum[n].top;
+#pragma unroll
+      for (int k = 0; k < kChunk; ++k) m = fmaxf(m, ml[n][k].x);
+      const float down = exp2_fast(sum[n].top - m);
+      sum[n].top = m;
+      sum[n].l *= down;
+      sum[n].lx *= down;
+      sum[n].acc *= down;
+#pragma unroll
+      for (int k = 0; k < kChunk; ++k)
+        if (s0 + k * WAYS <= w1) {
+          const float f = exp2_fast(ml[n][k].x - m);
+          sum[n].l += ml[n][k].y * f;
+          sum[n].lx += ml[n][k].z * f;
+          sum[n].acc += o[n][k] * f;
+        }
+    }
   }
   if (WAYS > 1) {
-    s_o[WAYS > 1 ? way : 0][col] = acc;
+    s_o[WAYS > 1 ? way : 0][col] = sum[0].acc;
     if (col == 0) {
-      s_ml[WAYS > 1 ? way : 0][0] = top;
-      s_ml[WAYS > 1 ? way : 0][1] = l;
-      s_ml[WAYS > 1 ? way : 0][2] = lx;
+      s_ml[WAYS > 1 ? way : 0][0] = sum[0].top;
+      s_ml[WAYS > 1 ? way : 0][1] = sum[0].l;
+      s_ml[WAYS > 1 ? way : 0][2] = sum[0].lx;
     }
     __syncthreads();
     if (way != 0) return;
-    const float own = top;
 #pragma unroll
-    for (int k = 1; k < WAYS; ++k) top = fmaxf(top, s_ml[k][0]);
-    const float down = exp2_fast(own - top);
-    l *= down;
-    lx *= down;
-    acc *= down;
-#pragma unroll
-    for (int k = 1; k < WAYS; ++k) {
-      const float f = exp2_fast(s_ml[k][0] - top);
-      l += s_ml[k][1] * f;
-      lx += s_ml[k][2] * f;
-      acc += s_o[k][col] * f;
-    }
+    for (int k = 1; k < WAYS; ++k)
+      sum[0].add({s_ml[WAYS > 1 ? k : 0][0], s_ml[WAYS > 1 ? k : 0][1], s_ml[WAYS > 1 ? k : 0][2], s_o[WAYS > 1 ? k : 0][col]});
   }
   const int64_t row0 = first_row(p.q_base, blk.r, p.n_queries);
-  const int i = (int)fast_div((uint32_t)row, p.fd_group);
-  const int64_t hq = (int64_t)blk.h * p.group + row - i * p.group;
-  acc *= l == 0.f ? 0.f : 1.0f / l;
-  if (there)
-    *reinterpret_cast<u32x2*>(p.out + (row0 + i) * p.out_s[0] + hq * p.out_s[1] + c0) =
-        u32x2{pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w)};
-  if (cq == 0 && col == 0 && p.lse != nullptr) p.lse[(row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] = row_lse(top, lx);
+#pragma unroll
+  for (int n = 0; n < OWN; ++n) {
+    const int row = blk.row_first + rr + 8 * n;
+    if (row >= blk.row_end) break;
+    const int i = (int)fast_div((uint32_t)row, p.fd_group);
+    const int64_t hq = (int64_t)blk.h * p.group + row - i * p.group;
+    const f32x4 a = sum[n].acc * (sum[n].l == 0.f ? 0.f : 1.0f / sum[n].l);
+    if (there)
+      *reinterpret_cast<u32x2*>(p.out + (row0 + i) * p.out_s[0] + hq * p.out_s[1] + c0) =
+          u32x2{pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w)};
+    if (cq == 0 && col == 0 && p.lse != nullptr)
+      p.lse[(row0 + i) * p.lse_s[0] + hq * p.lse_s[1]] = row_lse(sum[n].top, sum[n].lx);
+  }
 }
 
 hipError_t launch_mla_join(const MlaParams& p, hipStream_t s) {
@@ -112,11 +122,13 @@ hipError_t launch_mla_join(const MlaParams& p, hipStream_t s) {
   const int64_t most = (int64_t)p.n_queries * p.group;
   const uint32_t rows = (uint32_t)(most < p.rows_block ? most : p.rows_block), quarters = (uint32_t)(p.dim + 127) >> 7;
   const uint32_t x = (uint32_t)(p.n_tasks < p.n_parts ? p.n_tasks : p.n_parts - 1);
-  // eight ways where a task has many parts
+  // many parts a row: a workgroup a row; ranges that share few rows each: four rows a thread
   if (p.n_parts >= 16 * (int64_t)p.n_tasks)
-    hipLaunchKernelGGL(mla_join_kernel<8>, dim3(x, rows * quarters), dim3(kJoinThreads), 0, s, p);
+    hipLaunchKernelGGL((mla_join_kernel<16, 1>), dim3(x, rows * quarters), dim3(512), 0, s, p);
+  else if (p.n_tasks < p.n_parts)
+    hipLaunchKernelGGL((mla_join_kernel<1, 1>), dim3(x, (rows + 7) / 8 * quarters), dim3(256), 0, s, p);
   else
-    hipLaunchKernelGGL(mla_join_kernel<1>, dim3(x, (rows + 7) / 8 * quarters), dim3(kJoinThreads), 0, s, p);
+    hipLaunchKernelGGL((mla_join_kernel<1, 4>), dim3(x, (rows + 31) / 32 * quarters), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
