@@ -149,7 +149,7 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
     };
     uint32_t oks = 0;                              // two bits a slot
 #pragma unroll
-    for (int i = 0; i < (NB > 1 ? NB - 1 : 1); ++i)
+    for (int i = 0; i < (NB > 1 ? NB / 2 : 1); ++i)
       if (i < take) oks |= issue(i) << (2 * i);
 
     // this wave's rows; lane l has row l % 16 (past the end the last one, whose results
@@ -269,14 +269,19 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
         if (it + 1 < take) oks = issue(it + 1);
       }
     } else {
+      // NB / 2 steps between barriers: their slots are read while the others are filled
+      constexpr int kHalf = NB / 2;
+#pragma unroll 1
       for (int it = 0; it < take; ++it) {
-        // the wave's loads of the NB - 2 steps behind this one may be under way (half of
-        // them where waves load in turn)
-        if (it + NB - 2 < take) vm_wait<(RW == 8 ? (NB - 2) / 2 : NB - 2) * NA * LPG>();
-        else vm_wait<0>();
-        lds_barrier();                             // the step's keys are there, and the slot before is free
-        const int next = it + NB - 1, s = next % NB;
-        if (next < take) oks = (oks & ~(3u << (2 * s))) | (issue(next) << (2 * s));
+        if (it % kHalf == 0) {
+          vm_wait<0>();
+          lds_barrier();                           // the steps' keys are there, and the other slots are free
+#pragma unroll
+          for (int i = kHalf; i < NB; ++i) {
+            const int s = (it + i) % NB;
+            if (it + i < take) oks = (oks & ~(3u << (2 * s))) | (issue(it + i) << (2 * s));
+          }
+        }
         const int pos = key0 + it * kUnit;
         bf16x8 pf = {};
         if (busy(pos)) pf = weigh(pos, slot_of(it), (oks >> (2 * (it % NB))) & 3u);
