@@ -15,8 +15,11 @@
 // and it spills.
 //
 // LDS: a slot holds 32 keys.  16-byte chunks are exchanged by an exclusive-or of their
-// number with bits 1 .. 3 of the key, highest last, so that 16 keys' reads of a chunk
-// and eight keys' of 32 bytes both spread over all banks.
+// number with a mix of bits 1 .. 3 of the key, so that eight keys' reads of 32 bytes
+// spread over all banks, and so do those of a chunk of 16 keys, which the hardware takes
+// as lanes 0-3, 12-15 and 20-27 (and so on): keys 0-3 and 12-15 of one chunk with keys
+// 4-11 of its neighbour.  With the bits in plain order a third of the reads' cycles were
+// conflicts.
 //
 // Softmax in powers of two (scale * log2 e folded in), fp32.  A row's running maximum
 // moves only when a score passes it by more than 8.
@@ -30,7 +33,8 @@ namespace {
 constexpr int kStepKeys = 32;
 
 __device__ __forceinline__ uint32_t twist(uint32_t key) {
-  return ((key >> 1) & 1) << 2 | ((key >> 2) & 1) << 1 | ((key >> 3) & 1);
+  const uint32_t b1 = (key >> 1) & 1, b2 = (key >> 2) & 1, b3 = (key >> 3) & 1;
+  return (b2 ^ b3) << 2 | b1 << 1 | b3;
 }
 
 __device__ __forceinline__ float max_x16(float x) {
@@ -78,19 +82,20 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
   }
 
   // this lane's pieces of 8 keys that the wave loads: offset from the first one's row, and
-  // in bit 0 whether the chunk's number is odd (in LDS where registers are short)
+  // in the low bits bits 0 and 2 of the chunk's number, which keys 8 .. 15 of 16 have the
+  // other way round (in LDS where registers are short)
   const uint32_t t_stride = (uint32_t)p.pool_s[1];
   uint32_t off[NW == 8 ? 1 : LPG];
 #pragma unroll
   for (int b = 0; b < LPG; ++b) {
     const uint32_t i = b * 64 + lane, key = i / CH, c = (i % CH) ^ twist(key);
-    const uint32_t x = key * t_stride + c * 16 + (c & 1);
+    const uint32_t x = key * t_stride + c * 16 + (c & 1) + (c >> 1 & 2);
     if (NW == 8) s_off[NW == 8 ? b : 0][lane] = x;             // every wave writes the same
     else off[NW == 8 ? 0 : b] = x;
   }
   auto piece = [&](int b, uint32_t odd) {
     const uint32_t x = NW == 8 ? s_off[NW == 8 ? b : 0][lane] : off[NW == 8 ? 0 : b];
-    return (x & ~15u) + odd * (16 - (x & 1) * 32);
+    return (x & ~15u) + odd * (80 - (x & 1) * 32 - (x & 2) * 64);
   };
   // places of the operands in a slot: chunk 4 s + g of key c16, and of keys 4 g ..
   // (rows and slots are multiples of 128 bytes, so that chunks are exchanged in the address)
