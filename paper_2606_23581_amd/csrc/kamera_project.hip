@@ -209,7 +209,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void project_kernel(ProjectParams)
         const int page = p.page_table[(int64_t)r * p.pt_stride + fast_div((uint32_t)row, p.fd_page)];
         there = page >= 0 && page < p.n_pool_pages;
       }
-      if (there) *reinterpret_cast<u32x4*>(p.out + (out_row0 + row) * p.out_s[0] + g * p.out_s[1] + col) = v;
+      if (there) st16(p.out + (out_row0 + row) * p.out_s[0] + g * p.out_s[1] + col, v);
     }
   }
 }
