@@ -454,7 +454,8 @@ int build_mla(const A* a, int32_t dim, const void* pool, const int64_t* pool_s, 
   // lane offsets within a tile are 32-bit
   if (pool_s[1] < 0 || pool_s[1] > (int64_t)1 << 24)
     return fail(KAMERA_ERR_RANGE, "%s: token stride %lld of the cache", who, (long long)pool_s[1]);
-  const int64_t n_rows = a->q_base != nullptr ? a->n_queries : (int64_t)a->n_requests * a->n_queries;
+  // how far rows reach is known only without a row base
+  const int64_t n_rows = a->q_base != nullptr ? 1 : (int64_t)a->n_requests * a->n_queries;
   const int64_t ext_q[2] = {n_rows, a->n_heads}, ext_p[2] = {a->n_pool_pages, a->page_size};
   Range out[3] = {};
   if (!span(a->q, a->q_stride, ext_q, 2, dim + a->rope_dim, 2, in[n_in].lo, in[n_in].hi) ||
@@ -543,7 +544,7 @@ int build_expanded(const kamera_attend_expanded_args* a, kamera::MlaParams& P, b
     if (t < 0 || t > (int64_t)1 << 24) return fail(KAMERA_ERR_RANGE, "%s: row stride %lld of k or v", who, (long long)t);
   Range in[9] = {};
   // how far k and v reach is known only without a row base
-  const int64_t rows = a->kv_base != nullptr ? a->n_keys : (int64_t)a->n_requests * a->n_keys;
+  const int64_t rows = a->kv_base != nullptr ? 1 : (int64_t)a->n_requests * a->n_keys;
   const int64_t ext[2] = {rows, a->n_heads};
   if (!span(a->k, a->k_stride, ext, 2, a->head_dim, 2, in[0].lo, in[0].hi) ||
       !span(a->v, a->v_stride, ext, 2, a->head_dim, 2, in[1].lo, in[1].hi))

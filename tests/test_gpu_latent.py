@@ -370,7 +370,7 @@ def attend(form, c, parts=0, D=None, seed=7, poison=None):
     rng = np.random.default_rng(seed)
     H, page, kv, nq = c["H"], c["page"], c["kv"], c["nq"]
     D = D or (512 if form == "latent" else 128)
-    table, pool = table_for(rng, kv, page)
+    table, pool = table_for(rng, kv, page, -(-c.get("most", (0, 0))[1] // page))
     for r, j in c["bad"]:
         table[r, j] = -1 if j % 2 else pool + 2
     width = (D if form == "latent" else 512) + 64
@@ -388,7 +388,8 @@ def attend(form, c, parts=0, D=None, seed=7, poison=None):
     out = torch.full((n_rows, H, D), 7.0, dtype=torch.bfloat16, device=DEV)
     lse = torch.full((n_rows, H), 7.0, device=DEV)
     status = i32([0])
-    kw = dict(n_queries=max(nq), n_keys=max(kv), scale=scale, q_base=i32(base), q_tokens=i32(nq), causal=c["causal"],
+    most_q, most_kv = c.get("most", (max(nq), max(kv)))
+    kw = dict(n_queries=most_q, n_keys=most_kv, scale=scale, q_base=i32(base), q_tokens=i32(nq), causal=c["causal"],
               window=c["window"], lse=lse, n_parts=parts, status=status)
     if form == "latent":
         if poison is not None:
@@ -459,6 +460,24 @@ POISON_CASES = {
     "window": dict(kv=[300, 200], nq=[20, 11], H=4, window=30),
     "prompt": dict(kv=[150], nq=[150], H=2),
 }
+
+
+# More requests than a wave has lanes, empty ones among them; lengths that leave most of the sizes' room unused.
+MANY_CASES = {
+    "one_query": dict(kv=[(37 * r) % 90 for r in range(150)] + [900], nq=[1] * 151, H=4),
+    "blocks": dict(kv=[(53 * r) % 70 for r in range(70)] + [400], nq=[(11 * r) % 26 for r in range(70)] + [150], H=8),
+    "last_alone": dict(kv=[0] * 129 + [800], nq=[0] * 129 + [3], H=2),
+    "first_alone": dict(kv=[800] + [0] * 129, nq=[3] + [0] * 129, H=2),
+    "all_empty": dict(kv=[0] * 70 + [0], nq=[0] * 70 + [0], H=2, most=(4, 600)),
+    "whole_tasks": dict(kv=[600, 0, 1, 300] + [(7 * r) % 4 for r in range(2044)], nq=[3, 1, 1, 0] + [1] * 2044, H=2),
+}
+
+
+@pytest.mark.parametrize("form", ["latent", "expanded"])
+@pytest.mark.parametrize("parts", [0, 1, 9, 300, 1024])
+@pytest.mark.parametrize("name", sorted(MANY_CASES))
+def test_attend_many_requests(form, parts, name):
+    check(*attend(form, MANY_CASES[name], parts=parts, D=256 if form == "latent" else 64))
 
 
 @pytest.mark.parametrize("form", ["latent", "expanded"])

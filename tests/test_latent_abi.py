@@ -229,6 +229,11 @@ CASES = [
     (4, dict(out=0x48000000), km.ERR_ALIAS),
     (4, dict(kv_base=0x60000000), km.ERR_ALIAS),
     (4, dict(window=3, causal=0), km.ERR_SHAPE),
+    # how many rows there are behind a base is not known: n_queries or n_keys rows may reach past the tensor
+    (3, dict(q_base=P + 0x2000, n_queries=4096, out=0x20000000 + 2 * 2 * 16 * 576), km.OK),
+    (3, dict(n_queries=4096, out=0x20000000 + 2 * 2 * 16 * 576), km.ERR_ALIAS),
+    (4, dict(kv_base=P + 0x2000, workspace=0x40000000 + 2 * 2 * 16 * 128), km.OK),
+    (4, dict(workspace=0x40000000 + 2 * 2 * 16 * 128), km.ERR_ALIAS),
 ]
 
 
