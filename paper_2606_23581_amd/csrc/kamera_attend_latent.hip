@@ -23,6 +23,13 @@
 //
 // Softmax in powers of two (scale * log2 e folded in), fp32.  A row's running maximum
 // moves only when a score passes it by more than 8.
+//
+// Single queries of 16 heads are bound by HBM (64 requests of up to 8192 keys: 378 MB in
+// 82 us, 4.6 TB/s).  With more rows LDS is: 16 rows of a wave read 36 KB for the scores of
+// 32 keys and 32 KB for the results, and eight waves of these keep a CU's LDS at work for
+// longer than its matrix pipes (two queries of 128 heads, 16 requests of up to 8192 keys:
+// 75 us, 46 GFLOP, pipes busy 23%).  Short calls are a chain of latencies (256 keys:
+// 12 us, one workgroup).
 
 #include "kamera_mla_device.h"
 
@@ -46,9 +53,6 @@ __device__ __forceinline__ float sum_x16(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Columns of the groups' results that fit the slots at a time.
-constexpr int latent_join_cols(int lat, int rw) { return lat * latent_waves(rw) > 2048 ? lat / 2 : lat; }
-
 }  // namespace
 
 template <int LAT, int RW>
@@ -61,7 +65,7 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
   constexpr int LW = RW < 4 ? RW : 4;              // waves that load a step's keys (of 8, those take turns)
   constexpr int NA = 4 / LW;                       // groups of 8 keys that a wave loads
   constexpr int kAhead = NW == 4 ? 6 : 4;          // products whose operands are read ahead
-  constexpr int kCols = latent_join_cols(LAT, RW), kPad = kCols + 4;   // the epilogue's tile: columns, floats of a row
+  constexpr int kPad = LAT + 4;                    // floats of a row of the epilogue's tile
   static_assert(kUnit == 32 * KW && NB >= 1, "");
   extern __shared__ __attribute__((aligned(128))) u32x4 s_buf[];
   __shared__ float s_ml[NW][16][3];
@@ -343,7 +347,7 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
       if (wave_row + c16 < blk.row_end) store(place_of(wave_row + c16, 4 * g), 16, o, m, l, lx, g == 0);
       lds_barrier();
     } else {
-      // the groups' results are joined in LDS, kCols columns at a time
+      // the groups' results are joined in LDS
       if (g == 0) {
         s_ml[wave][c16][0] = m;
         s_ml[wave][c16][1] = l;
@@ -355,35 +359,28 @@ __global__ __launch_bounds__(latent_waves(RW) * 64, latent_waves(RW) / 4) void a
       const Place place = place_of(blk.row_first + mine, first);
       float* tile = reinterpret_cast<float*>(s_buf);
 #pragma unroll
-      for (int cq = 0; cq < LAT / kCols; ++cq) {
+      for (int b = 0; b < DT; ++b) *reinterpret_cast<f32x4*>(tile + (wave * 16 + c16) * kPad + b * 16 + 4 * g) = o[b];
+      lds_barrier();
+      float f[KW], mm = kLow, ll = 0.f, lxx = 0.f;
 #pragma unroll
-        for (int b = 0; b < kCols / 16; ++b)
-          *reinterpret_cast<f32x4*>(tile + (wave * 16 + c16) * kPad + b * 16 + 4 * g) = o[cq * (kCols / 16) + b];
-        lds_barrier();
-        float f[KW], mm = kLow, ll = 0.f, lxx = 0.f;
+      for (int k = 0; k < KW; ++k) mm = fmaxf(mm, s_ml[k * RW + (mine >> 4)][mine & 15][0]);
 #pragma unroll
-        for (int k = 0; k < KW; ++k) mm = fmaxf(mm, s_ml[k * RW + (mine >> 4)][mine & 15][0]);
-#pragma unroll
-        for (int k = 0; k < KW; ++k) {
-          f[k] = exp2_fast(s_ml[k * RW + (mine >> 4)][mine & 15][0] - mm);
-          ll += s_ml[k * RW + (mine >> 4)][mine & 15][1] * f[k];
-          lxx += s_ml[k * RW + (mine >> 4)][mine & 15][2] * f[k];
-        }
-        constexpr int N = kCols / (4 * kPer);
-        f32x4 a[N];
-#pragma unroll
-        for (int n = 0; n < N; ++n) a[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < KW; ++k)
-#pragma unroll
-          for (int n = 0; n < N; ++n)
-            a[n] += *reinterpret_cast<const f32x4*>(tile + (k * RW * 16 + mine) * kPad + first + n * kPer * 4) * f[k];
-        if (blk.row_first + mine < blk.row_end) {
-          const Place d = {place.out + cq * kCols, place.part_o + cq * kCols, place.lse, place.part_ml};
-          store(d, kPer * 4, a, mm, ll, lxx, cq == 0 && first == 0);
-        }
-        lds_barrier();
+      for (int k = 0; k < KW; ++k) {
+        f[k] = exp2_fast(s_ml[k * RW + (mine >> 4)][mine & 15][0] - mm);
+        ll += s_ml[k * RW + (mine >> 4)][mine & 15][1] * f[k];
+        lxx += s_ml[k * RW + (mine >> 4)][mine & 15][2] * f[k];
       }
+      constexpr int N = LAT / (4 * kPer);
+      f32x4 a[N];
+#pragma unroll
+      for (int n = 0; n < N; ++n) a[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KW; ++k)
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          a[n] += *reinterpret_cast<const f32x4*>(tile + (k * RW * 16 + mine) * kPad + first + n * kPer * 4) * f[k];
+      if (blk.row_first + mine < blk.row_end) store(place, kPer * 4, a, mm, ll, lxx, first == 0);
+      lds_barrier();
     }
     if (odd) {
       const int from = (blk.lo / kUnit + seg.from) * kUnit;
@@ -403,7 +400,7 @@ template <int LAT, int RW>
 hipError_t launch_rows(const MlaParams& p, hipStream_t s) {
   static std::atomic<bool> done[kMaxDevices];
   const int slots = 4 * kStepKeys * (LAT + kRopeCols) * 2;
-  const int tile = latent_waves(RW) * 16 * (latent_join_cols(LAT, RW) + 4) * 4;
+  const int tile = latent_groups(RW) > 1 ? latent_waves(RW) * 16 * (LAT + 4) * 4 : 0;
   const int lds = slots > tile ? slots : tile;
   const hipError_t e = ensure_lds_limit((const void*)attend_latent_kernel<LAT, RW>, lds, done);
   if (e != hipSuccess) return e;
@@ -417,7 +414,6 @@ hipError_t launch_lat(const MlaParams& p, hipStream_t s) {
   switch (p.row_waves) {
     case 1: return launch_rows<LAT, 1>(p, s);
     case 2: return launch_rows<LAT, 2>(p, s);
-    case 4: return launch_rows<LAT, 4>(p, s);
     default: return launch_rows<LAT, 8>(p, s);
   }
 }

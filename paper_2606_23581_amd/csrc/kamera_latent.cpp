@@ -245,9 +245,15 @@ int build_product(int32_t heads, int32_t n_in, int32_t n_out, const void* w, con
   P.n_heads = heads;
   P.n_in = n_in;
   P.n_out = n_out;
+  // Tiles of 32 rows for a few, which more CUs share (64 rows of 16 heads, 128 x 512: kernel 4.2 us, 5.8 in tiles of
+  // 128).  Tiles of 256 need half the operands for each product, but there is one to a CU: they are taken where the
+  // last round of the 256 CUs is not left mostly empty (us in tiles of 256 / 128, 16 heads, 512 x 256: 224 tiles 24.6 /
+  // 28.3, 320 tiles 39.4 / 36.5, 384 tiles 40.4 / 43.5, 640 tiles 59.7 / 59.8, 1024 tiles 91 / 122; 128 tiles 19.3 / 15.0).
   P.tile_rows = rows <= 64 ? 32 : 128;
-  if (n_out % 256 == 0 && rows >= 256 && bounded_product({requests, ceil_div(rows, 256), heads, n_out / 256}) >= 512)
-    P.tile_rows = 256;
+  if (n_out % 256 == 0 && rows >= 256) {
+    const int64_t tiles = bounded_product({requests, ceil_div(rows, 256), heads, n_out / 256});
+    if (tiles >= 1024 || (tiles >= 192 && (tiles - 1) % 256 >= 96)) P.tile_rows = 256;
+  }
   P.n_row_blocks = (int32_t)ceil_div(rows, P.tile_rows);
   P.n_col_blocks = (int32_t)ceil_div(n_out, P.tile_rows == 256 ? 256 : 128);
   const int64_t tasks = bounded_product({requests, heads, P.n_row_blocks, P.n_col_blocks});
@@ -380,14 +386,18 @@ int size_mla(const AttendSizes& a, kamera::MlaParams& P, bool& launch, int64_t& 
   P.task_heads = a.latent ? 1 : a.n_heads;
   const int64_t rows = (int64_t)a.n_queries * P.group;
   if (rows > INT32_MAX / 2) return fail(KAMERA_ERR_RANGE, "%s: too many query rows", who);
-  P.row_waves = rows > 64 ? 8 : (rows > 32 ? 4 : (rows > 16 ? 2 : 1));
+  // the fewest waves that have all rows of a request, from 33 rows on 8, whose keys are fetched once for 128 rows
+  // (64 requests of up to 8192 keys: 24 heads 90.4 us with 2, 93.0 with 8; 48 heads 102.5 with 8, 103.8 with two
+  // groups of 4, 137 with 2)
+  P.row_waves = rows > 32 ? 8 : (rows > 16 ? 2 : 1);
   P.rows_block = a.latent ? 16 * P.row_waves : 128;
   P.n_row_blocks = (int32_t)ceil_div(rows, P.rows_block);
   const int64_t tasks = bounded_product({a.n_requests, P.task_heads, P.n_row_blocks});
   if (tasks < 0 || (tasks + 8) * 256 > 0xFFFFFFFFLL) return fail(KAMERA_ERR_RANGE, "%s: too many workgroups for one launch", who);
   P.n_tasks = (int32_t)tasks;
   const int unit = P.unit = a.latent ? 32 * kamera::latent_groups(P.row_waves) : 64;
-  // about 14000 cycles, at some 4500 for 64 keys of the expanded form, 2400 for 32 of the latent one
+  // about 14000 cycles, at some 4500 for 64 keys of the expanded form, 2400 for 32 of the latent one (eight ragged
+  // prompts, expanded: 122 us, 143 without; 64 single queries of 16 heads, latent: 89.4, 91.0)
   P.fixed = !a.latent ? 4 : (unit == 32 ? 6 : (unit == 64 ? 3 : 1));
   P.lanes = 1;
   while (P.lanes < 64 && P.lanes < P.n_row_blocks) P.lanes *= 2;
@@ -399,8 +409,12 @@ int size_mla(const AttendSizes& a, kamera::MlaParams& P, bool& launch, int64_t& 
     if (!can) return fail(KAMERA_ERR_RANGE, "%s: too much work to divide", who);
     P.n_parts = a.n_parts;
     P.min_units = 1;
-  } else if (can && tasks < kamera::kMlaDivideTasks && units > 5) {
-    P.min_units = 2;
+  } else if (can && tasks < kamera::kMlaDivideTasks && units > (a.latent ? 6 : 10)) {
+    // Up to 512 keys (latent, 16 rows; expanded) one workgroup is done before a second could have joined its part:
+    // 512 keys, 16 heads 16.0 us whole, 18.0 divided (latent), 22.0 and 25.0 (128 queries, expanded); 1024 keys 23.2
+    // and 17.9, 33.2 and 25.3.  A part is 128 keys of the latent form, which its four groups take at once, else two
+    // units (single queries of 128 heads, 256 keys: 26.2 us, 27.8 in parts of one).
+    P.min_units = unit == 128 ? 1 : 2;
     P.n_parts = (int32_t)std::min<int64_t>(a.latent ? 256 : 512, ceil_div(total, P.min_units));
   }
   if (P.n_parts > 0) {

@@ -72,11 +72,15 @@ struct ProjectParams {
 
 // ---- attention ----
 
-constexpr int kMlaDivideTasks = 2048;   // from so many (request, head, row block) tasks on a workgroup takes one whole
+// From so many (request, head, row block) tasks on a workgroup takes one whole.  Whole tasks keep the row blocks of a
+// head, which read the same keys, together in time; divided ones end together.  Which counts for more depends on lengths
+// that the host does not know: prompts of 1024 queries over 4096 keys, 2048 equal tasks 622 us whole, 738 divided, 1024
+// tasks 319 and 353; ragged prompts, 1024 tasks 146 and 122, 2048 tasks 238 and 197.
+constexpr int kMlaDivideTasks = 2048;
 
 // Latent form: waves of a workgroup whose row blocks are `row_waves` waves (of 16 rows) high,
 // and its groups, which take 32 keys in turn.
-constexpr int latent_waves(int row_waves) { return row_waves >= 4 ? 8 : 4; }
+constexpr int latent_waves(int row_waves) { return row_waves == 8 ? 8 : 4; }
 constexpr int latent_groups(int row_waves) { return latent_waves(row_waves) / row_waves; }
 
 struct MlaParams {
@@ -94,7 +98,7 @@ struct MlaParams {
   float* part_o;                     // [workgroup][2][rows of a block][columns] unnormalised sums
   float* part_ml;                    // [workgroup][2][rows of a block][4] running maximum (in powers of 2), sum of
                                      // the rounded weights, sum of the weights
-  int32_t* prefix;                   // [n_tasks] units before each task, units of a workgroup, [n_parts] first tasks
+  int32_t* prefix;                   // [n_tasks] cost before each task, cost of a workgroup, [n_parts] first tasks
   uint32_t* status;
   int64_t q_s[2], out_s[2], lse_s[2];
   int64_t pool_s[2];                 // bytes: page, token
@@ -107,11 +111,11 @@ struct MlaParams {
   int32_t group;                     // heads of a token that are rows of one task (latent: all, expanded: 1)
   int32_t task_heads;                // heads that are tasks of their own (latent: 1, expanded: all)
   int32_t rows_block;                // rows of a task
-  int32_t row_waves;                 // latent: waves of a row block, 1, 2, 4 or 8
+  int32_t row_waves;                 // latent: waves of a row block, 1, 2 or 8
   int32_t n_row_blocks;
   int32_t n_tasks;
-  int32_t n_parts;                   // > 0: workgroups among which all tasks' units are divided; 0: one a task
-  int32_t min_units;                 // least units of a workgroup
+  int32_t n_parts;                   // > 0: workgroups among which all tasks' cost is divided; 0: one a task
+  int32_t min_units;                 // least cost of a workgroup
   int32_t unit;                      // keys of a unit
   int32_t fixed;                     // units that a task costs beside its own
   int32_t lanes;                     // of a wave that add up a request's units: a power of two up to 64

@@ -100,7 +100,7 @@ __device__ __forceinline__ int units_of(const Block& b, int unit) {
 
 // What a block costs, in units: p.fixed of them, in which nothing is walked, for taking it
 // up and storing its results, and its own.  Without the first, workgroups with many short
-// blocks end last (ragged prompts of eight requests: 122 us, now XX).
+// blocks end last.
 __device__ __forceinline__ int cost_of(const MlaParams& p, const Block& b, int unit) {
   const int u = units_of(b, unit);
   return u > 0 ? u + p.fixed : 0;

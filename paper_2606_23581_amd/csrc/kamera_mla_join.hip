@@ -4,9 +4,14 @@
 // With M the largest of the parts' maxima m_s,
 //   out = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s.
 // 32 threads take 128 columns of a row's parts: with WAYS > 1 every WAYS-th part, the
-// ways meeting in LDS, else all of them, for one row or for four.  Tasks that were divided are found
-// from where the workgroups' ranges begin: a grid over the ranges where there are
-// fewer of them than tasks, else over the tasks.
+// ways meeting in LDS, else all of them, for one row or for four.  Tasks that were
+// divided are found from where the workgroups' ranges begin: a grid over the ranges where
+// there are fewer of them than tasks, else over the tasks.
+//
+// Bound by latency: a launch, four dependent loads (the task's lengths, its cost, the
+// parts, their sums), and the parts once from the cache beyond the L2s, at 76 MB in
+// 15.6 us (16 requests of 256 rows of 512 columns in 256 ranges), 25 MB in 10 (48 rows
+// in 256 parts).
 
 #include "kamera_mla_device.h"
 
@@ -122,8 +127,11 @@ hipError_t launch_mla_join(const MlaParams& p, hipStream_t s) {
   const int64_t most = (int64_t)p.n_queries * p.group;
   const uint32_t rows = (uint32_t)(most < p.rows_block ? most : p.rows_block), quarters = (uint32_t)(p.dim + 127) >> 7;
   const uint32_t x = (uint32_t)(p.n_tasks < p.n_parts ? p.n_tasks : p.n_parts - 1);
-  // many parts a row: a workgroup a row; ranges that share few rows each: four rows a thread
-  if (p.n_parts >= 16 * (int64_t)p.n_tasks)
+  // Many parts of few rows: a workgroup a row and 128 columns (256 parts of 48 rows of 512 columns, 192 workgroups: 40 us
+  // with the attention, 77 with eight rows a workgroup; 768 workgroups 43.3 and 44.3, 1536 workgroups 52.3 and 39.6).
+  // Else all parts by one thread, and four rows of it where ranges share few tasks (1024 tasks in 512 ranges: 14.7 us,
+  // 20 one row a thread).
+  if (p.n_parts >= 16 * (int64_t)p.n_tasks && x * rows * quarters <= 512)
     hipLaunchKernelGGL((mla_join_kernel<16, 1>), dim3(x, rows * quarters), dim3(512), 0, s, p);
   else if (p.n_tasks < p.n_parts)
     hipLaunchKernelGGL((mla_join_kernel<1, 1>), dim3(x, (rows + 7) / 8 * quarters), dim3(256), 0, s, p);

@@ -11,6 +11,15 @@
 // LDS: 16-byte chunks are exchanged by an exclusive-or with bits of the row number,
 // so that the 16 lanes that read a chunk of 16 rows together, or four rows of 64
 // bytes, spread over all banks.
+//
+// Bound by bytes where a head's matrix is narrow (8192 rows of 16 heads, 512 x 128:
+// 170 MB, 26.8 us of kernel with rows in the cache, 39 us a call without), by the
+// matrix pipe's supply where it is wide (16384 pool rows, 16 heads, 512 x 256: 69
+// GFLOP in 84 us, 820 TFLOP/s; a library product of that shape takes 81): the pipe
+// is busy a third of the time, waits for the next step's tiles the rest, and neither
+// steps of 32 columns in more buffers (103 us) nor 128 x 256 tiles, two to a CU (108),
+// nor workgroups that stay (94) feed it better.  A few rows are a chain of latencies
+// (64 rows of 16 heads, 128 x 512: 4.2 us).
 
 #include "kamera_latent.h"
 #include "kamera_lds_device.h"
@@ -19,16 +28,17 @@ namespace kamera {
 
 namespace {
 
-
 // Place of 16-byte chunk c of row r in a tile of rows of STEP columns.
 template <int STEP>
 __device__ __forceinline__ uint32_t k_place(uint32_t r, uint32_t c) {
-  return STEP == 64 ? r * 128 + ((c ^ ((r >> 1) & 7)) << 4) : r * 64 + ((c ^ ((r >> 2) & 3)) << 4);
+  static_assert(STEP == 64, "");
+  return r * (STEP * 2) + ((c ^ ((r >> 1) & 7)) << 4);
 }
 // ... of a tile of rows of BN columns.
 template <int BN>
 __device__ __forceinline__ uint32_t n_place(uint32_t r, uint32_t c) {
-  return r * (BN * 2) + ((c ^ (BN >= 128 ? (r & 3) << 2 : (r & 2) << 1)) << 4);
+  static_assert(BN >= 128, "");
+  return r * (BN * 2) + ((c ^ (r & 3) << 2) << 4);
 }
 
 }  // namespace
