@@ -14,8 +14,8 @@
 // moves only when a score passes it by more than 8.
 //
 // Bound by issue: five vector instructions for each MFMA, which keeps the matrix pipe
-// busy 43% of the time with two workgroups a CU (81,920 bytes of LDS each, all there
-// is).  1024 queries of 16 heads over 16384 keys: 171 us, 974 TFLOP/s; eight ragged
+// busy 45% of the time with two workgroups a CU (81,920 bytes of LDS each, all there
+// is).  1024 queries of 16 heads over 16384 keys: 172 us, 970 TFLOP/s; eight ragged
 // prompts of up to 1024 queries over up to 2048 keys, 1024 tasks of 1 to 32 tiles: 101 us,
 // where taking a task up and storing its results (some 14000 cycles) weighs as much as
 // its tiles.

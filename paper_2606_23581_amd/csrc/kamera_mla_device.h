@@ -213,8 +213,8 @@ __device__ __forceinline__ Share divide(const MlaParams& p, uint32_t w) {
     s.task = __builtin_amdgcn_readfirstlane(s.task);
     s.skip = __builtin_amdgcn_readfirstlane(s.skip);
   }
-  // for the kernel that joins the parts: the task that each range begins in, and (left by
-  // the workgroup that begins a task) the cost before each task
+  // for the kernel that joins the parts: the task that each range begins in (and, from
+  // take_segment, the cost before each task)
   if (threadIdx.x == 0) p.prefix[p.n_tasks + 1 + w] = (int)s.task;
   s.begin = (int)begin;
   return s;
