@@ -89,7 +89,7 @@ kamera_attend_latent_args latent() {
 kamera_attend_expanded_args expanded() {
   auto a = attend<kamera_attend_expanded_args>();
   a.head_dim = 128; a.rope_cache = at<void>(0x30000000); a.k = at<void>(0x40000000); a.v = at<void>(0x48000000);
-  set(a.q_stride, {3072, 192}); set(a.out_stride, {2048, 128}); set(a.rope_cache_stride, {9216, 576});
+  set(a.q_stride, {3200, 192}); set(a.out_stride, {2048, 128}); set(a.rope_cache_stride, {9216, 576});
   set(a.k_stride, {2048, 128}); set(a.v_stride, {2048, 128});
   return a;
 }
