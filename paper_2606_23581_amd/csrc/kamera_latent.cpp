@@ -396,9 +396,10 @@ int size_mla(const AttendSizes& a, kamera::MlaParams& P, bool& launch, int64_t& 
   if (tasks < 0 || (tasks + 8) * 256 > 0xFFFFFFFFLL) return fail(KAMERA_ERR_RANGE, "%s: too many workgroups for one launch", who);
   P.n_tasks = (int32_t)tasks;
   const int unit = P.unit = a.latent ? 32 * kamera::latent_groups(P.row_waves) : 64;
-  // about 14000 cycles, at some 4500 for 64 keys of the expanded form, 2400 for 32 of the latent one (eight ragged
-  // prompts, expanded: 122 us, 143 without; 64 single queries of 16 heads, latent: 89.4, 91.0)
-  P.fixed = !a.latent ? 4 : (unit == 32 ? 6 : (unit == 64 ? 3 : 1));
+  // what 256 keys cost, 288 of the latent form (us with none of it, half of it, all, half as much again: eight ragged
+  // prompts, expanded, 143, 123, 115, 116; 64 single queries of 16 heads, latent, 91.0, 89.3, 87.8, 88.0; 16 requests of
+  // two queries of 128 heads 90 with 128 keys, 87.4 with 192, 85.3 with 288, 86.2 with 384)
+  P.fixed = (a.latent ? 288 : 256) / unit;
   P.lanes = 1;
   while (P.lanes < 64 && P.lanes < P.n_row_blocks) P.lanes *= 2;
   int64_t keys = a.n_keys;
