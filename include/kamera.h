@@ -746,7 +746,9 @@ typedef struct {
  * (KAMERA_STATUS_BAD_PAGE); their queries are rotated all the same.
  * Outputs must not overlap inputs or each other (checked on the extents that
  * the sizes imply; rows of one tensor that lie beside each other, the same
- * strides and disjoint columns, are no overlap). */
+ * strides and disjoint columns, are no overlap).  Where two rows of an output
+ * share memory (two chunks with the same new page, a stride of 0) the result
+ * is either's; in place such rows have none. */
 typedef struct {
   int32_t n_chunks;
   int32_t n_layers;
