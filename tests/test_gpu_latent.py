@@ -545,6 +545,64 @@ def test_attend_a_query_that_is_not_finite_stays_in_its_row(form):
     assert torch.equal(got, want)
 
 
+def test_attend_views():
+    """Tensors in other orders and inside wider ones give the same bits as packed ones: heads outermost, tokens of
+    all layers side by side, pages in reverse of the allocation, results and sums between other columns."""
+    rng = np.random.default_rng(4)
+    kv, nq, H = [300, 90], [5, 20], 6
+    table, pages = table_for(rng, kv, 16)
+    table, base, n = i32(table), i32([0, 5]), 25
+    rand = lambda *shape: bf16(rng.standard_normal(shape))[0]
+    wide = rand(16, pages, 3, 640)                 # token, page, layer, columns
+    cache = wide[:, :, 1, 32:608].transpose(0, 1)
+    q = rand(H, n, 648)[..., 8:584].transpose(0, 1)
+    ex = rand(H, sum(kv), 264)[..., 8:].transpose(0, 1)
+    kw = dict(n_queries=20, n_keys=300, scale=0.05, q_base=base, q_tokens=i32(nq))
+    for parts in (0, 9):
+        kw["n_parts"] = parts
+        out = [torch.full((H, n, 528), 7.0, dtype=torch.bfloat16, device=DEV), torch.zeros(n, H, 512, dtype=torch.bfloat16, device=DEV)]
+        lse = [torch.full((H, 2, n), 7.0, device=DEV), torch.zeros(n, H, device=DEV)]
+        km.attend_latent(q, cache, out[0][..., 8:520].transpose(0, 1), table, i32(kv), lse=lse[0][:, 1].transpose(0, 1), **kw)
+        km.attend_latent(q.contiguous(), cache.contiguous(), out[1], table, i32(kv), lse=lse[1], **kw)
+        assert torch.equal(out[0][..., 8:520].transpose(0, 1), out[1]) and out[1].abs().sum() > 0
+        assert torch.equal(lse[0][:, 1].transpose(0, 1), lse[1])
+        assert (out[0][..., :8] == 7.0).all() and (out[0][..., 520:] == 7.0).all() and (lse[0][:, 0] == 7.0).all()
+        out = [torch.full((H, n, 144), 7.0, dtype=torch.bfloat16, device=DEV), torch.zeros(n, H, 128, dtype=torch.bfloat16, device=DEV)]
+        kx = dict(kw, kv_base=i32([0, 300]))
+        km.attend_expanded(q[..., :192], ex[..., 128:], ex[..., :128], cache[..., 512:], out[0][..., 8:136].transpose(0, 1), table,
+                           i32(kv), lse=lse[0][:, 1].transpose(0, 1), **kx)
+        km.attend_expanded(q[..., :192].contiguous(), ex[..., 128:].contiguous(), ex[..., :128].contiguous(),
+                           cache[..., 512:].contiguous(), out[1], table, i32(kv), lse=lse[1], **kx)
+        assert torch.equal(out[0][..., 8:136].transpose(0, 1), out[1]) and out[1].abs().sum() > 0
+        assert torch.equal(lse[0][:, 1].transpose(0, 1), lse[1])
+        assert (out[0][..., :8] == 7.0).all() and (out[0][..., 136:] == 7.0).all()
+    # one key and value for all heads (a head stride of 0), as heads of their own
+    one = [torch.zeros(n, H, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    k1 = ex[:, :1, 128:].expand(-1, H, -1)
+    km.attend_expanded(q[..., :192], k1, k1, cache[..., 512:], one[0], table, i32(kv), **kx)
+    km.attend_expanded(q[..., :192], k1.contiguous(), k1.contiguous(), cache[..., 512:], one[1], table, i32(kv), **kx)
+    assert torch.equal(*one) and one[0].abs().sum() > 0
+
+
+def test_expand_views():
+    """The pool's columns from a wider row, W shared by all heads, results with heads outermost."""
+    rng = np.random.default_rng(6)
+    kv, H = [200, 1, 70], 3
+    table, pages = table_for(rng, kv, 16)
+    rand = lambda *shape: bf16(rng.standard_normal(shape))[0]
+    cache = rand(16, pages, 2, 640)[:, :, 1, 64:].transpose(0, 1)
+    for w in (rand(H, 512, 192), rand(1, 512, 256).expand(H, -1, -1), rand(H, 192, 512).transpose(1, 2)):
+        out = [torch.full((H, 271, w.shape[2] + 16), 7.0, dtype=torch.bfloat16, device=DEV),
+               torch.zeros(271, H, w.shape[2], dtype=torch.bfloat16, device=DEV)]
+        kw = dict(n_keys=200, row_base=i32([0, 200, 201]))
+        view = out[0][..., 8:-8].transpose(0, 1)
+        km.expand_latent(cache, w, view, i32(table), i32(kv), **kw)
+        km.expand_latent(cache.contiguous(), w.contiguous(), out[1], i32(table), i32(kv), **kw)
+        # the two orders of W sum the same products in the same order
+        assert torch.equal(view, out[1]) and out[1].abs().sum() > 0
+        assert (out[0][..., :8] == 7.0).all() and (out[0][..., -8:] == 7.0).all()
+
+
 @pytest.mark.parametrize("form", ["latent", "expanded"])
 def test_attend_repeats_bit_for_bit(form):
     for name in ("long", "chunk"):
