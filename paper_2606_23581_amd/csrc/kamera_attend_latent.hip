@@ -25,10 +25,10 @@
 // moves only when a score passes it by more than 8.
 //
 // Single queries of 16 heads are bound by HBM (64 requests of up to 8192 keys: 378 MB in
-// 80 us, 4.7 TB/s).  With more rows LDS is: 16 rows of a wave read 36 KB for the scores of
-// 32 keys and 32 KB for the results, and eight waves of these keep a CU's LDS at work for
-// longer than its matrix pipes (two queries of 128 heads, 16 requests of up to 8192 keys:
-// 72 us, 46 GFLOP, pipes busy 25%).  Short calls are a chain of latencies (256 keys:
+// 80 us, 4.7 TB/s).  With more rows the reads of LDS bound it: a wave reads 36 KB for the
+// scores of its 16 rows with 32 keys and 32 KB for their results, eight waves 550 KB, 4300
+// cycles at 128 bytes a cycle (measured 1.8 us for 32 more keys), beside 2200 of products (two queries
+// of 128 heads, 16 requests of up to 8192 keys: 72 us, 46 GFLOP, pipes busy 25%).  Short calls are a chain of latencies (256 keys:
 // 12 us, one workgroup).
 
 #include "kamera_mla_device.h"
