@@ -393,7 +393,8 @@ int size_mla(const AttendSizes& a, kamera::MlaParams& P, bool& launch, int64_t& 
   P.rows_block = a.latent ? 16 * P.row_waves : 128;
   P.n_row_blocks = (int32_t)ceil_div(rows, P.rows_block);
   const int64_t tasks = bounded_product({a.n_requests, P.task_heads, P.n_row_blocks});
-  if (tasks < 0 || (tasks + 8) * 256 > 0xFFFFFFFFLL) return fail(KAMERA_ERR_RANGE, "%s: too many workgroups for one launch", who);
+  const int threads = a.latent ? kamera::latent_waves(P.row_waves) * 64 : 256;
+  if (tasks < 0 || (tasks + 8) * threads > 0xFFFFFFFFLL) return fail(KAMERA_ERR_RANGE, "%s: too many workgroups for one launch", who);
   P.n_tasks = (int32_t)tasks;
   const int unit = P.unit = a.latent ? 32 * kamera::latent_groups(P.row_waves) : 64;
   // what 256 keys cost, 288 of the latent form (us with none of it, half of it, all, half as much again: eight ragged

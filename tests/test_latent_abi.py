@@ -244,6 +244,22 @@ def test_validation(which, change, code):
     assert (km.last_error() == "") == (code == km.OK)
 
 
+def test_launches_past_32_bits_of_threads_are_refused():
+    """A workgroup of the latent form has 256 threads, 512 where a block has more than 32 rows; of the expanded 256."""
+    def code(which, requests, **kw):
+        a = MAKE[which](n_requests=requests, n_keys=16, pt_stride=1, workspace=None, q_base=P, **kw)
+        return km.lib().kamera_validate_latent(which, ctypes.byref(a))
+
+    for heads, block, threads in ((16, 16, 256), (32, 32, 256), (48, 128, 512), (128, 128, 512)):
+        for n_queries in (1, 1 << 17) if heads == 128 else (1,):
+            blocks = -(-n_queries * heads // block)              # of a request; a workgroup each
+            most = (1 << 32) // threads // blocks
+            assert code(3, most, n_heads=heads, n_queries=n_queries) == km.ERR_RANGE
+            assert code(3, most - 16, n_heads=heads, n_queries=n_queries) == km.OK, km.last_error()
+    assert code(4, 1 << 20, kv_base=P) == km.ERR_RANGE           # 2^20 requests of 16 heads
+    assert code(4, (1 << 20) - 1, kv_base=P) == km.OK, km.last_error()
+
+
 def test_validation_of_nothing():
     L = km.lib()
     for which in range(5):
