@@ -26,13 +26,13 @@ __device__ __forceinline__ uint32_t lds_offset(const void* p) { return (uint32_t
 // wave-uniform).  The instructions are written out because the compiler, which
 // cannot tell the tile that is being loaded from the one that is being read, would
 // wait for all of them before each read of LDS; vm_wait stands where a tile has to
-// be there.  No register is written, and the address registers are read at issue.
+// be there.  No register but m0 is written, and the address registers are read at issue.
 __device__ __forceinline__ void load_lds(const uint8_t* base, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
 }
 __device__ __forceinline__ void load_lds(uint64_t address, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(address)
-               : "memory");
+               : "memory", "m0");
 }
 
 // Until at most N of the wave's loads are under way.

@@ -417,3 +417,42 @@ def test_host_layer_under_address_and_undefined_behaviour_sanitizers(tmp_path):
 
 def test_host_layer_under_thread_sanitizer(tmp_path):
     _host_program(tmp_path, "latent_tsan", ["-fsanitize=thread"])
+
+
+MIXED_LOADS = """
+#include "kamera_lds_device.h"
+using namespace kamera;
+// a load into LDS by the compiler, one by load_lds, and one by the compiler to the first one's place
+template <bool PAIR>
+__global__ void mixed_loads(const uint8_t* a, const uint8_t* b, uint32_t* out) {
+  __shared__ uint32_t s[4096];
+  const auto lds = (__attribute__((address_space(3))) void*)s;
+  __builtin_amdgcn_global_load_lds((GlobalBytes)(a + threadIdx.x * 16), lds, 16, 0, 0);
+  if (PAIR) load_lds(b, threadIdx.x * 16, lds_offset(s) + 4096);
+  else load_lds((uint64_t)b + threadIdx.x * 16, lds_offset(s) + 4096);
+  __builtin_amdgcn_global_load_lds((GlobalBytes)(a + 4096 + threadIdx.x * 16), lds, 16, 64, 0);
+  vm_wait<0>();
+  out[threadIdx.x] = s[threadIdx.x + 64];
+}
+template __global__ void mixed_loads<true>(const uint8_t*, const uint8_t*, uint32_t*);
+template __global__ void mixed_loads<false>(const uint8_t*, const uint8_t*, uint32_t*);
+"""
+
+
+def test_loads_into_lds_say_that_they_write_m0(tmp_path):
+    """load_lds sets m0, which holds the place in LDS of every such load: the compiler, which sets it for its own ones,
+    has to set it anew behind it."""
+    hipcc = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
+    if not os.path.exists(hipcc):
+        pytest.skip("no hipcc")
+    src, asm = tmp_path / "mixed_loads.hip", tmp_path / "mixed_loads.s"
+    src.write_text(MIXED_LOADS)
+    r = subprocess.run([hipcc, "-S", "--cuda-device-only", "-O3", "--offload-arch=gfx950", "-std=c++17", "-I",
+                        os.path.join(ROOT, "include"), "-I", CSRC, str(src), "-o", str(asm)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+    kernels = [k.split("s_endpgm")[0] for k in asm.read_text().split("; -- Begin function")[1:]]
+    assert len(kernels) == 2
+    for k in kernels:
+        loads = k.split("global_load_lds_dwordx4")
+        assert len(loads) == 4                                   # three loads, m0 set before each
+        assert all("s_mov_b32 m0" in before for before in loads[:3]), k
