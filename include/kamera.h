@@ -841,7 +841,11 @@ typedef struct {
  *               scale * <q[i][g], x[t]>.
  * Which keys a query sees, rows that see none, values in what a row does not
  * see, lse, pages outside the pool and the precision of sums and weights are as
- * in kamera_attend_paged.
+ * in kamera_attend_paged.  A value that is not finite in a key that a row does
+ * see leaves that column of the row not finite, also where the key's weight is 0
+ * or falls to 0 beside larger ones (a row whose every score is -infinity gets 0
+ * in its other columns): there it is an infinity or NaN, whichever the order of
+ * the work gives.
  *
  * The work is spread evenly over n_parts workgroups (0: chosen from the
  * sizes); where that divides a row's keys a second kernel on the same stream

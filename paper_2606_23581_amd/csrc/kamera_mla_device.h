@@ -274,8 +274,9 @@ __device__ __forceinline__ bool clean_chunk(uint32_t at) {
 // A value that is not finite must reach the rows that see its key, and no others:
 // 0 * NaN is NaN, so the product over keys that some rows see and others do not leaves
 // such values out, and this adds them to those rows' results in memory afterwards (v
-// itself: any positive weight of it is the same).  It runs only where the workgroup met
-// one.  Keys [from, to) in steps of `step`; value_at(key): its row of values, or null
+// itself: any positive weight of it is the same; with a weight of 0 an infinity stays one
+// here and is NaN in the product and the join, not finite in either).  It runs only where
+// the workgroup met one.  Keys [from, to) in steps of `step`; value_at(key): its row of values, or null
 // where its page is outside the pool.  Called by all threads after their results are
 // stored; a column is one thread's.
 template <typename F>

@@ -518,6 +518,70 @@ def test_attend_values_that_a_row_does_not_see(form, parts, what, name):
                     assert (got[0][i, h, cols] == x).all()
 
 
+def weightless(form, kv, nq, keys, parts, alone=False):
+    """One request of `nq` queries of 4 heads over `kv` keys, of which `keys` (with `alone` all) have a weight of 0 and
+    a value in column 5 that is not finite: got out, got lse, and what the other keys give (as `attend` does), seen."""
+    rng = np.random.default_rng(11)
+    H, D = 4, 256 if form == "latent" else 64
+    table, pool = table_for(rng, [kv], 16)
+    rows, rows64 = bf16(rng.standard_normal((pool, 16, (D if form == "latent" else 256) + 64)))
+    q, _ = bf16(rng.standard_normal((nq, H, D + 64)))
+    ex, ex64 = bf16(rng.standard_normal((kv, H, 2 * D)))
+    keys = list(range(kv)) if alone else keys
+    if form == "latent":                           # the score is -infinity by the value itself
+        q[..., 5] = 1.0
+        for t in keys:
+            rows[table[0, t // 16], t % 16, 5] = -float("inf")
+    else:                                          # far below the others', or -infinity
+        q[..., 0] = 8.0
+        ex[..., 0], ex64[..., 0] = 0.0, 0.0
+        for t in keys:
+            ex[t, :, 0], ex[t, :, D + 5] = -float("inf") if alone else -30000.0, float("inf")
+    q64 = values(q)
+    out, lse = torch.zeros(nq, H, D, dtype=torch.bfloat16, device=DEV), torch.zeros(nq, H, device=DEV)
+    kw = dict(n_queries=nq, n_keys=kv, scale=0.08, lse=lse, n_parts=parts)
+    if form == "latent":
+        km.attend_latent(q, rows, out, i32(table), i32([kv]), **kw)
+    else:
+        km.attend_expanded(q, ex[..., :D], ex[..., D:], rows[..., -64:], out, i32(table), i32([kv]), **kw)
+    x, ok = ref.gather(rows64, table[0], kv, 16)
+    seen = ref.seen_keys(kv, nq, True, 0, ok)
+    rest = seen.copy()
+    rest[:, keys] = False
+    if form == "latent":
+        k, v = x[None], x[None, :, :D]
+    else:
+        e = ex64.transpose(1, 0, 2)
+        k, v = np.concatenate([e[..., :D], np.broadcast_to(x[None, :, -64:], (H, kv, 64))], -1), e[..., D:]
+    want, size, want_lse, most = ref.attend_rows(q64, k, v, rest, 0.08)
+    return values(out), values(lse), want, size, want_lse, most * (D + 64 + 8) * 2.0 ** -24, seen[:, keys].any(1)
+
+
+@pytest.mark.parametrize("form", ["latent", "expanded"])
+@pytest.mark.parametrize("parts", [0, 1, 3, 50])
+@pytest.mark.parametrize("keys", [[10], [291], [40, 100, 285]])
+@pytest.mark.parametrize("nq", [2, 20])
+def test_attend_a_value_that_is_not_finite_with_no_weight(form, parts, keys, nq):
+    """A key that a row sees with a weight of 0, in steps that all rows see whole and in others: its value that is not
+    finite leaves that column not finite, whatever divides the keys, and nothing else of the row."""
+    *got, seen = weightless(form, 300, nq, keys, parts)
+    assert not np.isfinite(got[0][seen][..., 5]).any()
+    assert np.isfinite(got[0][~seen]).all()
+    got[0][seen, :, 5], got[2][seen, :, 5] = 0.0, 0.0
+    check(*got)
+
+
+@pytest.mark.parametrize("form", ["latent", "expanded"])
+@pytest.mark.parametrize("parts", [0, 1, 9])
+@pytest.mark.parametrize("kv,nq", [(1, 1), (5, 3), (70, 1), (200, 40)])
+def test_attend_rows_whose_every_score_is_minus_infinity(form, parts, kv, nq):
+    """They get 0 and an lse of -infinity, but for a column whose values are not finite."""
+    out, lse = weightless(form, kv, nq, [], parts, alone=True)[:2]
+    assert not np.isfinite(out[..., 5]).any()
+    assert (out[..., :5] == 0).all() and (out[..., 6:] == 0).all()
+    assert (lse == -np.inf).all()
+
+
 @pytest.mark.parametrize("form", ["latent", "expanded"])
 def test_attend_a_query_that_is_not_finite_stays_in_its_row(form):
     torch.manual_seed(0)
