@@ -582,6 +582,30 @@ def test_attend_rows_whose_every_score_is_minus_infinity(form, parts, kv, nq):
     assert (lse == -np.inf).all()
 
 
+@pytest.mark.parametrize("parts", [0, 3, 50])
+@pytest.mark.parametrize("name", sorted(POISON_CASES))
+@pytest.mark.parametrize("what", ["nan", "inf", "-inf"])
+def test_attend_latent_values_arrive_at_the_rows_that_see_them(name, what, parts):
+    """A NaN in a pool row makes its score NaN, and so the whole of every row that sees it; an infinity makes its column
+    not finite there."""
+    c = POISON_CASES[name]
+    kv, nq = c["kv"][0], c["nq"][0]
+    keys = [kv - 1, kv - 3, max(0, kv - nq - 2), max(0, kv - nq - 25)]
+
+    def poison(rows, rows64, table):
+        for t in keys:
+            rows[table[0, t // 16], t % 16, 5 + t % 7] = float(what)
+
+    got, lse = attend("latent", c, parts=parts, poison=poison)[:2]
+    per = ref.seen_keys(kv, nq, True, c.get("window", 0), np.ones(kv, dtype=bool))[:, keys]
+    assert per.any()
+    for i in np.flatnonzero(per.any(1)):
+        if what == "nan":
+            assert np.isnan(got[i]).all() and np.isnan(lse[i]).all()
+        else:
+            assert not np.isfinite(got[i][:, sorted({5 + t % 7 for t, there in zip(keys, per[i]) if there})]).any()
+
+
 @pytest.mark.parametrize("form", ["latent", "expanded"])
 def test_attend_a_query_that_is_not_finite_stays_in_its_row(form):
     torch.manual_seed(0)
