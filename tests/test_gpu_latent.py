@@ -324,6 +324,25 @@ def test_expand_latent(lengths, page, heads, n_in, n_out, w_rows):
         assert (out2[r * max(lengths) + n:(r + 1) * max(lengths)] == 5.0).all()
 
 
+# Shapes that are taken in tiles of 256 rows and columns (test_latent_abi.py asserts that they are).
+PROJECT_256 = [(515, 85, 192, 512), (257, 97, 128, 256), (300, 64, 512, 512)]          # rows, heads, in, out
+EXPAND_256 = [([257, 31, 300] * 16, 16, 4, 192, 256), ([300, 0, 256, 255] * 12, 64, 2, 512, 512),  # lengths, page, heads, in, out
+              ([1100, 1300], 7, 20, 320, 256)]
+
+
+@pytest.mark.parametrize("w_rows", [True, False])
+@pytest.mark.parametrize("rows,heads,n_in,n_out", PROJECT_256)
+def test_project_heads_in_tiles_of_256(rows, heads, n_in, n_out, w_rows):
+    test_project_heads(rows, heads, n_in, n_out, w_rows)
+
+
+@pytest.mark.parametrize("w_rows", [True, False])
+@pytest.mark.parametrize("lengths,page,heads,n_in,n_out", EXPAND_256)
+def test_expand_latent_in_tiles_of_256(lengths, page, heads, n_in, n_out, w_rows):
+    """Ragged requests, and one with a page outside the pool."""
+    test_expand_latent(lengths, page, heads, n_in, n_out, w_rows)
+
+
 # ---------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------

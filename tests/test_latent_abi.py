@@ -456,3 +456,24 @@ def test_loads_into_lds_say_that_they_write_m0(tmp_path):
         loads = k.split("global_load_lds_dwordx4")
         assert len(loads) == 4                                   # three loads, m0 set before each
         assert all("s_mov_b32 m0" in before for before in loads[:3]), k
+
+
+def test_tiles_of_the_products(tmp_path):
+    """The tile that the host picks for the shapes of the GPU tests of each one."""
+    from tests import test_gpu_latent as gpu
+
+    if shutil.which("g++") is None or not os.path.exists("/opt/rocm/include/hip/hip_runtime_api.h"):
+        pytest.skip("no g++ or HIP headers")
+    exe = str(tmp_path / "latent_params")
+    r = subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-D__HIP_PLATFORM_AMD__", "-I", "/opt/rocm/include", "-I",
+                        os.path.join(ROOT, "include"), "-I", CSRC, "-I", TC,
+                        *[os.path.join(CSRC, f) for f in ("kamera_abi.cpp", "kamera_latent.cpp")],
+                        *[os.path.join(TC, f) for f in ("launch_stub.cpp", "latent_params.cpp")], "-o", exe, "-pthread"],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+    calls = [("project", 1, *c, 256) for c in gpu.PROJECT_256]
+    calls += [("expand", len(c[0]), max(c[0]), *c[2:], 256) for c in gpu.EXPAND_256]
+    calls += [("project", 1, 64, 16, 128, 512, 32), ("project", 1, 65, 3, 64, 192, 128), ("expand", 4, 300, 4, 256, 256, 128)]
+    for *call, rows in calls:
+        r = subprocess.run([exe, *map(str, call)], capture_output=True, text=True, timeout=60)
+        assert r.returncode == 0 and int(r.stdout) == rows, (call, r.stdout, r.stderr)
