@@ -947,3 +947,55 @@ def test_calls_on_a_given_stream():
     torch.cuda.synchronize()
     for d in (o, e, r, x):
         assert torch.equal(d["a"], d["b"]) and d["a"].abs().sum() > 0
+
+
+@pytest.mark.parametrize("heads", [16, 40])
+def test_prompt_and_decode_over_recalled_rows(heads):
+    """Two chunks rebuilt by rehydrate at their new places, a question behind them and a token behind that: rows in the
+    pool, both forms of attention and the products, each link in 64 bits from what it was handed."""
+    y = Layer(heads=heads, seed=3)
+    n, nq, H = 48, 20, heads
+    chunks = y.rand(2, 1, n, 1, 576)
+    table = i32([[7, 2, 31, 4, 0, 9, 12, 30]])     # the chunks' pages, then the question's
+    km.rehydrate(chunks, y.pool.view(1, -1, 1, 576), rope=y.rope, chunk_pos=i32([[0] * 3, [n] * 3]),
+                 page_table=table[0, :6].view(2, 3).contiguous(), page_size=16, n_pool_pages=y.pool.shape[0])
+    new, q = y.rand(nq + 1, 576), y.rand(nq + 1, H, 192)
+    q_lat = torch.zeros(nq + 1, H, 576, dtype=torch.bfloat16, device=DEV)
+    o_lat = torch.zeros(nq + 1, H, 512, dtype=torch.bfloat16, device=DEV)
+    out = torch.zeros(nq + 1, H, 128, dtype=torch.bfloat16, device=DEV)
+    rows = torch.zeros(128, H, 256, dtype=torch.bfloat16, device=DEV)
+    a, b = slice(0, nq), slice(nq, nq + 1)         # the question, in the expanded form; the token, in the absorbed one
+    y.append(new[a], q[a], q_lat[a], table, i32([2 * n]), nq, i32([0]))
+    km.expand_latent(y.pool, y.w.transpose(1, 2), rows, table, i32([2 * n + nq]), n_keys=128)
+    q_exp = torch.cat([q[a, :, :128], q_lat[a, :, 512:]], -1)
+    lse = torch.zeros(nq + 1, H, device=DEV)
+    km.attend_expanded(q_exp, rows[..., :128], rows[..., 128:], y.pool[..., 512:], out[a], table, i32([2 * n + nq]),
+                       n_queries=nq, n_keys=128, scale=y.scale, lse=lse[a])
+    y.append(new[b], q[b], q_lat[b], table, i32([2 * n + nq]), 1, i32([0]))
+    y.absorbed(q[b], q_lat[b], table, i32([2 * n + nq + 1]), 1, 128, o_lat[b], out[b], lse=lse[b])
+    torch.cuda.synchronize()
+
+    kv = 2 * n + nq + 1
+    pool = values(y.pool[table[0].long()]).reshape(128, 576)
+    src = np.concatenate([values(chunks).reshape(2 * n, 576), values(new)])
+    f = ref.frequencies(1e4, 64)
+    for t in range(kv):
+        r, size = ref.rotate(src[t, 512:], t * f, "interleaved")
+        assert (np.abs(pool[t, 512:] - r) <= U * np.abs(r) + 2.0 ** -18 * size).all()
+    np.testing.assert_array_equal(pool[:kv, :512], src[:, :512])
+    for i in range(nq + 1):
+        r, size = ref.rotate(values(q[i, :, 128:]), (2 * n + i) * f, "interleaved")
+        assert (np.abs(values(q_lat[i, :, 512:]) - r) <= U * np.abs(r) + 2.0 ** -18 * size).all()
+    w, ex = values(y.w), values(rows)
+    for h in range(H):
+        for got, x, m in ((ex[:kv - 1, h], pool[:kv - 1, :512], w[h].T), (values(q_lat[b, h, :512]), values(q[b, h, :128]), w[h, :128]),
+                          (values(out[b, h]), values(o_lat[b, h]), w[h, 128:].T)):
+            want, tol = product_bound(x, m)
+            assert (np.abs(got - want) <= tol).all()
+    e = ex[:kv - 1].transpose(1, 0, 2)
+    k = np.concatenate([e[..., :128], np.broadcast_to(pool[None, :kv - 1, 512:], (H, kv - 1, 64))], -1)
+    seen = ref.seen_keys(kv - 1, nq, True, 0, np.ones(kv - 1, dtype=bool))
+    want = ref.attend_rows(values(q_exp), k, e[..., 128:], seen, y.scale)
+    check(values(out[a]), values(lse[a]), *want[:3], want[3] * (192 + 8) * 2.0 ** -24)
+    want = ref.attend_rows(values(q_lat[b]), pool[None, :kv], pool[None, :kv, :512], np.ones((1, kv), dtype=bool), y.scale)
+    check(values(o_lat[b]), values(lse[b]), *want[:3], want[3] * (576 + 8) * 2.0 ** -24)
