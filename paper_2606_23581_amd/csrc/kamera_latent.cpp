@@ -22,32 +22,36 @@ struct View {
   const int64_t* ext;
   int nd;
   int64_t width;
+  int open = -1;                     // a dimension of which only one element is known to be there
 };
 
 bool range_of(const View& v, Range& r) { return span(v.base, v.s, v.ext, v.nd, v.width, 2, r.lo, r.hi); }
 
-// Two views whose ranges overlap, but not their elements: with the same outer
-// strides, the inner blocks of one lie beside those of the other (keys and values of a
-// token, columns of one row).
-bool beside(const View& a, const View& b) {
-  const View& lo = (uintptr_t)a.base <= (uintptr_t)b.base ? a : b;
-  const View& hi = &lo == &a ? b : a;
-  const __int128 d = (__int128)(uintptr_t)hi.base - (uintptr_t)lo.base;
-  if (d % 2 != 0 || a.nd != b.nd) return false;
-  for (int k = 0; k < a.nd; ++k) {
-    if (a.s[k] != b.s[k] || a.s[k] < 0) return false;
-    // blocks of the dimensions behind k, side by side in a stride of k
-    __int128 in_lo = lo.width, in_hi = hi.width;
-    bool whole = true;
-    for (int j = k + 1; j < a.nd; ++j) {
-      if (lo.s[j] < 0 || hi.s[j] < 0) whole = false;
-      in_lo += (__int128)(lo.ext[j] - 1) * lo.s[j];
-      in_hi += (__int128)(hi.ext[j] - 1) * hi.s[j];
-    }
-    for (int j = 0; j < k; ++j)
-      if (std::max(a.ext[j], b.ext[j]) > 1 && (a.s[k] == 0 || a.s[j] % a.s[k] != 0)) whole = false;
-    if (whole && in_lo <= d / 2 && d / 2 + in_hi <= a.s[k]) return true;
+// Where the elements of a view lie within a stride `s`: in its first `in` places, counted from the base; false
+// where that is not so.  Dimensions of a multiple of s leave an element's place as it is.
+bool within(const View& v, int64_t s, __int128& in) {
+  in = v.width;
+  for (int k = 0; k < v.nd; ++k) {
+    if (v.s[k] % s == 0 || (v.ext[k] <= 1 && k != v.open)) continue;
+    if (v.s[k] < 0 || (k == v.open && v.s[k] > s)) return false;
+    in += (__int128)(v.ext[k] - 1) * v.s[k];
   }
+  return in <= s;
+}
+
+// Two views whose ranges overlap, but not their elements: the places of one within some stride lie beside those of
+// the other (keys and values of a token, columns of one row).
+bool beside(const View& a, const View& b) {
+  const __int128 d = (__int128)(uintptr_t)b.base - (__int128)(uintptr_t)a.base;
+  if (d % 2 != 0) return false;
+  for (const View* v : {&a, &b})
+    for (int k = 0; k < v->nd; ++k) {
+      const int64_t s = v->s[k];
+      __int128 in_a, in_b;
+      if (s <= 0 || !within(a, s, in_a) || !within(b, s, in_b)) continue;
+      const __int128 at = (d / 2 % s + s) % s;     // b's first place, a's being 0
+      if (in_a <= at && at + in_b <= s) return true;
+    }
   return false;
 }
 
@@ -167,10 +171,11 @@ int build_rotate(const kamera_append_rotated_args* a, kamera::RotateParams& P, b
   const int64_t ext_q[4] = {a->n_chunks, a->n_layers, n, qh};
   const int64_t ext_kc[4] = {a->n_layers, a->n_pool_pages, a->page_size, kh};
   const int64_t ext_vc[4] = {a->n_layers, a->n_pool_pages, a->page_size, vh};
-  const View in[3] = {{a->k, a->k_stride, ext_k, 4, a->k_dim}, {a->v, a->v_stride, ext_v, 4, a->v_dim},
-                      {a->q, a->q_stride, ext_q, 4, a->rope.rope_dim}};
+  const int open = a->row_base != nullptr ? 2 : -1;
+  const View in[3] = {{a->k, a->k_stride, ext_k, 4, a->k_dim, open}, {a->v, a->v_stride, ext_v, 4, a->v_dim, open},
+                      {a->q, a->q_stride, ext_q, 4, a->rope.rope_dim, open}};
   const View out[3] = {{a->k_cache, a->k_cache_stride, ext_kc, 4, a->k_dim}, {a->v_cache, a->v_cache_stride, ext_vc, 4, a->v_dim},
-                       {a->q_out, a->q_out_stride, ext_q, 4, a->rope.rope_dim}};
+                       {a->q_out, a->q_out_stride, ext_q, 4, a->rope.rope_dim, open}};
   const int64_t heads[3] = {kh, vh, qh};
   Range in_r[3] = {}, out_r[3] = {};
   for (int i = 0; i < 3; ++i)

@@ -7,6 +7,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import random
 import shutil
 import subprocess
 
@@ -242,6 +243,75 @@ def test_validation(which, change, code):
     a = MAKE[which](**change)
     assert km.lib().kamera_validate_latent(which, ctypes.byref(a)) == code, km.last_error()
     assert (km.last_error() == "") == (code == km.OK)
+
+
+# Pools whose strides do not fall from the first dimension to the last, keys and values beside each other in every
+# (page, layer), every token, every head: pages outermost, heads outermost, tokens outermost.
+@pytest.mark.parametrize("order", ["page layer plane token head", "head page plane layer token", "token page layer plane head",
+                                   "plane token head layer page", "page layer head token plane", "layer page token plane head"])
+def test_keys_and_values_beside_each_other_in_any_order(order):
+    size = dict(page=10, layer=3, token=16, head=4, plane=2)
+    stride, at = {}, 128
+    for d in reversed(order.split()):
+        stride[d], at = at, at * size[d]
+    strides = tuple(stride[d] for d in ("layer", "page", "token", "head"))
+
+    def code(shift=0):
+        a = rotate_args(k_cache_stride=strides, v_cache_stride=strides, v_cache=0x30000000 + 2 * (stride["plane"] + shift))
+        return km.lib().kamera_validate_latent(0, ctypes.byref(a))
+
+    assert code() == km.OK, km.last_error()
+    for shift in (-8, 8, 64, -stride["plane"]):
+        met = bool(_elements(0, strides, (3, 10, 16, 4), 128) & _elements(stride["plane"] + shift, strides, (3, 10, 16, 4), 128))
+        assert not met or code(shift) == km.ERR_ALIAS, shift
+
+
+def _elements(base, strides, sizes, width):
+    x = [base]
+    for s, n in zip(strides, sizes):
+        x = [y + i * s for y in x for i in range(n)]
+    return {y + c for y in x for c in range(0, width, 8)}
+
+
+def test_bands_beside_each_other_in_packed_rows():
+    """Queries' bands in and out in one tensor of rows behind row bases, of which no number is known."""
+    def code(q_row, out_row, out_at, head=128):
+        a = rotate_args(row_base=P + 0x100, k_stride=(0, 20480, 512, 128), v_stride=(0, 20480, 512, 128),
+                        q_stride=(0, 1 << 20, q_row, head), q_out=0x22000000 + 2 * out_at, q_out_stride=(0, 1 << 20, out_row, head))
+        return km.lib().kamera_validate_latent(0, ctypes.byref(a))
+
+    assert code(1024, 1024, 64) == km.OK, km.last_error()        # columns of a head
+    assert code(2048, 2048, 1024) == km.OK, km.last_error()      # heads of a row
+    assert code(1024, 1024, 1 << 19) == km.OK, km.last_error()   # rows of a layer
+    assert code(1024, 2048, 64) == km.OK, km.last_error()        # every other row's
+    assert code(1024, 1024, 56) == km.ERR_ALIAS
+    assert code(1000, 1024, 64) == km.ERR_ALIAS                  # the second rows meet
+
+
+def test_outputs_that_meet_are_refused_whatever_their_strides():
+    """Two pools at random strides, also 0 and negative ones, and distances: every pair that shares memory is refused."""
+    rng = random.Random(0)
+    sizes, allowed = (2, 3, 4, 2), 0
+    for _ in range(3000):
+        dims = [0, 1, 2, 3, 4]
+        rng.shuffle(dims)                          # 4: keys or values
+        stride, at = [0] * 5, 16
+        for d in dims:
+            stride[d] = at * rng.choice((1, 1, 1, 1, 1, -1))
+            at *= (2 if d == 4 else sizes[d]) + rng.choice((0, 0, 0, 1))
+        other = list(stride)
+        if rng.random() < 0.3:
+            other[rng.randrange(4)] = 8 * rng.randrange(-6, 12)
+        apart = stride[4] + 8 * rng.choice((0, 0, 0, 1, -1, 3, rng.randrange(-40, 40)))
+        a = rotate_args(n_layers=2, n_pool_pages=3, page_size=4, n_k_heads=2, n_v_heads=2, k_dim=16, v_dim=16, pt_stride=16,
+                        k_cache_stride=tuple(stride[:4]), v_cache_stride=tuple(other[:4]), v_cache=0x30000000 + 2 * apart, q=None,
+                        q_out=None, **{"rope.rope_dim": 16})
+        code = km.lib().kamera_validate_latent(0, ctypes.byref(a))
+        assert code in (km.OK, km.ERR_ALIAS), km.last_error()
+        if code == km.OK:
+            allowed += 1
+            assert not _elements(0, stride, sizes, 16) & _elements(apart, other, sizes, 16), (stride, other, apart)
+    assert allowed > 500
 
 
 def test_launches_past_32_bits_of_threads_are_refused():
