@@ -13,12 +13,15 @@
 // Softmax in powers of two (scale * log2 e folded in), fp32.  A row's running maximum
 // moves only when a score passes it by more than 8.
 //
-// Bound by issue: five vector instructions for each MFMA, which keeps the matrix pipe
-// busy 45% of the time with two workgroups a CU (81,920 bytes of LDS each, all there
-// is).  1024 queries of 16 heads over 16384 keys: 172 us, 970 TFLOP/s; eight ragged
-// prompts of up to 1024 queries over up to 2048 keys, 1024 tasks of 1 to 32 tiles: 101 us,
-// where taking a task up and storing its results (some 14000 cycles) weighs as much as
-// its tiles.
+// Neither pipe is full: with two workgroups a CU (81,920 bytes of LDS each, all there is),
+// two waves a SIMD, the matrix pipe is busy 45% of the time and vector instructions, four
+// beside each MFMA, issue 34% of it.  What is missing is their overlap: one wave's exponentials
+// and the other's products run one after the other for the most part.  1024 queries of
+// 16 heads over 16384 keys: 172 us, 970 TFLOP/s; eight ragged prompts of up to 1024
+// queries over up to 2048 keys, 1024 tasks of 1 to 32 tiles: 101 us, of which some 14000
+// cycles a task, as much as its tiles, go to its start (lengths, pages, first loads) and its
+// end, where results are stored as the products leave them, 16 bytes of each of 32 rows at a
+// time.
 
 #include "kamera_mla_device.h"
 

@@ -12,7 +12,8 @@
 //   order, which transposed reads give at no cost.
 // 16 rows a wave and not 32, which would halve the reads of LDS for each product: the
 // results of 32 rows (256 registers) and their queries (144) leave the compiler no room
-// and it spills.
+// and it spills.  16 rows of 512 columns fill the 256 registers of a wave of eight: two of
+// them spill there (12 bytes of scratch a lane), none in the other forms.
 //
 // LDS: a slot holds 32 keys.  16-byte chunks are exchanged by an exclusive-or of their
 // number with a mix of bits 1 .. 3 of the key, so that eight keys' reads of 32 bytes

@@ -402,9 +402,9 @@ int size_mla(const AttendSizes& a, kamera::MlaParams& P, bool& launch, int64_t& 
   if (tasks < 0 || (tasks + 8) * threads > 0xFFFFFFFFLL) return fail(KAMERA_ERR_RANGE, "%s: too many workgroups for one launch", who);
   P.n_tasks = (int32_t)tasks;
   const int unit = P.unit = a.latent ? 32 * kamera::latent_groups(P.row_waves) : 64;
-  // what 256 keys cost, 288 of the latent form (us with none of it, half of it, all, half as much again: eight ragged
-  // prompts, expanded, 143, 123, 115, 116; 64 single queries of 16 heads, latent, 91.0, 89.3, 87.8, 88.0; 16 requests of
-  // two queries of 128 heads 90 with 128 keys, 87.4 with 192, 85.3 with 288, 86.2 with 384)
+  // what 256 keys cost, 288 of the latent form's blocks of 128 rows (us with none of it, half of it, all, half as much
+  // again: eight ragged prompts, expanded, 143, 123, 115, 116; 64 single queries of 16 heads, latent, 91.0, 89.3, 87.8,
+  // 88.0; 16 requests of two queries of 128 heads 90 with 128 keys, 87.4 with 192, 85.3 with 288, 86.2 with 384)
   P.fixed = (a.latent ? 288 : 256) / unit;
   P.lanes = 1;
   while (P.lanes < 64 && P.lanes < P.n_row_blocks) P.lanes *= 2;
@@ -417,10 +417,14 @@ int size_mla(const AttendSizes& a, kamera::MlaParams& P, bool& launch, int64_t& 
     P.n_parts = a.n_parts;
     P.min_units = 1;
   } else if (can && tasks < kamera::kMlaDivideTasks && units > (a.latent ? 6 : 10)) {
-    // Up to 512 keys (latent, 16 rows; expanded) one workgroup is done before a second could have joined its part:
-    // 512 keys, 16 heads 16.0 us whole, 18.0 divided (latent), 22.0 and 25.0 (128 queries, expanded); 1024 keys 23.2
-    // and 17.9, 33.2 and 25.3.  A part is 128 keys of the latent form, which its four groups take at once, else two
-    // units (single queries of 128 heads, 256 keys: 26.2 us, 27.8 in parts of one).
+    // Up to 512 keys (latent, 16 rows; expanded) one workgroup is done before a second could have joined its part.  One
+    // request, us whole / divided: single query of 16 heads, 512 keys 15.4 / 17.3, 640 17.1 / 17.6, 768 18.8 / 17.5;
+    // 128 queries of 16 heads, expanded, 512 keys 20.8 / 20.3, 576 22.2 / 20.7, 1024 31.9 / 22.3.  Blocks of more rows
+    // have shorter units and are divided from fewer keys on: 32 rows, 256 keys 14.0 / 18.1, 320 15.5 / 18.4, 448 18.2 /
+    // 18.5, 512 19.6 / 18.4; 128 rows, 128 keys 22.4 / 25.2, 192 25.9 / 25.5, 256 29.4 / 25.4.  Many requests would gain
+    // from later on: 16 of 128 rows, 192 keys 26.6 / 32.7, 320 33.7 / 33.2; 64 of them, 192 keys 27.7 / 41.8, 512
+    // 46.0 / 48.6.  A part is 128 keys of the latent form, which its four groups take at once, else two units (single
+    // queries of 128 heads, 256 keys: 26.2 us, 27.8 in parts of one).
     P.min_units = unit == 128 ? 1 : 2;
     P.n_parts = (int32_t)std::min<int64_t>(a.latent ? 256 : 512, ceil_div(total, P.min_units));
   }
@@ -461,7 +465,7 @@ int size_expanded(const kamera_attend_expanded_args* a, kamera::MlaParams& P, bo
 }
 
 // Checks, ranges and parameters of what both take: q, out, lse, page table, pool, workspace.
-// in[0 .. n_in) are filled by the caller; five more are added.
+// in[0 .. n_in) are filled by the caller; six more are added.
 template <typename A>
 int build_mla(const A* a, int32_t dim, const void* pool, const int64_t* pool_s, int32_t pool_cols, Range* in, int n_in,
               int64_t workspace, kamera::MlaParams& P, const char* who) {

@@ -74,8 +74,12 @@ struct ProjectParams {
 
 // From so many (request, head, row block) tasks on a workgroup takes one whole.  Whole tasks keep the row blocks of a
 // head, which read the same keys, together in time; divided ones end together.  Which counts for more depends on lengths
-// that the host does not know: prompts of 1024 queries over 4096 keys, 2048 equal tasks 622 us whole, 738 divided, 1024
-// tasks 319 and 353; ragged prompts, 1024 tasks 146 and 122, 2048 tasks 238 and 197.
+// that the host does not know (us whole / divided).  Expanded: prompts of 1024 queries over 4096 keys, 2048 equal tasks
+// 622 / 738, 1024 tasks 319 / 353; ragged prompts, 1024 tasks 146 / 122, 2048 tasks 238 / 197, 4096 of 16 requests 602 /
+// 467; 128 heads, two prompts of 1024 (2048 tasks) 150 / 139, four ragged ones (6656) 486 / 247.  Latent: 2048 single
+// queries of 16 heads over 1024 keys 441 / 488, over 1 to 2047 484 / 496, over 1 to 8191 1647 / 1629; of 128 heads over
+// 2048 keys 1412 / 1425, over 1 to 4095 1673 / 1499; 64 prompts of 64 queries of 128 heads (4096 tasks) 1275 / 1392,
+// ragged 1303 / 1448.
 constexpr int kMlaDivideTasks = 2048;
 
 // Latent form: waves of a workgroup whose row blocks are `row_waves` waves (of 16 rows) high,

@@ -52,7 +52,7 @@ __global__ __launch_bounds__(WAYS > 1 ? WAYS * 32 : 256) void mla_join_kernel(Ml
   if (w0 == w1 || (!by_task && (int)blockIdx.x != w0)) return;     // one workgroup had it all, or not its first range
   const int quarters = (p.dim + 127) >> 7, cq = blockIdx.y % quarters;
   const int rr = blockIdx.y / quarters * (WAYS > 1 ? 1 : 8 * OWN) + (WAYS > 1 ? 0 : tid >> 5);
-  if (blk.row_first + rr >= blk.row_end) return;   // of all 256 threads where they meet in LDS
+  if (blk.row_first + rr >= blk.row_end) return;   // of all threads where they meet in LDS
   const int c0 = cq * 128 + col * 4;
   const bool there = c0 < p.dim;
   // the first part is its workgroup's first segment only where that's range begins with it
